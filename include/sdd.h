@@ -44,6 +44,7 @@ typedef struct ihipStream_t* sdd_stream_t; /* a hipStream_t; NULL = default stre
 /* element types */
 #define SDD_F32 0
 #define SDD_BF16 1
+#define SDD_E4M3 2 /* paged caches only */
 
 /* acceptance modes (Sec. 3.1; Appendix "Baselines and Sweep Settings") */
 #define SDD_GREEDY 0  /* accept x^_j iff it is the target argmax (lowest index on ties) */
@@ -230,6 +231,91 @@ int sdd_verify_full(sdd_model* m, sdd_kv* scratch, const int32_t* tokens, int n,
  * token outside [0, vocab) (sticky bit0) leave that sequence unchanged. */
 int sdd_kv_commit(sdd_kv* kv, const int32_t* seq_ids, int n_seq, const int32_t* accepted_len,
                   const int32_t* next_token, sdd_stream_t stream);
+/* ---- paged KV cache ------------------------------------------------------ */
+
+/* A pool of pages for one layer, in a caller-owned device buffer of
+ * sdd_pages_bytes() bytes (256-byte aligned).  A page holds page_size positions
+ * of every KV head; the pages of a sequence, in any order and anywhere in the
+ * pool, are the entries of its row of a block table (device int32
+ * [B][table_width]): position p lies in page table[b][p / page_size].  Several
+ * sequences may hold the same page (a common prefix); rows appended to it by
+ * more than one of them in one call leave one of the values, any of them.
+ * Stored order, for callers that move pages themselves: head h of page p starts
+ * at byte (p * n_kv_heads + h) * head_bytes with K (page_size * head_dim
+ * elements), V (as many) and, for SDD_E4M3, page_size scale bytes of K and of V
+ * (head_bytes is the sum).  K and V are 32-position steps; position
+ * 32 s + 8 a + 4 b + i (a < 4, b < 2, i < 4), dimension d, is element
+ *   bf16  K[s][b][d / 32][d % 32 / 8][a][i][d % 8]     V[s][d / 16][a][d % 16][4 b + i]
+ *   e4m3  K[s][b][d / 64][d % 64 / 16][a][i][d % 16]   V[s][d / 32][a][d % 16][d % 32 / 16][4 b + i]
+ * A row (position, head, side) of an e4m3 pool stands for its codes (OCP e4m3:
+ * no infinities) times 2^(scale byte - 127), scale bytes being 1..254. */
+typedef struct {
+  int n_kv_heads, head_dim; /* head_dim 64 or 128 */
+  int page_size;            /* positions: a power of two in [32, 1024] */
+  int dtype;                /* SDD_BF16 or SDD_E4M3 */
+  int n_pages;
+  void* pages; /* device */
+} sdd_pages;
+
+/* Bytes of the pool's buffer (pg->pages is not read).  Errors: SDD_EINVAL,
+ * SDD_EUNSUPPORTED (head_dim). */
+int sdd_pages_bytes(const sdd_pages* pg, size_t* bytes);
+
+/* Cosines and sines of the rotation: table fp32 [max_pos][head_dim / 2][2] (device)
+ * of the angles pos * theta^(-2 j / head_dim), computed in double precision. */
+int sdd_rope_table(float* table, int max_pos, int head_dim, float theta, sdd_stream_t stream);
+
+/* Common to the calls on a pool.  len (device int32 [B]) is the position of each
+ * sequence's first row of the call, i.e. what its cache holds before it; row r
+ * of sequence b is position len[b] + r.  A negative len marks a padded slot: its
+ * outputs are left as they were.  So are those of a sequence whose rows do not
+ * fit (past table_width pages, the rotation table, or max_len), which sets bit0
+ * of the sticky error word err (device int32, caller-zeroed; may be NULL).  A
+ * page id outside [0, n_pages) sets bit2 and is never followed: nothing is
+ * written there, attention does not see its positions, and reads give zeros. */
+
+/* Writes R new rows of each of B sequences into the pages.  qkv: rows
+ * [B * R][(n_q_heads + 2 n_kv_heads) * head_dim] (q heads, then k, then v;
+ * SDD_BF16 or SDD_F32), row_stride elements apart, 16-byte aligned.  q and k heads are
+ * normed (x / sqrt(mean x^2 + eps) * gain, gains fp32 [head_dim]; NULL both: no
+ * norm) and rotated (rotate-half; rope a table of sdd_rope_table with max_pos
+ * positions; NULL: no rotation), all in fp32.  q goes to q_out bf16
+ * [B][R][n_q_heads][head_dim]; k and v go to the pages, rounded once: to bf16,
+ * or to e4m3 codes of y 2^-e with e the smallest exponent that brings the row
+ * within +-448.  A row with an infinity or NaN becomes NaN codes.  Errors:
+ * SDD_EINVAL (NULL pointer, bad shape, misaligned), SDD_EUNSUPPORTED. */
+int sdd_paged_append(const sdd_pages* pg, const int32_t* table, int table_width, const int32_t* len, int B, int R,
+                     int n_q_heads, const void* qkv, int qkv_dtype, size_t row_stride, const float* q_gain,
+                     const float* k_gain, float eps, const float* rope, int max_pos, uint16_t* q_out, int32_t* err,
+                     sdd_stream_t stream);
+
+/* Workspace of sdd_paged_attention for calls of at most max_len positions a
+ * sequence (0: none is needed).  It needs no initialization and carries nothing
+ * from one call to the next. */
+int sdd_paged_attention_workspace_bytes(const sdd_pages* pg, int B, int R, int n_q_heads, int max_len, size_t* bytes);
+
+/* Causal attention of R rows (their own K/V appended before) of each of B
+ * sequences: out[b][r][h] = sum_p w_p v_p / sum_p w_p, w_p = exp(scale q.k_p), over
+ * the positions p <= len[b] + r; query head h reads KV head h / (n_q_heads /
+ * n_kv_heads).  q, out: bf16 [B][R][n_q_heads][head_dim].  R = 1 is a decode
+ * step, R = gamma + 1 a block's verification, a larger R a chunk of a prompt.
+ * max_len: no sequence's len + R is larger (a longer one is refused); the
+ * host's bound sizes the launch, so that a captured call serves all lengths up
+ * to it.  A row that sees nothing (its pages are invalid) gives zeros.  Sums and
+ * softmax statistics are fp32 and in a fixed order: results are
+ * bit-reproducible and do not depend on the other sequences of the call (they
+ * do on R, whose rows share work).  Errors: SDD_EINVAL, SDD_ENOMEM (small
+ * workspace), SDD_EUNSUPPORTED. */
+int sdd_paged_attention(const sdd_pages* pg, const int32_t* table, int table_width, const int32_t* len, int B, int R,
+                        int n_q_heads, const uint16_t* q, float scale, int max_len, uint16_t* out, int32_t* err,
+                        void* ws, size_t ws_bytes, sdd_stream_t stream);
+
+/* Reads positions start[b] .. start[b] + n - 1 of each of B sequences back:
+ * k, v bf16 [B][n][n_kv_heads][head_dim].  Exact for bf16 pools, and for e4m3 ones
+ * where the value is a normal bf16 number. */
+int sdd_paged_read(const sdd_pages* pg, const int32_t* table, int table_width, const int32_t* start, int B, int n,
+                   uint16_t* k, uint16_t* v, int32_t* err, sdd_stream_t stream);
+
 /* ---- acceptance and confidence ---------------------------------------- */
 
 /* Workspace bytes for sdd_accept / sdd_confidence_prefix at these shapes
@@ -294,6 +380,29 @@ int sdd_confidence_prefix(const void* logits, int dtype, size_t seq_stride, int 
                           int V, float tau, int32_t* skip_len, float* log_conf,
                           const int32_t* draft, float* log_p_draft, void* ws, size_t ws_bytes,
                           sdd_stream_t stream);
+
+/* ---- token log probabilities --------------------------------------------- */
+
+/* Workspace bytes for sdd_token_logprobs over up to n_rows rows and n_top
+ * alternatives (zeroed once by sdd_workspace_init; calls leave it reusable by
+ * calls of other shapes up to these). */
+int sdd_logprobs_workspace_bytes(int n_rows, int V, int n_top, size_t* bytes);
+
+/* What a served answer reports beside its tokens.  Row r of sequence b at logits +
+ * b * seq_stride + r * V elements (SDD_F32 or SDD_BF16).  Outputs (device):
+ *   logprob      fp32 [B][R]: log softmax at tokens[b][r] (int32; both NULL: none);
+ *                NaN for a token outside [0, V)
+ *   entropy      fp32 [B][R]: -sum p ln p (may be NULL)
+ *   top          int32 [B][R][n_top]: the n_top largest logits' tokens, largest
+ *                first, lowest index on ties; top_logprob fp32: theirs
+ * Logits of -inf are tokens of probability 0: log probability -inf, no
+ * alternative; where fewer than n_top others are left the rest of top is -1 and
+ * of top_logprob -inf.  A row with a NaN or +inf, or with nothing above -inf, has
+ * no distribution: NaN, NaN, -1, NaN.  Errors: SDD_EINVAL (NULL pointer, bad
+ * shape or dtype, n_top outside [0, 32]), SDD_ENOMEM (small workspace). */
+int sdd_token_logprobs(const void* logits, int dtype, size_t seq_stride, int B, int R, int V, const int32_t* tokens,
+                       int n_top, float* logprob, float* entropy, int32_t* top, float* top_logprob, void* ws,
+                       size_t ws_bytes, sdd_stream_t stream);
 
 /* ---- skip scheduler ------------------------------------------------------ */
 
@@ -397,6 +506,8 @@ int sdd_survival_mlp(const sdd_mlp* m, const uint16_t* hidden, const float* scal
 #define SDD_PROF_CONF 256u
 #define SDD_PROF_SCHED 512u
 #define SDD_PROF_MLP 1024u
+#define SDD_PROF_LOGPROBS 2048u
+#define SDD_PROF_PAGES 4096u /* paged cache: append and read (its attention: SDD_PROF_ATTN) */
 
 /* Starts timing: until sdd_profile_stop, every every-th launch (1: each) of
  * the classes in class_mask is bracketed by two HIP events on its own stream

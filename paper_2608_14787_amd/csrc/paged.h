@@ -1,0 +1,76 @@
+// Paged KV cache: device descriptor and stored order, shared by the operators on it (internal to libsdd).
+#pragma once
+
+#include "model.h"
+
+namespace sdd {
+
+// Sticky bits of the operators' error word (those of sdd_kv_state).
+constexpr int kErrCapacity = 1, kErrId = 4;
+
+// A pool of pages as the kernels see it.  The bytes of head h of page p start at (p * hkv + h) * head_bytes: K, V (side
+// bytes each), then for e4m3 a scale byte per position of K and of V.
+struct PageDesc {
+  char* base;
+  const int32_t* table;  // [B][width] page of positions page_size i ..
+  int width, n_pages, hkv, log_page;
+  int side;        // page_size * head_dim * element size
+  int head_bytes;  // 2 side, + 2 page_size for e4m3
+};
+
+// Checks a pool's description; fills everything but the table.
+int page_desc(const sdd_pages* pg, PageDesc* d);
+
+__device__ inline char* page_head(const PageDesc& d, int page, int h) {
+  return d.base + ((int64_t)page * d.hkv + h) * d.head_bytes;
+}
+
+// Stored order of a side of a page: steps of 32 positions, each the list of 1 KiB blocks that one attention step loads
+// with one 16-byte load per lane.  Position p, dimension c (offsets in bytes from the side's start):
+//   bf16  K block b * hd/32 + kk, lane 16 g + rho: dimensions 32 kk + 8 g .. + 7 of position kv_row(rho, b)
+//         V block db,             lane 16 g + rho: positions 8 g .. 8 g + 7 of dimension 16 db + rho
+//   e4m3  K block b * hd/64 + j,  lane 16 g + rho: dimensions 64 j + 16 g .. + 15 of position kv_row(rho, b)
+//         V block jj,             lane 16 g + rho: positions 8 g .. 8 g + 7 of dimension 32 jj + rho, then of 32 jj + 16 + rho
+// where kv_row(rho, b) = 8 (rho / 4) + 4 b + rho % 4 is the position that K sub-tile b feeds to MFMA row rho: the scores
+// then leave lane group g on the positions 8 g .. 8 g + 7 of its V entries.
+template <bool E4, int HD>
+__device__ inline int page_k_offset(int p, int c) {
+  const int i = p % 32, rho = 4 * (i / 8) + i % 4, b = (i / 4) % 2;
+  if constexpr (E4) return p / 32 * 32 * HD + (b * (HD / 64) + c / 64) * 1024 + (16 * (c % 64 / 16) + rho) * 16 + c % 16;
+  return p / 32 * 64 * HD + (b * (HD / 32) + c / 32) * 1024 + (16 * (c % 32 / 8) + rho) * 16 + c % 8 * 2;
+}
+template <bool E4, int HD>
+__device__ inline int page_v_offset(int p, int c) {
+  const int i = p % 32;
+  if constexpr (E4) return p / 32 * 32 * HD + c / 32 * 1024 + (16 * (i / 8) + c % 16) * 16 + c % 32 / 16 * 8 + i % 8;
+  return p / 32 * 64 * HD + c / 16 * 1024 + (16 * (i / 8) + c % 16) * 16 + i % 8 * 2;
+}
+
+// e4m3 rows are stored as codes of y 2^-e and a scale byte e + 127, e the smallest exponent with max |y| <= 448 2^e
+// (1 <= e + 127 <= 254; a row of zeros has 127).  A power of two, so that the only rounding is the codes'.  A row that
+// holds an infinity or a NaN is stored as NaN codes (0x7f) with byte 127.
+__device__ inline int scale_byte(float amax) {
+  if (!(amax > 0.f)) return 127;
+  const uint32_t u = __builtin_bit_cast(uint32_t, amax);
+  // amax = f 2^x, f in [1, 2); 448 = 1.75 2^8
+  const int x = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u);
+  return max(1, min(254, x + 127));
+}
+__device__ inline float scale_value(int byte) { return __builtin_bit_cast(float, (uint32_t)byte << 23); }
+
+// ---- attention over a pool (paged_attn.hip) ------------------------------------------------------------
+struct PagedAttnArgs {
+  PageDesc pg;
+  const int32_t* len;   // [B] positions before the rows; < 0: the sequence is skipped
+  const RowInfo* rows;  // instead of len: row b R holds the sequence (its table row), position and validity
+  const uint16_t* q;    // [B][R][hq][hd]
+  uint16_t* out;        // the same, or fragment-major rows (frag)
+  int frag;
+  int B, R, hq, grp, max_len;
+  float scale;  // of the scores, times log2(e)
+  int32_t* err;
+  int qtiles, splits, max_splits;
+  float* part;  // partial results
+};
+
+}  // namespace sdd

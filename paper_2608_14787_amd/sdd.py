@@ -15,7 +15,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libsdd.so")
 
 OK, EINVAL, ENOMEM, EHIP, ECAPACITY, EUNSUPPORTED = 0, -1, -2, -3, -4, -5
-F32, BF16 = 0, 1
+F32, BF16, E4M3 = 0, 1, 2
 GREEDY, RATIO, TOPK, LENIENT, RATIO_SAMPLE = 0, 1, 2, 3, 4
 (T_EMBED, T_LM_HEAD, T_FINAL_NORM, T_WQ, T_WK, T_WV, T_WO, T_WGATE, T_WUP, T_WDOWN,
  T_ATTN_NORM, T_FFN_NORM, T_Q_NORM, T_K_NORM) = range(14)
@@ -71,6 +71,14 @@ _SIGS = {
     "sdd_audit_accumulate": (I, [P, P, I, P, P]),
     "sdd_survival_workspace_bytes": (I, [P, I, P]),
     "sdd_survival_mlp": (I, [P, P, P, I, P, P, P, SZ, P]),
+    "sdd_pages_bytes": (I, [P, P]),
+    "sdd_rope_table": (I, [P, I, I, F, P]),
+    "sdd_paged_append": (I, [P, P, I, P, I, I, I, P, I, SZ, P, P, F, P, I, P, P, P]),
+    "sdd_paged_attention_workspace_bytes": (I, [P, I, I, I, I, P]),
+    "sdd_paged_attention": (I, [P, P, I, P, I, I, I, P, F, I, P, P, P, SZ, P]),
+    "sdd_paged_read": (I, [P, P, I, P, I, I, P, P, P, P]),
+    "sdd_logprobs_workspace_bytes": (I, [I, I, I, P]),
+    "sdd_token_logprobs": (I, [P, I, SZ, I, I, I, P, I, P, P, P, P, P, SZ, P]),
     "sdd_profile_start": (I, [C.c_uint, I, I]),
     "sdd_profile_read": (I, [C.c_uint, P, P, P, P]),
     "sdd_profile_stop": (I, []),
@@ -78,7 +86,7 @@ _SIGS = {
 
 PROF_EMBED, PROF_GEMM_QKV, PROF_ATTN, PROF_GEMM_O = 1, 2, 4, 8
 PROF_GEMM_GATEUP, PROF_GEMM_DOWN, PROF_GEMM_LM, PROF_ACCEPT, PROF_CONF = 16, 32, 64, 128, 256
-PROF_SCHED, PROF_MLP = 512, 1024
+PROF_SCHED, PROF_MLP, PROF_LOGPROBS, PROF_PAGES = 512, 1024, 2048, 4096
 SIG_RAW, SIG_MARGINAL, SIG_CONDITIONAL = 0, 1, 2
 (SKIP_OK, SKIP_STALE, SKIP_NO_CANDIDATE, SKIP_SHORT, SKIP_SHORT_BLOCK, SKIP_SPECIAL,
  SKIP_REPEAT) = range(7)
@@ -217,6 +225,39 @@ def confidence_prefix(logits: torch.Tensor, gamma: int, tau: float, *, draft=Non
     return sk, (lc[:, :gamma] if lc is not None else None), (lp[:, :gamma] if lp is not None else None)
 
 
+def logprobs_workspace(n_rows: int, V: int, n_top: int, device="cuda") -> torch.Tensor:
+    ws = torch.empty(_size_out(lib().sdd_logprobs_workspace_bytes, n_rows, V, n_top), dtype=torch.uint8, device=device)
+    workspace_init(ws)
+    return ws
+
+
+def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, n_top: int = 0, *,
+                   ws: torch.Tensor | None = None, out=None, stream=None):
+    """sdd_token_logprobs over logit rows [B, R, V]: log probabilities of tokens int32 [B, R], entropies, alternatives.
+
+    Returns (logprob, entropy) fp32 [B, R] (logprob None without tokens) and, with n_top, (top int32, top_logprob
+    fp32) [B, R, n_top] as well; `out` gives the tensors to write into, in that order."""
+    B, R, V = logits.shape
+    _rows(logits, "logits")
+    _i32(tokens, "tokens", allow_none=True)
+    _need(tokens is None or tokens.numel() == B * R, "tokens must be [B, R]")
+    if ws is None:
+        ws = logprobs_workspace(B * R, V, n_top, logits.device)
+    if out is None:
+        new = lambda *shape, dtype=torch.float32: torch.empty(*shape, dtype=dtype, device=logits.device)
+        out = (new(B, R) if tokens is not None else None, new(B, R))
+        if n_top:
+            out += (new(B, R, n_top, dtype=torch.int32), new(B, R, n_top))
+    lp, ent, top, top_lp = tuple(out) + (None,) * (4 - len(out))
+    for t, nm, n in ((lp, "logprob", B * R), (ent, "entropy", B * R), (top_lp, "top_logprob", B * R * n_top)):
+        _need(t is None or (t.dtype == torch.float32 and t.is_contiguous() and t.numel() == n), f"{nm} must be contiguous fp32, {n} values")
+    _i32(top, "top", allow_none=n_top == 0)
+    _need(top is None or top.numel() == B * R * n_top, "top must be [B, R, n_top]")
+    _check(lib().sdd_token_logprobs(_ptr(logits), _dtype_code(logits), logits.stride(0), B, R, V, _ptr(tokens), n_top,
+                                    _ptr(lp), _ptr(ent), _ptr(top), _ptr(top_lp), _ptr(ws), ws.numel(), _stream(stream)))
+    return out
+
+
 def schedule(log_q: torch.Tensor, D: torch.Tensor, signal: int, eta_b: float, eta_c: float, *,
              k_min: int = 0, s_max: int = 1 << 30, draft=None, block_len=None, special=None,
              rep_max: int = 0, out=None, stream=None):
@@ -289,6 +330,105 @@ def profile_read(cls: int):
 
 def profile_stop():
     _check(lib().sdd_profile_stop())
+
+
+# ---- paged KV cache -------------------------------------------------------------------------
+
+
+class PagesDesc(C.Structure):
+    _fields_ = [("n_kv_heads", C.c_int), ("head_dim", C.c_int), ("page_size", C.c_int), ("dtype", C.c_int),
+                ("n_pages", C.c_int), ("pages", P)]
+
+
+def rope_table(max_pos: int, head_dim: int, theta: float, device="cuda", stream=None) -> torch.Tensor:
+    """Rotation table fp32 [max_pos, head_dim / 2, 2] (cos, sin)."""
+    t = torch.empty((max_pos, head_dim // 2, 2), dtype=torch.float32, device=device)
+    _check(lib().sdd_rope_table(_ptr(t), max_pos, head_dim, theta, _stream(stream)))
+    return t
+
+
+class PagePool:
+    """One layer's pages of KV cache (sdd_pages) in a torch-owned device buffer; dtype "bf16" or "e4m3".
+
+    Sequences are rows of a block table int32 [B, width] of page ids; lens int32 [B] is each sequence's cached length
+    before the call (negative: a padded slot, left alone).  err: an int32 tensor of one sticky error word, or None."""
+
+    def __init__(self, n_pages: int, n_kv_heads: int, head_dim: int, page_size: int = 64, dtype: str = "bf16",
+                 device="cuda", buf: torch.Tensor | None = None):
+        _need(dtype in ("bf16", "e4m3"), f"dtype must be bf16 or e4m3, got {dtype}")
+        self.n_kv_heads, self.head_dim, self.page_size = n_kv_heads, head_dim, page_size
+        self.desc = PagesDesc(n_kv_heads, head_dim, page_size, BF16 if dtype == "bf16" else E4M3, n_pages, None)
+        n = _size_out(lib().sdd_pages_bytes, C.byref(self.desc))
+        if buf is None:
+            buf = torch.empty(n, dtype=torch.uint8, device=device)
+        _need(buf.is_contiguous() and buf.numel() * buf.element_size() >= n, f"buf must be contiguous and hold {n} bytes")
+        self.buf = buf
+        self.desc.pages = buf.data_ptr()
+
+    def _seqs(self, table, lens, rows):
+        _i32(table, "table")
+        _i32(lens, "lens")
+        _need(table.dim() == 2 and lens.numel() == rows and table.shape[0] >= rows, "table must be [B, width] and lens [B]")
+
+    def append(self, qkv: torch.Tensor, n_q_heads: int, table: torch.Tensor, lens: torch.Tensor, *, q_norm=None, k_norm=None,
+               eps: float = 1e-6, rope: torch.Tensor | None = None, q_out=None, err=None, stream=None) -> torch.Tensor:
+        """sdd_paged_append of qkv [B, R, (n_q_heads + 2 n_kv_heads) * head_dim]; returns q bf16 [B, R, n_q_heads, head_dim]."""
+        B, R, n = qkv.shape
+        self._seqs(table, lens, B)
+        _need(n == (n_q_heads + 2 * self.n_kv_heads) * self.head_dim, "qkv must be [B, R, (n_q_heads + 2 n_kv_heads) * head_dim]")
+        _need(qkv.stride(2) == 1 and (B == 1 or R == 1 or qkv.stride(0) == R * qkv.stride(1)), "qkv rows must be evenly spaced")
+        for t, nm in ((q_norm, "q_norm"), (k_norm, "k_norm")):
+            _need(t is None or (t.dtype == torch.float32 and t.is_contiguous() and t.numel() == self.head_dim), f"{nm} must be fp32 [head_dim]")
+        _need(rope is None or (rope.dtype == torch.float32 and rope.is_contiguous() and rope.shape[1:] == (self.head_dim // 2, 2)),
+              "rope must be contiguous fp32 [max_pos, head_dim / 2, 2]")
+        _i32(err, "err", allow_none=True)
+        if q_out is None:
+            q_out = torch.empty((B, R, n_q_heads, self.head_dim), dtype=torch.bfloat16, device=qkv.device)
+        _need(q_out.dtype == torch.bfloat16 and q_out.is_contiguous() and q_out.numel() == B * R * n_q_heads * self.head_dim,
+              "q_out must be contiguous bf16 [B, R, n_q_heads, head_dim]")
+        _check(lib().sdd_paged_append(C.byref(self.desc), _ptr(table), table.shape[1], _ptr(lens), B, R, n_q_heads, _ptr(qkv),
+                                      _dtype_code(qkv), qkv.stride(1) if R > 1 else qkv.stride(0) if B > 1 else n,
+                                      _ptr(q_norm), _ptr(k_norm), eps, _ptr(rope), 0 if rope is None else rope.shape[0],
+                                      _ptr(q_out), _ptr(err), _stream(stream)))
+        return q_out
+
+    def attention_workspace(self, B: int, R: int, n_q_heads: int, max_len: int) -> torch.Tensor:
+        n = _size_out(lib().sdd_paged_attention_workspace_bytes, C.byref(self.desc), B, R, n_q_heads, max_len)
+        return torch.empty(n, dtype=torch.uint8, device=self.buf.device)
+
+    def attention(self, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, *, max_len: int = 0,
+                  scale: float | None = None, out=None, ws=None, err=None, stream=None) -> torch.Tensor:
+        """sdd_paged_attention of q bf16 [B, R, n_q_heads, head_dim] (rows at lens .. lens + R - 1, appended before); same
+        shape returned.  max_len bounds lens + R (default: what the table can hold); scale defaults to head_dim^-1/2."""
+        B, R, H, hd = q.shape
+        self._seqs(table, lens, B)
+        _need(q.dtype == torch.bfloat16 and q.is_contiguous() and hd == self.head_dim, "q must be contiguous bf16 [B, R, n_q_heads, head_dim]")
+        max_len = max_len or table.shape[1] * self.page_size
+        if ws is None:
+            ws = self.attention_workspace(B, R, H, max_len)
+        if out is None:
+            out = torch.empty_like(q)
+        _need(out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == q.numel(), "out must be contiguous bf16 like q")
+        _i32(err, "err", allow_none=True)
+        _check(lib().sdd_paged_attention(C.byref(self.desc), _ptr(table), table.shape[1], _ptr(lens), B, R, H, _ptr(q),
+                                         hd ** -0.5 if scale is None else scale, max_len, _ptr(out), _ptr(err), _ptr(ws),
+                                         ws.numel(), _stream(stream)))
+        return out
+
+    def read(self, table: torch.Tensor, start: torch.Tensor, n: int, *, out=None, err=None, stream=None):
+        """sdd_paged_read of positions start .. start + n - 1: (k, v) bf16 [B, n, n_kv_heads, head_dim]."""
+        B = start.numel()
+        self._seqs(table, start, B)
+        if out is None:
+            shape = (B, n, self.n_kv_heads, self.head_dim)
+            out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=self.buf.device) for _ in range(2))
+        for t in out:
+            _need(t.dtype == torch.bfloat16 and t.is_contiguous() and t.numel() == B * n * self.n_kv_heads * self.head_dim,
+                  "k and v must be contiguous bf16 [B, n, n_kv_heads, head_dim]")
+        _i32(err, "err", allow_none=True)
+        _check(lib().sdd_paged_read(C.byref(self.desc), _ptr(table), table.shape[1], _ptr(start), B, n, _ptr(out[0]),
+                                    _ptr(out[1]), _ptr(err), _stream(stream)))
+        return tuple(out)
 
 
 # ---- decoder ------------------------------------------------------------------------------
