@@ -274,6 +274,30 @@ int sdd_rope_table(float* table, int max_pos, int head_dim, float theta, sdd_str
  * page id outside [0, n_pages) sets bit2 and is never followed: nothing is
  * written there, attention does not see its positions, and reads give zeros. */
 
+/* A decoder's KV cache in pages, for bf16 models: one pool of n_pages pages a
+ * layer, page ids meaning the same page in each of them, and one block table
+ * (device int32 [max_batch][ceil(max_len / page_size)], caller-owned, read by
+ * every call and kept up to date by the caller, ordered with the calls on their
+ * stream).  The handle takes the place of sdd_kv_create's in every call:
+ * prefill, verify (and decode, gamma = 0), full recompute, commit, state.  A
+ * sequence needs pages for the positions that a call writes (len + gamma + 1);
+ * missing ones (ids outside [0, n_pages)) set sticky bit2 and are not seen.
+ * Results equal the contiguous cache's up to rounding: q, k and v pass through
+ * fp32 rows, norms and rotation being a launch of their own (sdd_paged_append),
+ * and the attention (sdd_paged_attention) adds in its own order; SDD_E4M3 pages
+ * round K and V to 8 bits besides.  Errors: SDD_EINVAL, SDD_ENOMEM,
+ * SDD_EUNSUPPORTED (fp32 model). */
+int sdd_paged_kv_bytes(const sdd_model_config* cfg, int max_batch, int max_len, int page_size, int dtype, int n_pages,
+                       size_t* bytes);
+int sdd_paged_kv_create(sdd_model* m, int max_batch, int max_len, int page_size, int dtype, int n_pages,
+                        const int32_t* table, void* buf, size_t bytes, sdd_stream_t stream, sdd_kv** out);
+/* The pool of one layer of a paged cache (for sdd_paged_read, or for moving pages). */
+int sdd_kv_pages(const sdd_kv* kv, int layer, sdd_pages* out);
+/* Workspace for calls of up to max_rows rows on this cache: sdd_workspace_bytes,
+ * and for a paged one room for the projection's rows and the attention's
+ * partial results. */
+int sdd_kv_workspace_bytes(const sdd_kv* kv, int max_rows, size_t* bytes);
+
 /* Writes R new rows of each of B sequences into the pages.  qkv: rows
  * [B * R][(n_q_heads + 2 n_kv_heads) * head_dim] (q heads, then k, then v;
  * SDD_BF16 or SDD_F32), row_stride elements apart, 16-byte aligned.  q and k heads are

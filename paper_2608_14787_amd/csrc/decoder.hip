@@ -30,6 +30,7 @@
 #include <new>
 
 #include "gemm.h"
+#include "paged.h"
 
 namespace sdd {
 
@@ -1292,7 +1293,104 @@ struct CallCtx {
   char* ws;
   WsLayout L;
   hipStream_t st;
+  size_t paged;  // offset of the paged cache's part of the workspace
 };
+
+// A paged cache's part of the workspace for nb blocks of R rows: the projection's rows (fp32), the column maxima that its
+// epilogue leaves, and the attention's partial results.
+struct PagedWs {
+  size_t amax_v, amax_i, part, total;
+};
+static PagedAttnArgs paged_attn_shape(const sdd_kv* kv, int nb, int R) {
+  const sdd_model_config& c = kv->m->cfg;
+  PagedAttnArgs a{};
+  a.B = nb;
+  a.R = R;
+  a.hq = c.n_q_heads;
+  a.grp = c.n_q_heads / c.n_kv_heads;
+  a.max_len = kv->max_len;
+  a.pg.hkv = c.n_kv_heads;
+  return a;
+}
+static PagedWs paged_ws(const sdd_kv* kv, int nb, int R, size_t part_bytes) {
+  const sdd_model* m = kv->m;
+  const sdd_model_config& c = m->cfg;
+  const size_t mp = align_up((size_t)nb * R, 16), N = (size_t)(c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim;
+  PagedWs p{};
+  p.amax_v = align_up(mp * N * 4, 256);
+  p.amax_i = p.amax_v + align_up((size_t)m->plan_qkv.G * mp * 4, 256);
+  p.part = p.amax_i + align_up((size_t)m->plan_qkv.G * mp * 4, 256);
+  p.total = align_up(p.part + part_bytes, 256);
+  return p;
+}
+// Partial results of nb blocks of R rows; of nb blocks of up to R rows (fewer rows may be cut into more chunks).
+static size_t paged_part(const sdd_kv* kv, int nb, int R) {
+  return paged_attn_workspace(paged_attn_shape(kv, nb, R), kv->m->cfg.head_dim);
+}
+static size_t paged_part_upto(const sdd_kv* kv, int nb, int R) {
+  size_t most = 0;
+  for (int r = 1; r <= R; ++r) {
+    const size_t n = paged_part(kv, nb, r);
+    if (n == 0) break;  // blocks of this many rows are not cut, nor are larger ones
+    most = std::max(most, n);
+  }
+  return most;
+}
+// What a call of nb blocks of R rows needs, and a prefill whose chunks are of at most R rows; 0 for a contiguous cache.
+static size_t paged_bytes(const sdd_kv* kv, int nb, int R) { return kv->page_size ? paged_ws(kv, nb, R, paged_part(kv, nb, R)).total : 0; }
+static size_t paged_chunk_bytes(const sdd_kv* kv, int R) { return kv->page_size ? paged_ws(kv, 1, R, paged_part_upto(kv, 1, R)).total : 0; }
+// What a prefill's chunks of at most R rows leave of a workspace for their layout: a paged cache's part sits at its end.
+static size_t prefill_room(const sdd_kv* kv, int R, size_t bytes) {
+  const size_t p = paged_chunk_bytes(kv, R);
+  return p == 0 ? bytes : p < bytes ? (bytes - p) / 256 * 256 : 0;
+}
+static sdd_pages kv_pages(const sdd_kv* kv, int layer) {
+  const sdd_model_config& c = kv->m->cfg;
+  return sdd_pages{c.n_kv_heads, c.head_dim, kv->page_size, kv->page_dtype, kv->n_pages, kv->k + (size_t)layer * kv->layer_stride};
+}
+
+// Head norms, rotation and cache rows of a layer's projection, then its attention, over a paged cache.
+static int paged_layer(CallCtx& cx, int layer, int nb, int R) {
+  sdd_kv* kv = cx.kv;
+  const sdd_model* m = cx.m;
+  const sdd_model_config& c = m->cfg;
+  const sdd_pages pg = kv_pages(kv, layer);
+  const bool e4 = kv->page_dtype == SDD_E4M3;
+  char* pw = cx.ws + cx.paged;
+  PageDesc d{};
+  int rc = page_desc(&pg, &d);
+  if (rc) return rc;
+  d.table = kv->table;
+  d.width = (int)ceil_div(kv->max_len, kv->page_size);
+  AppendArgs a{};
+  a.pg = d;
+  a.rows = reinterpret_cast<const RowInfo*>(cx.ws + cx.L.rowinfo);
+  a.qkv = pw;
+  a.row_stride = (int64_t)(c.n_q_heads + 2 * c.n_kv_heads) * c.head_dim;
+  if (c.qk_norm) {
+    a.q_gain = reinterpret_cast<const float*>(m->base + m->layers[layer].q_norm);
+    a.k_gain = reinterpret_cast<const float*>(m->base + m->layers[layer].k_norm);
+  }
+  a.rope = kv->rope;
+  a.q_out = reinterpret_cast<uint16_t*>(cx.ws + cx.L.q);
+  a.err = kv->err;
+  a.B = nb;
+  a.R = R;
+  a.hq = c.n_q_heads;
+  a.max_pos = kv->max_len;
+  a.eps = c.rms_eps;
+  if ((rc = launch_paged_append(a, c.head_dim, e4, true, cx.st))) return rc;
+  PagedAttnArgs t = paged_attn_shape(kv, nb, R);
+  t.pg = d;
+  t.rows = a.rows;
+  t.q = a.q_out;
+  t.out = reinterpret_cast<uint16_t*>(cx.ws + cx.L.ao);
+  t.frag = 1;
+  t.scale = kLog2e / sqrtf((float)c.head_dim);
+  t.err = kv->err;
+  t.part = reinterpret_cast<float*>(pw + paged_ws(kv, nb, R, 0).part);
+  return launch_paged_attn(t, c.head_dim, e4, cx.st);
+}
 
 template <typename T, int NG, int EPI>
 static void launch_gemm_tb(int tb, const GemmArgs& a, int nblocks, hipStream_t st) {
@@ -1405,7 +1503,7 @@ static int run_gemm(CallCtx& cx, int epi, unsigned prof, size_t w_off, int64_t N
             launch_gemm_ng<uint16_t, EPI_SWIGLU>(ng, tb, a, nblocks, cx.st);
           break;
         default:
-          if (ng == 8 && tb <= 3)
+          if (ng == 8 && tb <= 3 && epi != EPI_ROWS)  // (the two-half kernel is built for shares of several groups)
             launch_gemm_ws<EPI_LOGITS>(tb, a, nblocks, cx.st);
           else
             launch_gemm_ng<uint16_t, EPI_LOGITS>(ng, tb, a, nblocks, cx.st);
@@ -1486,10 +1584,20 @@ static int forward_rows(CallCtx& cx, int nb, int R, float* logits, int32_t* argm
       a.kc = kv->k + (size_t)l * kv->layer_stride;
       a.vc = kv->v + (size_t)l * kv->layer_stride;
       const GemmRef nx{Ly.o, d, (int)hq, m->ng_o};
-      if ((rc = run_gemm(cx, EPI_QKV, PROF_GEMM_QKV, Ly.qkv, hq + 2 * hk, (int)d, xa, a, M, m->ng_qkv, tp.qkv, &nx))) return rc;
+      if (kv->page_size) {
+        const PagedWs p = paged_ws(kv, nb, R, 0);
+        a.logits = reinterpret_cast<float*>(ws + cx.paged);
+        a.V = (int)(hq + 2 * hk);
+        a.amax_v = reinterpret_cast<float*>(ws + cx.paged + p.amax_v);
+        a.amax_i = reinterpret_cast<int*>(ws + cx.paged + p.amax_i);
+        if ((rc = run_gemm(cx, EPI_ROWS, PROF_GEMM_QKV, Ly.qkv, hq + 2 * hk, (int)d, xa, a, M, m->ng_qkv, tp.qkv, &nx))) return rc;
+        if ((rc = paged_layer(cx, l, nb, R))) return rc;
+      } else if ((rc = run_gemm(cx, EPI_QKV, PROF_GEMM_QKV, Ly.qkv, hq + 2 * hk, (int)d, xa, a, M, m->ng_qkv, tp.qkv, &nx))) return rc;
     }
     // attention
-    if (prefill && prefill_attention(m, R)) {
+    if (kv->page_size) {
+      // done above
+    } else if (prefill && prefill_attention(m, R)) {
       AttnPrefillArgs a{};
       a.q = reinterpret_cast<const uint16_t*>(ws + L.q);
       a.kc = reinterpret_cast<const uint16_t*>(kv->k + (size_t)l * kv->layer_stride);
@@ -1698,6 +1806,83 @@ extern "C" int sdd_kv_create(sdd_model* m, int max_batch, int max_len, void* buf
   return SDD_OK;
 }
 
+extern "C" int sdd_paged_kv_bytes(const sdd_model_config* cfg, int max_batch, int max_len, int page_size, int dtype, int n_pages,
+                                  size_t* bytes) {
+  SDD_REQUIRE(cfg && bytes, "NULL pointer");
+  SDD_REQUIRE(max_batch > 0 && max_len > 0 && max_len <= (1 << 30), "bad max_batch/max_len");
+  if (cfg->dtype != SDD_BF16) return fail(SDD_EUNSUPPORTED, "paged caches serve bf16 models");
+  const sdd_pages pg{cfg->n_kv_heads, cfg->head_dim, page_size, dtype, n_pages, nullptr};
+  size_t layer = 0;
+  int rc = sdd_pages_bytes(&pg, &layer);
+  if (rc) return rc;
+  *bytes = align_up((size_t)(2 * max_batch + 1) * 4, 256) + align_up((size_t)max_len * cfg->head_dim * 4, 256) +
+           align_up(layer, 256) * (size_t)std::max(1, cfg->n_layers);
+  return SDD_OK;
+}
+
+extern "C" int sdd_paged_kv_create(sdd_model* m, int max_batch, int max_len, int page_size, int dtype, int n_pages,
+                                   const int32_t* table, void* buf, size_t bytes, sdd_stream_t stream, sdd_kv** out) {
+  SDD_REQUIRE(m && buf && out && table, "NULL pointer");
+  size_t need = 0, layer = 0;
+  int rc = sdd_paged_kv_bytes(&m->cfg, max_batch, max_len, page_size, dtype, n_pages, &need);
+  if (rc) return rc;
+  if (bytes < need) return fail(SDD_ENOMEM, "paged KV buffer needs %zu bytes, got %zu", need, bytes);
+  SDD_REQUIRE((uintptr_t)buf % 256 == 0, "KV buffer must be 256-byte aligned");
+  sdd_kv* kv = new (std::nothrow) sdd_kv();
+  if (!kv) return fail(SDD_ENOMEM, "host allocation failed");
+  const sdd_model_config& c = m->cfg;
+  kv->m = m;
+  kv->max_batch = max_batch;
+  kv->max_len = max_len;
+  kv->base = reinterpret_cast<char*>(buf);
+  kv->bytes = bytes;
+  kv->len = reinterpret_cast<int32_t*>(kv->base);
+  kv->pending = kv->len + max_batch;
+  kv->err = kv->pending + max_batch;
+  const size_t hdr = align_up((size_t)(2 * max_batch + 1) * 4, 256);
+  kv->rope = reinterpret_cast<float*>(kv->base + hdr);
+  kv->k = kv->base + hdr + align_up((size_t)max_len * c.head_dim * 4, 256);
+  kv->page_size = page_size;
+  kv->page_dtype = dtype;
+  kv->n_pages = n_pages;
+  kv->table = table;
+  const sdd_pages pg{c.n_kv_heads, c.head_dim, page_size, dtype, n_pages, nullptr};
+  sdd_pages_bytes(&pg, &layer);
+  kv->layer_stride = align_up(layer, 256);
+  const int64_t n = (int64_t)max_len * (c.head_dim / 2);
+  hipLaunchKernelGGL(kv_init_kernel, dim3((int)std::min<int64_t>(ceil_div(n, 256), 4096)), dim3(256), 0,
+                     reinterpret_cast<hipStream_t>(stream), kv->len, kv->pending, kv->err, max_batch, kv->rope, max_len,
+                     c.head_dim / 2, (double)c.rope_theta);
+  rc = check_launch("kv_init_kernel");
+  if (rc) {
+    delete kv;
+    return rc;
+  }
+  *out = kv;
+  return SDD_OK;
+}
+
+extern "C" int sdd_kv_pages(const sdd_kv* kv, int layer, sdd_pages* out) {
+  SDD_REQUIRE(kv && out, "NULL pointer");
+  SDD_REQUIRE(kv->page_size > 0, "the cache is not paged");
+  SDD_REQUIRE(layer >= 0 && layer < kv->m->cfg.n_layers, "bad layer %d", layer);
+  *out = kv_pages(kv, layer);
+  return SDD_OK;
+}
+
+extern "C" int sdd_kv_workspace_bytes(const sdd_kv* kv, int max_rows, size_t* bytes) {
+  SDD_REQUIRE(kv && bytes, "NULL pointer");
+  SDD_REQUIRE(max_rows > 0 && max_rows <= 65536, "bad max_rows %d", max_rows);
+  size_t paged = 0;
+  if (kv->page_size) {
+    size_t part = 0;  // the largest partial results of any nb blocks of R rows, nb R <= max_rows
+    for (int nb = 1; nb <= std::min(kv->max_batch, max_rows); ++nb) part = std::max(part, paged_part_upto(kv, nb, max_rows / nb));
+    paged = paged_ws(kv, 1, max_rows, part).total + 256;
+  }
+  *bytes = ws_layout(kv->m, max_rows).total + paged;
+  return SDD_OK;
+}
+
 extern "C" int sdd_kv_destroy(sdd_kv* kv) {
   delete kv;
   return SDD_OK;
@@ -1727,7 +1912,8 @@ extern "C" int sdd_workspace_bytes(const sdd_model* m, int max_rows, size_t* byt
   return SDD_OK;
 }
 
-static int make_ctx(CallCtx& cx, sdd_model* m, sdd_kv* kv, void* ws, size_t ws_bytes, int rows, hipStream_t st) {
+static int make_ctx(CallCtx& cx, sdd_model* m, sdd_kv* kv, void* ws, size_t ws_bytes, int nb, int R, hipStream_t st) {
+  const int rows = nb * R;
   SDD_REQUIRE(m && kv && ws, "NULL pointer");
   SDD_REQUIRE(kv->m == m, "KV cache belongs to another model");
   SDD_REQUIRE((uintptr_t)ws % 256 == 0, "workspace must be 256-byte aligned");
@@ -1736,8 +1922,10 @@ static int make_ctx(CallCtx& cx, sdd_model* m, sdd_kv* kv, void* ws, size_t ws_b
   cx.ws = reinterpret_cast<char*>(ws);
   cx.L = ws_layout(m, rows);
   cx.st = st;
-  if (cx.L.total > ws_bytes)
-    return fail(SDD_ECAPACITY, "workspace of %zu bytes is too small for %d rows (%zu needed)", ws_bytes, rows, cx.L.total);
+  cx.paged = cx.L.total;
+  const size_t need = cx.L.total + paged_bytes(kv, nb, R);
+  if (need > ws_bytes)
+    return fail(SDD_ECAPACITY, "workspace of %zu bytes is too small for %d rows (%zu needed)", ws_bytes, rows, need);
   return SDD_OK;
 }
 
@@ -1756,15 +1944,17 @@ struct PrefillPlan {
 // depend on the chunk, so the rows of the passes over 64 rows are cut into as few chunks as the workspace holds (without
 // argmax records, everything past the rows' buffers being room for partial tiles), or up to three more where the GEMMs'
 // estimated time comes out lower.
-static PrefillPlan plan_prefill(const sdd_model* m, int n, size_t bytes) {
+static PrefillPlan plan_prefill(const sdd_kv* kv, int n, size_t bytes) {
+  const sdd_model* m = kv->m;
+  auto room = [&](int r) { return prefill_room(kv, r, bytes); };
   int pass = 16;
   for (int r : {256, 128, 64, 32})
-    if (ws_layout(m, r).total <= bytes) {
+    if (ws_layout(m, r).total <= room(r)) {
       pass = r;
       break;
     }
   if (m->es != 2) return PrefillPlan{0, 0, pass, pass};
-  auto fits = [&](int r) { return prefill_layout(m, r, bytes).total <= bytes; };
+  auto fits = [&](int r) { return prefill_layout(m, r, room(r)).total <= room(r); };
   if (pass <= kMaxPassRows) {
     int r = kMaxPassRows;
     while (r > 16 && !fits(r)) r -= 16;
@@ -1787,7 +1977,7 @@ static PrefillPlan plan_prefill(const sdd_model* m, int n, size_t bytes) {
   for (int k = k0; k < k0 + 4; ++k) {
     if (k > k0 && tiles / k < 6) break;
     const int r = 16 * (int)ceil_div(tiles, k);
-    const double us = k * plan_forward(m, r, prefill_layout(m, r, bytes), false).layer_us();
+    const double us = k * plan_forward(m, r, prefill_layout(m, r, room(r)), false).layer_us();
     if (us < best_us) {
       best_us = us;
       p.k = k;
@@ -1804,14 +1994,15 @@ extern "C" int sdd_kv_prefill(sdd_model* m, sdd_kv* kv, int seq, const int32_t* 
   SDD_REQUIRE(n >= 1, "prefill needs at least one token");
   if (n - 1 > kv->max_len) return fail(SDD_ECAPACITY, "prompt of %d tokens exceeds max_len %d", n, kv->max_len);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
-  if (ws_layout(m, 16).total > ws_bytes) return fail(SDD_ECAPACITY, "workspace too small for prefill");
-  const PrefillPlan plan = plan_prefill(m, n - 1, ws_bytes);
+  if (ws_layout(m, 16).total > prefill_room(kv, 16, ws_bytes)) return fail(SDD_ECAPACITY, "workspace too small for prefill");
+  const PrefillPlan plan = plan_prefill(kv, n - 1, ws_bytes);
   for (int i = 0, c0 = 0; c0 < n - 1; ++i) {
     const int rows = c0 < plan.main ? plan.begin(i + 1) - c0 : std::min(plan.rest, n - 1 - c0);
     CallCtx cx;
-    int rc = make_ctx(cx, m, kv, ws, ws_bytes, 16, st);
+    int rc = make_ctx(cx, m, kv, ws, ws_bytes, 1, 16, st);
     if (rc) return rc;
-    cx.L = prefill_layout(m, plan.layout, ws_bytes);
+    cx.paged = prefill_room(kv, plan.layout, ws_bytes);
+    cx.L = prefill_layout(m, plan.layout, cx.paged);
     EmbedArgs e{};
     e.prefill = 1;
     e.seq = seq;
@@ -1837,7 +2028,7 @@ extern "C" int sdd_verify_block(sdd_model* m, sdd_kv* kv, const int32_t* seq_ids
   if (gamma + 1 > kv->max_len) return fail(SDD_ECAPACITY, "block of %d rows exceeds max_len", gamma + 1);
   const int R = gamma + 1, M = n_seq * R;
   CallCtx cx;
-  int rc = make_ctx(cx, m, kv, ws, ws_bytes, M, reinterpret_cast<hipStream_t>(stream));
+  int rc = make_ctx(cx, m, kv, ws, ws_bytes, n_seq, R, reinterpret_cast<hipStream_t>(stream));
   if (rc) return rc;
   EmbedArgs e{};
   e.prefill = 0;
@@ -1862,7 +2053,7 @@ extern "C" int sdd_verify_full(sdd_model* m, sdd_kv* scratch, const int32_t* tok
   int rc = sdd_kv_prefill(m, scratch, 0, tokens, n - gamma, ws, ws_bytes, stream);
   if (rc) return rc;
   CallCtx cx;
-  if ((rc = make_ctx(cx, m, scratch, ws, ws_bytes, gamma + 1, reinterpret_cast<hipStream_t>(stream)))) return rc;
+  if ((rc = make_ctx(cx, m, scratch, ws, ws_bytes, 1, gamma + 1, reinterpret_cast<hipStream_t>(stream)))) return rc;
   EmbedArgs e{};
   e.prefill = 0;
   e.seq_ids = nullptr;  // block 0 is slot 0

@@ -12,7 +12,10 @@
 
 namespace sdd {
 
-enum Epi { EPI_QKV = 0, EPI_RESID = 1, EPI_SWIGLU = 2, EPI_LOGITS = 3 };
+enum Epi {
+  EPI_QKV = 0, EPI_RESID = 1, EPI_SWIGLU = 2, EPI_LOGITS = 3,
+  EPI_ROWS = 4  // the projection's rows as they are in fp32 (paged caches): the LM head's epilogue over any matrix
+};
 
 constexpr int kGemmThreads = 256;
 constexpr int kXcds = 8;  // XCDs of the MI355X (32 CUs each); workgroups go to them round-robin by linear id

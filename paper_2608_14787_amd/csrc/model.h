@@ -141,7 +141,10 @@ struct sdd_kv {
   float* rope;       // [max_len][head_dim/2][2] (cos, sin)
   char* k;           // [layers][max_batch][n_kv_heads][ld][head_dim]
   char* v;           // [layers][max_batch][n_kv_heads][head_dim][ld] (transposed)
-  size_t layer_stride;  // bytes per layer of k (and of v)
+  size_t layer_stride;  // bytes per layer of k (and of v), or of the pool
+  // paged cache (page_size > 0): k holds [layers] pools of n_pages pages (paged.h), v is NULL
+  int page_size, page_dtype, n_pages;
+  const int32_t* table;  // caller's block table [max_batch][ceil(max_len / page_size)]
 };
 
 namespace sdd {

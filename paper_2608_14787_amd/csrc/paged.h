@@ -58,11 +58,30 @@ __device__ inline int scale_byte(float amax) {
 }
 __device__ inline float scale_value(int byte) { return __builtin_bit_cast(float, (uint32_t)byte << 23); }
 
+// ---- new rows into a pool (paged.hip) -------------------------------------------------------------------
+struct AppendArgs {
+  PageDesc pg;
+  const int32_t* len;
+  const RowInfo* rows;  // instead of len: row b R holds the sequence (its table row), position and validity
+  const char* qkv;
+  int64_t row_stride;  // elements
+  const float *q_gain, *k_gain, *rope;
+  uint16_t* q_out;
+  int32_t* err;
+  int B, R, hq, max_pos;
+  float eps;
+  int n_qk;       // workgroups of the q/k part
+  int per_wave;   // head sets that a wave takes one after the other
+  int v_groups;   // 8-position groups that R rows can touch
+};
+
+int launch_paged_append(AppendArgs a, int head_dim, bool e4, bool f32, hipStream_t st);
+
 // ---- attention over a pool (paged_attn.hip) ------------------------------------------------------------
 struct PagedAttnArgs {
   PageDesc pg;
   const int32_t* len;   // [B] positions before the rows; < 0: the sequence is skipped
-  const RowInfo* rows;  // instead of len: row b R holds the sequence (its table row), position and validity
+  const RowInfo* rows;  // instead of len, as above
   const uint16_t* q;    // [B][R][hq][hd]
   uint16_t* out;        // the same, or fragment-major rows (frag)
   int frag;
@@ -72,5 +91,9 @@ struct PagedAttnArgs {
   int qtiles, splits, max_splits;
   float* part;  // partial results
 };
+constexpr float kLog2e = 1.44269504088896340736f;
+// Bytes of partial results that a call needs (B, R, hq, grp, max_len and pg.hkv are read).
+size_t paged_attn_workspace(PagedAttnArgs a, int head_dim);
+int launch_paged_attn(PagedAttnArgs a, int head_dim, bool e4, hipStream_t st);
 
 }  // namespace sdd

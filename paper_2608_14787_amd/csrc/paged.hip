@@ -53,22 +53,6 @@ __device__ inline int page_of(const PageDesc& d, int row, int64_t pos, int32_t* 
 
 // ---- append ----------------------------------------------------------------------------------------------
 
-struct AppendArgs {
-  PageDesc pg;
-  const int32_t* len;
-  const RowInfo* rows;  // instead of len (paged.h, PagedAttnArgs)
-  const char* qkv;
-  int64_t row_stride;  // elements
-  const float *q_gain, *k_gain, *rope;
-  uint16_t* q_out;
-  int32_t* err;
-  int B, R, hq, max_pos;
-  float eps;
-  int n_qk;       // workgroups of the q/k part
-  int per_wave;   // head sets that a wave takes one after the other
-  int v_groups;   // 8-position groups that R rows can touch
-};
-
 struct Start {
   int64_t pos;
   int row;
@@ -421,7 +405,9 @@ void launch_append_t(const AppendArgs& a, int hd, int blocks, hipStream_t st) {
     hipLaunchKernelGGL((append_kernel<T, E4, 64>), dim3(blocks), dim3(256), 0, st, a);
 }
 
-int run_append(AppendArgs& a, int hd, bool e4, bool f32, hipStream_t st) {
+}  // namespace
+
+int launch_paged_append(AppendArgs a, int hd, bool e4, bool f32, hipStream_t st) {
   const int H = a.hq + a.pg.hkv, hs = kWave / (hd / 16), sets = (int)ceil_div(H, hs);
   const int64_t rows = (int64_t)a.B * a.R;
   // one set of heads per wave while the waves are few (latency), all of a row's with many rows (the table's and the gains'
@@ -446,7 +432,6 @@ int run_append(AppendArgs& a, int hd, bool e4, bool f32, hipStream_t st) {
   return check_launch("append_kernel");
 }
 
-}  // namespace
 }  // namespace sdd
 
 using namespace sdd;
@@ -513,7 +498,7 @@ extern "C" int sdd_paged_append(const sdd_pages* pg, const int32_t* table, int t
   a.hq = n_q_heads;
   a.max_pos = max_pos;
   a.eps = eps;
-  return run_append(a, pg->head_dim, pg->dtype == SDD_E4M3, qkv_dtype == SDD_F32, reinterpret_cast<hipStream_t>(stream));
+  return launch_paged_append(a, pg->head_dim, pg->dtype == SDD_E4M3, qkv_dtype == SDD_F32, reinterpret_cast<hipStream_t>(stream));
 }
 
 extern "C" int sdd_paged_read(const sdd_pages* pg, const int32_t* table, int table_width, const int32_t* start, int B, int n,

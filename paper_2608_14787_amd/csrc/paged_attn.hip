@@ -20,7 +20,6 @@ namespace {
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
 constexpr int kMinChunk = 128;      // positions: one step a wave
 constexpr int kTargetItems = 512;   // workgroups a sequence is cut into at most
-constexpr float kLog2e = 1.44269504088896340736f;
 
 __host__ __device__ inline int chunk_of(int total, int max_splits) {
   const int c = (total + max_splits - 1) / max_splits;
@@ -270,9 +269,9 @@ __global__ void __launch_bounds__(kThreads) paged_attn_kernel(PagedAttnArgs a) {
     s_l[wave][lane] = l;
   }
   __syncthreads();
-  const int64_t slot = ((int64_t)(b * hkv + kvh) * a.qtiles + qt) * a.max_splits + c;
+  const int64_t slot = ((int64_t)(b * hkv + kvh) * a.qtiles + qt) * a.splits + c;
   float* part_o = a.part + slot * 16 * HD;
-  float* part_ml = a.part + (int64_t)a.B * hkv * a.qtiles * a.max_splits * 16 * HD + slot * 32;
+  float* part_ml = a.part + (int64_t)a.B * hkv * a.qtiles * a.splits * 16 * HD + slot * 32;
   for (int e = threadIdx.x; e < 16 * HD / 4; e += kThreads) {
     const int q = e / (HD / 4), d = e % (HD / 4) * 4;
     if (qt * 16 + q >= QV) continue;
@@ -318,9 +317,9 @@ __global__ void __launch_bounds__(256) paged_combine_kernel(PagedAttnArgs a) {
   if (sq.pos < 0) return;
   const int total = sq.pos + a.R, chunk = chunk_of(total, a.max_splits), n = (total + chunk - 1) / chunk;
   if (n == 1) return;
-  const int64_t slot = (bh * a.qtiles + qv / 16) * a.max_splits;
+  const int64_t slot = (bh * a.qtiles + qv / 16) * a.splits;
   const float* o = a.part + (slot * 16 + qv % 16) * HD + d;
-  const float* ml = a.part + (int64_t)a.B * a.pg.hkv * a.qtiles * a.max_splits * 16 * HD + (slot * 16 + qv % 16) * 2;
+  const float* ml = a.part + (int64_t)a.B * a.pg.hkv * a.qtiles * a.splits * 16 * HD + (slot * 16 + qv % 16) * 2;
   float M = -INFINITY;
   for (int c = 0; c < n; ++c) M = fmaxf(M, ml[32 * c]);
   float y[4] = {0.f, 0.f, 0.f, 0.f}, L = 0.f;
@@ -360,7 +359,7 @@ static void attn_splits(PagedAttnArgs* a) {
 size_t paged_attn_workspace(PagedAttnArgs a, int hd) {
   attn_splits(&a);
   if (a.splits == 1) return 0;
-  return (size_t)a.B * a.pg.hkv * a.qtiles * a.max_splits * 16 * (hd + 2) * 4;
+  return (size_t)a.B * a.pg.hkv * a.qtiles * a.splits * 16 * (hd + 2) * 4;
 }
 
 int launch_paged_attn(PagedAttnArgs a, int hd, bool e4, hipStream_t st) {

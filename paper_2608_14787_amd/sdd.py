@@ -72,6 +72,10 @@ _SIGS = {
     "sdd_survival_workspace_bytes": (I, [P, I, P]),
     "sdd_survival_mlp": (I, [P, P, P, I, P, P, P, SZ, P]),
     "sdd_pages_bytes": (I, [P, P]),
+    "sdd_paged_kv_bytes": (I, [P, I, I, I, I, I, P]),
+    "sdd_paged_kv_create": (I, [P, I, I, I, I, I, P, P, SZ, P, P]),
+    "sdd_kv_pages": (I, [P, I, P]),
+    "sdd_kv_workspace_bytes": (I, [P, I, P]),
     "sdd_rope_table": (I, [P, I, I, F, P]),
     "sdd_paged_append": (I, [P, P, I, P, I, I, I, P, I, SZ, P, P, F, P, I, P, P, P]),
     "sdd_paged_attention_workspace_bytes": (I, [P, I, I, I, I, P]),
@@ -539,3 +543,59 @@ class KVCache:
             _i32(t, nm)
         _check(lib().sdd_kv_commit(self.handle, _ptr(seq_ids), seq_ids.numel(), _ptr(accepted_len),
                                    _ptr(next_token), _stream(stream)))
+
+    def workspace(self, max_rows: int) -> torch.Tensor:
+        """Workspace for calls of up to max_rows rows on this cache (Model.workspace serves contiguous caches as well)."""
+        ws = torch.empty(_size_out(lib().sdd_kv_workspace_bytes, self.handle, max_rows), dtype=torch.uint8, device=self.buf.device)
+        workspace_init(ws)
+        return ws
+
+
+class PagedKVCache(KVCache):
+    """A KV cache in pages (sdd_paged_kv_create): memory for n_pages pages a layer, shared out to sequences as they grow.
+
+    `table` (int32 [max_batch, width], device) may be written by the caller; assign() and release() keep it from a free
+    list on the host."""
+
+    def __init__(self, model: Model, max_batch: int, max_len: int, n_pages: int, page_size: int = 64, dtype: str = "bf16",
+                 stream=None):
+        _need(dtype in ("bf16", "e4m3"), f"dtype must be bf16 or e4m3, got {dtype}")
+        self.model, self.max_batch, self.max_len, self.page_size = model, max_batch, max_len, page_size
+        self.n_pages, self.dtype = n_pages, dtype
+        code = BF16 if dtype == "bf16" else E4M3
+        n = _size_out(lib().sdd_paged_kv_bytes, C.byref(model.cfg), max_batch, max_len, page_size, code, n_pages)
+        dev = model.buf.device
+        self.buf = torch.empty(n, dtype=torch.uint8, device=dev)
+        self.table = torch.full((max_batch, -(-max_len // page_size)), -1, dtype=torch.int32, device=dev)
+        h = C.c_void_p()
+        _check(lib().sdd_paged_kv_create(model.handle, max_batch, max_len, page_size, code, n_pages, _ptr(self.table),
+                                         _ptr(self.buf), n, _stream(stream), C.byref(h)))
+        self.handle = h
+        self.free = list(range(n_pages - 1, -1, -1))
+        self.held = [[] for _ in range(max_batch)]
+
+    def assign(self, seq: int, positions: int):
+        """Gives sequence seq the pages that `positions` positions need (those it holds stay); raises when none are free."""
+        have, want = len(self.held[seq]), -(-positions // self.page_size)
+        _need(positions <= self.max_len, f"{positions} positions exceed max_len {self.max_len}")
+        if want <= have:
+            return
+        if want - have > len(self.free):
+            raise SDDError(ECAPACITY, f"{want - have} pages needed, {len(self.free)} free")
+        new = [self.free.pop() for _ in range(want - have)]
+        self.held[seq] += new
+        self.table[seq, have:want] = torch.tensor(new, dtype=torch.int32, device=self.table.device)
+
+    def release(self, seq: int):
+        """Takes all pages back from sequence seq."""
+        self.free += reversed(self.held[seq])
+        self.held[seq] = []
+        self.table[seq] = -1
+
+    def pool(self, layer: int) -> PagePool:
+        """One layer's pages (for PagePool.read)."""
+        d = PagesDesc()
+        _check(lib().sdd_kv_pages(self.handle, layer, C.byref(d)))
+        at = d.pages - self.buf.data_ptr()
+        n = _size_out(lib().sdd_pages_bytes, C.byref(d))
+        return PagePool(self.n_pages, d.n_kv_heads, d.head_dim, self.page_size, self.dtype, buf=self.buf[at:at + n])
