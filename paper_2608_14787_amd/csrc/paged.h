@@ -5,6 +5,19 @@
 
 namespace sdd {
 
+// Division by a number known on the host: the kernels' indices come apart by a few of them before the first load, and a
+// division is some twenty instructions here.  n / d = n m >> (31 + s) for 0 <= n < 2^31, with s = ceil(log2 d) and m =
+// ceil(2^(31 + s) / d) < 2^32 (the rounding of m moves the quotient by less than n / 2^(31 + s) < 1 / d).
+struct FastDiv {
+  uint32_t d, m, s;
+  FastDiv() : d(1), m(1u << 31), s(0) {}
+  explicit FastDiv(uint32_t by) : d(by), s(0) {
+    while ((1u << s) < by) ++s;
+    m = (uint32_t)((((uint64_t)1 << (31 + s)) + by - 1) / by);
+  }
+  __host__ __device__ inline int div(int n) const { return (int)((uint64_t)(uint32_t)n * m >> (31 + s)); }
+};
+
 // Sticky bits of the operators' error word (those of sdd_kv_state).
 constexpr int kErrCapacity = 1, kErrId = 4;
 
@@ -89,6 +102,7 @@ struct PagedAttnArgs {
   float scale;  // of the scores, times log2(e)
   int32_t* err;
   int qtiles, splits, max_splits;
+  FastDiv by_grp, by_hkv, by_b, by_qtiles;  // (set by the launch)
   float* part;  // partial results
 };
 constexpr float kLog2e = 1.44269504088896340736f;

@@ -10,6 +10,7 @@
 // results by combine_kernel in chunk order.  The cut into chunks depends on the sequence's own length alone.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "gemm.h"
 #include "paged.h"
@@ -18,28 +19,30 @@ namespace sdd {
 namespace {
 
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
-constexpr int kMinChunk = 128;      // positions: one step a wave
+constexpr int kMinChunk = 256;      // positions: two steps a wave
 constexpr int kTargetItems = 512;   // workgroups a sequence is cut into at most
 
 __host__ __device__ inline int chunk_of(int total, int max_splits) {
   const int c = (total + max_splits - 1) / max_splits;
-  return max(kMinChunk, (c + kMinChunk - 1) / kMinChunk * kMinChunk);
+  return max(kMinChunk, (c + 127) / 128 * 128);
 }
 
 struct Seq {
   int pos, row;  // position of the block's row 0 (-1: nothing to do), row of the table
 };
 __device__ inline Seq attn_seq(const PagedAttnArgs& a, int b, bool report) {
+  int p, row = b, ok = 1;
   if (a.rows) {
-    const RowInfo ri = a.rows[(int64_t)b * a.R];
-    return Seq{ri.valid && ri.pos + a.R <= a.max_len ? ri.pos : -1, ri.seq};
+    const RowInfo* ri = a.rows + (int64_t)b * a.R;
+    p = ri->pos, row = ri->seq, ok = ri->valid;
+  } else {
+    p = a.len[b];
   }
-  const int p = a.len[b];
-  if (p >= 0 && (int64_t)p + a.R > a.max_len) {
-    if (report && a.err) atomicOr(a.err, kErrCapacity);
-    return Seq{-1, b};
-  }
-  return Seq{p < 0 ? -1 : p, b};
+  // (uniform values, in scalar registers: what is addressed with them stays there)
+  p = __builtin_amdgcn_readfirstlane(p), row = __builtin_amdgcn_readfirstlane(row), ok = __builtin_amdgcn_readfirstlane(ok);
+  const bool fits = (int64_t)p + a.R <= a.max_len;
+  if (report && !fits && a.err && !a.rows) atomicOr(a.err, kErrCapacity);
+  return Seq{ok && fits && p >= 0 ? p : -1, row};
 }
 
 __device__ inline void store_out4(const PagedAttnArgs& a, int b, int r, int h, int HD, int dim, const float* y) {
@@ -61,27 +64,20 @@ __device__ inline bf16x8 e4m3_frag(uint32_t x, uint32_t y) {
 }
 __device__ inline uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-// One step's operands (32 positions): K blocks, V blocks, e4m3 scale bytes of the lane's 8 positions.
 template <bool E4, int HD>
-struct StepRegs {
-  static constexpr int NK = E4 ? HD / 64 : HD / 32, NV = E4 ? HD / 32 : HD / 16;
-  uint4 k[2][NK], v[NV];
-  uint2 ks, vs;
-  bool ok;  // the page exists
-};
-
-template <bool E4, int HD>
-__global__ void __launch_bounds__(kThreads) paged_attn_kernel(PagedAttnArgs a) {
+__global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a) {
   constexpr int KK = HD / 32, DB = HD / 16;
-  using Regs = StepRegs<E4, HD>;
+  constexpr int NK = E4 ? HD / 64 : HD / 32, NV = E4 ? HD / 32 : HD / 16;  // 16-byte loads of a step: 2 NK of K, NV of V
   __shared__ __align__(16) float s_o[kWaves][16][HD + 4];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+  __shared__ __align__(16) char s_q[KK * 1024];
+  touch_kernargs<PagedAttnArgs>();
   const int hkv = a.pg.hkv;
   // workgroups go to the XCDs round-robin by id: the query tiles of one (chunk, sequence, head) share an XCD's L2
   const int low = blockIdx.x % kXcds, rest = blockIdx.x / kXcds;
-  const int qt = rest % a.qtiles, item = rest / a.qtiles * kXcds + low;
+  const int group = a.by_qtiles.div(rest), qt = rest - group * a.qtiles, item = group * kXcds + low;
   if (item >= a.splits * a.B * hkv) return;
-  const int kvh = item % hkv, b = item / hkv % a.B, c = item / hkv / a.B;
+  const int bc = a.by_hkv.div(item), kvh = item - bc * hkv, c = a.by_b.div(bc), b = bc - c * a.B;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const Seq sq = attn_seq(a, b, threadIdx.x == 0 && c == 0 && kvh == 0 && qt == 0);
   if (sq.pos < 0) return;
@@ -89,62 +85,89 @@ __global__ void __launch_bounds__(kThreads) paged_attn_kernel(PagedAttnArgs a) {
   if (c >= n_chunks) return;
   const int QV = a.R * a.grp, qv = qt * 16 + lane % 16;
   const bool qok = qv < QV;
-  const int r = qok ? qv / a.grp : 0, hh = qok ? qv % a.grp : 0;
+  const int r = qok ? a.by_grp.div(qv) : 0, hh = qok ? qv - r * a.grp : 0;
   const int qpos = qok ? sq.pos + r : -1;
-  const int lo = sq.pos + qt * 16 / a.grp;  // position of the tile's first row
-  const int tile_end = sq.pos + min(a.R - 1, (qt * 16 + 15) / a.grp) + 1;
+  const int lo = __builtin_amdgcn_readfirstlane(sq.pos + a.by_grp.div(qt * 16));  // position of the tile's first row
+  const int tile_end = __builtin_amdgcn_readfirstlane(sq.pos + min(a.R - 1, a.by_grp.div(qt * 16 + 15)) + 1);
   const int p_begin = c * chunk, p_end = min(tile_end, p_begin + chunk);
-
-  uint4 qf[KK];  // fragment i: the 8 dimensions that the i-th K operand of a step holds
-  {
-    const uint16_t* Q = a.q + ((int64_t)(b * a.R + r) * a.hq + kvh * a.grp + hh) * HD;
-#pragma unroll
-    for (int i = 0; i < KK; ++i)
-      qf[i] = load16(Q + (E4 ? 64 * (i / 2) + 16 * (lane / 16) + 8 * (i % 2) : 32 * i + 8 * (lane / 16)));
-  }
   const int g8 = 8 * (lane / 16);
+
   // the chunk's page ids, 64 at a time across the lanes
   const int lg = a.pg.log_page;
   int page0 = p_begin >> lg, ids = 0;
   auto load_ids = [&]() { ids = a.pg.table[(int64_t)sq.row * a.pg.width + min(page0 + lane, a.pg.width - 1)]; };
   load_ids();
+  // Query fragments (fragment i: the 8 dimensions that the i-th K operand of a step holds) sit in LDS.
+  uint4 q_frag = make_uint4(0, 0, 0, 0);
+  if (wave < KK) {
+    const uint16_t* Q = a.q + ((int64_t)(b * a.R + r) * a.hq + kvh * a.grp + hh) * HD;
+    q_frag = load16(Q + (E4 ? 64 * (wave / 2) + 16 * (lane / 16) + 8 * (wave % 2) : 32 * wave + g8));
+  }
   bool bad_page = false;
-  auto load_step = [&](int p, Regs& st) {
-    int i = (p >> lg) - page0;
-    if (i >= kWave) {
+  // Where a step lies: the head's part of its page as a descriptor (one address register for all of a step's loads), the
+  // position in the page, and whether the page exists.  Past the wave's last step the descriptor is of size zero and loads by
+  // it touch no memory: every path through the loop has the same loads in flight, so each wait is for what it needs alone.
+  struct Place {
+    __amdgpu_buffer_rsrc_t page;
+    int in;
+    bool ok;
+  };
+  auto place = [&](int p) {
+    const bool in_range = p < p_end;
+    const int i = in_range ? (p >> lg) - page0 : 0;
+    int id;
+    if (i < kWave) {
+      id = __builtin_amdgcn_readlane(ids, i);
+    } else {  // (read here as well, so that only this path waits for the load)
       page0 += kWave;
       load_ids();
-      i -= kWave;
+      id = __builtin_amdgcn_readlane(ids, i - kWave);
     }
-    const int id = __builtin_amdgcn_readlane(ids, i);
-    st.ok = (unsigned)id < (unsigned)a.pg.n_pages;
-    bad_page |= !st.ok;
-    const int in = p & ((1 << lg) - 1);
-    const char* base = page_head(a.pg, st.ok ? id : 0, kvh);
-    const char* k = base + in * HD * (E4 ? 1 : 2) + lane * 16;
-    const char* v = k + a.pg.side;
+    const bool ok = (unsigned)id < (unsigned)a.pg.n_pages;
+    bad_page |= in_range && !ok;
+    return Place{__builtin_amdgcn_make_buffer_rsrc(page_head(a.pg, ok ? id : 0, kvh), 0, in_range ? a.pg.head_bytes : 0,
+                                                   kBufferRsrcWord3),
+                 p & ((1 << lg) - 1), ok};
+  };
+  uint4 kr[2][NK], vr[NV];
+  uint2 ks = {0, 0}, vs = {0, 0};
+  auto load = [&](const Place& pl, int off) {
+    // (non-temporal: a decode step reads a position once)
+    return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(pl.page, lane * 16, off, kNtCpol));
+  };
+  auto load_scales = [&](const Place& pl, int off) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(pl.page, g8, off, 0);
+    return make_uint2(v[0], v[1]);
+  };
+  auto load_k = [&](const Place& pl) {
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int j = 0; j < Regs::NK; ++j) st.k[s][j] = load16(k + (s * Regs::NK + j) * 1024);
+      for (int j = 0; j < NK; ++j) kr[s][j] = load(pl, pl.in * HD * (E4 ? 1 : 2) + (s * NK + j) * 1024);
+    if constexpr (E4) ks = load_scales(pl, 2 * a.pg.side + pl.in);
+  };
+  auto load_v = [&](const Place& pl) {
 #pragma unroll
-    for (int j = 0; j < Regs::NV; ++j) st.v[j] = load16(v + j * 1024);
-    if constexpr (E4) {
-      st.ks = *reinterpret_cast<const uint2*>(base + 2 * a.pg.side + in + g8);
-      st.vs = *reinterpret_cast<const uint2*>(base + 2 * a.pg.side + (1 << lg) + in + g8);
-    }
+    for (int j = 0; j < NV; ++j) vr[j] = load(pl, a.pg.side + pl.in * HD * (E4 ? 1 : 2) + j * 1024);
+    if constexpr (E4) vs = load_scales(pl, 2 * a.pg.side + (1 << lg) + pl.in);
   };
 
   f32x4 o[DB];
+  float m, l;
+  bool wild;
+  auto reset = [&]() {
 #pragma unroll
-  for (int db = 0; db < DB; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, l = 0.f;
+    for (int db = 0; db < DB; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m = -INFINITY, l = 0.f, wild = false;
+  };
+  reset();
   // V operand of 16 dimensions, positions outside `mask` (a bit for each of the lane's 8) zeroed: their weights are 0, and 0
   // times a stale or foreign non-finite value would not be
-  auto v_frag = [&](const Regs& st, int db, uint32_t mask) {
+  auto v_frag = [&](int db, uint32_t mask) {
     if constexpr (E4) {
-      uint32_t x = word(st.v[db / 2], db % 2 * 2), y = word(st.v[db / 2], db % 2 * 2 + 1);
-      if (mask != 255) {
+      uint32_t x = word(vr[db / 2], db % 2 * 2), y = word(vr[db / 2], db % 2 * 2 + 1);
+      if (mask != 255) {  // (lane by lane: no product in here)
         uint32_t mx = 0, my = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -155,47 +178,62 @@ __global__ void __launch_bounds__(kThreads) paged_attn_kernel(PagedAttnArgs a) {
       }
       return e4m3_frag(x, y);
     } else {
-      uint4 v = st.v[db];
+      uint4 w = vr[db];
       if (mask != 255) {
-        uint32_t w[4];
+        uint32_t k[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          w[i] = ((mask >> (2 * i) & 1) ? 0xffffu : 0u) | ((mask >> (2 * i + 1) & 1) ? 0xffff0000u : 0u);
-        v.x &= w[0], v.y &= w[1], v.z &= w[2], v.w &= w[3];
+          k[i] = ((mask >> (2 * i) & 1) ? 0xffffu : 0u) | ((mask >> (2 * i + 1) & 1) ? 0xffff0000u : 0u);
+        w.x &= k[0], w.y &= k[1], w.z &= k[2], w.w &= k[3];
       }
-      return __builtin_bit_cast(bf16x8, v);
+      return __builtin_bit_cast(bf16x8, w);
     }
   };
   auto below = [&](int p, int end) {  // mask of the lane's positions of step p that lie before end
     const int n = max(0, min(8, end - (p + g8)));
     return (1u << n) - 1u;
   };
-  auto step = [&](int p, const Regs& st) {
-    f32x4 s[2];
+  constexpr int kStride = 32 * kWaves;
+  const int p0 = p_begin + 32 * wave;
+  Place pl;
+  // Step p, whose place is pl; issues the next one's loads.  ONE: every query vector's product by itself, V zeroed where it is
+  // hidden from it.
+  auto step = [&](auto one, int p) {
+    const bool ok = pl.ok;
+    f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < KK; ++i) {
+      const bf16x8 q = *reinterpret_cast<const bf16x8*>(s_q + i * 1024 + lane * 16);
 #pragma unroll
-      for (int i = 0; i < KK; ++i) {
+      for (int t = 0; t < 2; ++t) {
         bf16x8 k;
         if constexpr (E4)
-          k = e4m3_frag(word(st.k[t][i / 2], i % 2 * 2), word(st.k[t][i / 2], i % 2 * 2 + 1));
+          k = e4m3_frag(word(kr[t][i / 2], i % 2 * 2), word(kr[t][i / 2], i % 2 * 2 + 1));
         else
-          k = __builtin_bit_cast(bf16x8, st.k[t][i]);
-        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, __builtin_bit_cast(bf16x8, qf[i]), s[t], 0, 0, 0);
+          k = __builtin_bit_cast(bf16x8, kr[t][i]);
+        s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q, s[t], 0, 0, 0);
       }
     }
     // s[i / 4][i % 4]: position p + g8 + i, query vector lane % 16
     float sv[8];
-    float top = -INFINITY;
-    const int end = st.ok ? min(qpos + 1, p_end) : 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      float v = s[i / 4][i % 4] * a.scale;
-      if constexpr (E4) v *= scale_value(((i < 4 ? st.ks.x : st.ks.y) >> (8 * (i % 4))) & 255);
-      sv[i] = p + g8 + i < end ? v : -INFINITY;
-      top = fmaxf(top, sv[i]);
+      sv[i] = s[i / 4][i % 4] * a.scale;
+      if constexpr (E4) sv[i] *= scale_value(((i < 4 ? ks.x : ks.y) >> (8 * (i % 4))) & 255);
     }
+    // K's registers are free: the next step's loads go out ahead of this one's softmax, V's after its product
+    pl = place(p + kStride);
+    load_k(pl);
+    __builtin_amdgcn_sched_barrier(0);
+    const bool whole = p + 32 <= p_end && ok;  // (the same in every lane: products run with all of them)
+    if (p + 31 > lo || !whole) {
+      const int end = ok ? min(qpos + 1, p_end) : 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sv[i] = p + g8 + i < end ? sv[i] : -INFINITY;
+    }
+    float top = sv[0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) top = fmaxf(top, sv[i]);
     top = xor16_op(top, [](float x, float y) { return fmaxf(x, y); });
     top = xor32_op(top, [](float x, float y) { return fmaxf(x, y); });
     const float mn = fmaxf(m, top);
@@ -206,58 +244,70 @@ __global__ void __launch_bounds__(kThreads) paged_attn_kernel(PagedAttnArgs a) {
       for (int db = 0; db < DB; ++db) o[db] *= f;
       m = mn;
     }
+    const float ref = m == -INFINITY ? 0.f : m;  // (a hidden score's weight is then exp2(-inf) = 0)
     float e[8], sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      e[i] = sv[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sv[i] - mn);
+      e[i] = __builtin_amdgcn_exp2f(sv[i] - ref);
       sum += e[i];
-      if constexpr (E4) e[i] *= sv[i] == -INFINITY ? 0.f : scale_value(((i < 4 ? st.vs.x : st.vs.y) >> (8 * (i % 4))) & 255);
     }
     l += sum;
-    const bf16x8 pf = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]),
-                                                            pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])));
-    const uint32_t mask = below(p, st.ok ? p_end : 0);
-    bf16x8 vf[DB];
+    if constexpr (E4) {
 #pragma unroll
-    for (int db = 0; db < DB; ++db) vf[db] = v_frag(st, db, mask);
-    // Steps on the tile's diagonal: a position may be hidden from some of the query vectors only.  Where its V is not finite,
-    // their zero weights would not keep it out; then every query vector's product leaves out what is hidden from it.
-    if (p + 31 > lo && lo + 1 < tile_end) {
-      bool wild = false;
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) wild |= !__builtin_isfinite((float)vf[db][i]);
-      if (__any(wild)) {
-        for (int q = 0; q < 16; ++q) {
-          const uint32_t seen = mask & below(p, __builtin_amdgcn_readlane(qpos, q) + 1);
-#pragma unroll
-          for (int db = 0; db < DB; ++db) {
-            const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(st, db, seen), pf, o[db], 0, 0, 0);
-            if (lane % 16 == q) o[db] = y;  // (a product's columns are independent: the others are not taken)
-          }
-        }
-        return;
+      for (int i = 0; i < 8; ++i) {
+        const float x = e[i] * scale_value(((i < 4 ? vs.x : vs.y) >> (8 * (i % 4))) & 255);
+        e[i] = sv[i] == -INFINITY ? 0.f : x;  // (a position that was never written may have any scale byte)
       }
     }
+    const bf16x8 pf = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]),
+                                                            pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])));
+    if constexpr (decltype(one)::value) {
+#pragma unroll 1
+      for (int q = 0; q < 16; ++q) {
+        const uint32_t seen = below(p, ok ? min(p_end, __builtin_amdgcn_readlane(qpos, q) + 1) : 0);
 #pragma unroll
-    for (int db = 0; db < DB; ++db) o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[db], pf, o[db], 0, 0, 0);
-  };
-  const int p_first = p_begin + 32 * wave;
-  constexpr int kStride = 32 * kWaves;
-  if (p_first < p_end) {
-    Regs s0, s1;
-    load_step(p_first, s0);
-    for (int p = p_first;; p += 2 * kStride) {
-      const bool more = p + kStride < p_end;
-      if (more) load_step(p + kStride, s1);
-      step(p, s0);
-      if (!more) break;
-      const bool again = p + 2 * kStride < p_end;
-      if (again) load_step(p + 2 * kStride, s0);
-      step(p + kStride, s1);
-      if (!again) break;
+        for (int db = 0; db < DB; ++db) {
+          const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(db, seen), pf, o[db], 0, 0, 0);
+          if (lane % 16 == q) o[db] = y;  // (a product's columns are independent: the others are not taken)
+        }
+      }
+    } else if (whole && p + 31 <= lo) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(db, 255), pf, o[db], 0, 0, 0);
+    } else {
+      const uint32_t mask = below(p, ok ? p_end : 0);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const bf16x8 v = v_frag(db, mask);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) wild |= !__builtin_isfinite((float)v[i]);
+        o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf, o[db], 0, 0, 0);
+      }
     }
+  };
+  auto steps = [&](auto one) {
+    pl = place(p0);
+    load_k(pl);
+    load_v(pl);
+    if constexpr (!decltype(one)::value) {
+      if (wave < KK) *reinterpret_cast<uint4*>(s_q + wave * 1024 + lane * 16) = q_frag;
+      __syncthreads();  // the queries are in LDS
+    }
+#pragma unroll 1
+    for (int p = p0; p < p_end; p += kStride) {
+      step(one, p);
+      __builtin_amdgcn_sched_barrier(0);
+      load_v(pl);
+    }
+  };
+  steps(std::false_type{});
+  // On the tile's diagonal a position may be hidden from some of the query vectors only.  Where a V value there is not finite,
+  // the zero weight of those vectors has not kept it out: the wave's steps again, each vector's product by itself.
+  if (lo + 1 < tile_end && __any(wild)) {
+    reset();
+    page0 = p_begin >> lg;
+    load_ids();
+    steps(std::true_type{});
   }
   if (a.err && bad_page && lane == 0) atomicOr(a.err, kErrId);
   l = xor16_op(l, [](float x, float y) { return x + y; });
@@ -293,7 +343,7 @@ __global__ void __launch_bounds__(kThreads) paged_attn_kernel(PagedAttnArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) y[i] = L == 0.f ? 0.f : y[i] * inv;
       const int qq = qt * 16 + q;
-      store_out4(a, b, qq / a.grp, kvh * a.grp + qq % a.grp, HD, d, y);
+      store_out4(a, b, a.by_grp.div(qq), kvh * a.grp + qq - a.by_grp.div(qq) * a.grp, HD, d, y);
     } else {
       *reinterpret_cast<f32x4*>(part_o + q * HD + d) = f32x4{y[0], y[1], y[2], y[3]};
       if (d == 0) {
@@ -304,32 +354,58 @@ __global__ void __launch_bounds__(kThreads) paged_attn_kernel(PagedAttnArgs a) {
   }
 }
 
-// Joins the chunks of one query vector per HD / 4 lanes, in chunk order.
+// Joins the chunks of a query vector: kJoin groups of HD / 4 lanes (4 dimensions a lane) take the chunks g, g + kJoin, ... in
+// order, several loads in flight, and are added in order of g.  A workgroup holds kThreads / (kJoin HD / 4) query vectors.
+constexpr int kJoin = 4;
 template <int HD>
-__global__ void __launch_bounds__(256) paged_combine_kernel(PagedAttnArgs a) {
-  constexpr int LN = HD / 4;
-  const int64_t idx = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LN;
-  const int d = 4 * (threadIdx.x % LN), QV = a.R * a.grp;
-  const int64_t bh = idx / QV;
+__global__ void __launch_bounds__(kThreads) paged_combine_kernel(PagedAttnArgs a) {
+  constexpr int LN = HD / 4, VEC = kThreads / (LN * kJoin), U = 4;
+  __shared__ __align__(16) float s_y[kThreads][4];
+  __shared__ float s_l[kThreads / LN];
+  const int grp = threadIdx.x / LN, g = grp % kJoin, ln = threadIdx.x % LN, d = 4 * ln, QV = a.R * a.grp;
+  const int64_t idx = (int64_t)blockIdx.x * VEC + grp / kJoin, bh = idx / QV;
   const int qv = (int)(idx % QV), b = (int)(bh / a.pg.hkv), kvh = (int)(bh % a.pg.hkv);
-  if (b >= a.B) return;
-  const Seq sq = attn_seq(a, b, false);
-  if (sq.pos < 0) return;
-  const int total = sq.pos + a.R, chunk = chunk_of(total, a.max_splits), n = (total + chunk - 1) / chunk;
-  if (n == 1) return;
-  const int64_t slot = (bh * a.qtiles + qv / 16) * a.splits;
-  const float* o = a.part + (slot * 16 + qv % 16) * HD + d;
-  const float* ml = a.part + (int64_t)a.B * a.pg.hkv * a.qtiles * a.splits * 16 * HD + (slot * 16 + qv % 16) * 2;
-  float M = -INFINITY;
-  for (int c = 0; c < n; ++c) M = fmaxf(M, ml[32 * c]);
+  Seq sq{-1, 0};
+  if (b < a.B) sq = attn_seq(a, b, false);
+  const int total = sq.pos + a.R, chunk = chunk_of(total, a.max_splits), n = sq.pos < 0 ? 1 : (total + chunk - 1) / chunk;
   float y[4] = {0.f, 0.f, 0.f, 0.f}, L = 0.f;
-  for (int c = 0; c < n; ++c) {
-    const float mc = ml[32 * c], lc = ml[32 * c + 1];
-    const float f = mc == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mc - M);
-    L += f * lc;
-    const f32x4 v = *reinterpret_cast<const f32x4*>(o + (int64_t)c * 16 * HD);
+  if (n > 1) {
+    const int64_t slot = (bh * a.qtiles + qv / 16) * a.splits;
+    const float* o = a.part + (slot * 16 + qv % 16) * HD + d;
+    const float* ml = a.part + (int64_t)a.B * a.pg.hkv * a.qtiles * a.splits * 16 * HD + (slot * 16 + qv % 16) * 2;
+    float M = -INFINITY;
+    for (int c = ln; c < n; c += LN) M = fmaxf(M, ml[32 * c]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] += f * v[i];
+    for (int k = 1; k < LN; k *= 2) M = fmaxf(M, __shfl_xor(M, k));
+    for (int c0 = g; c0 < n; c0 += kJoin * U) {
+      f32x4 v[U];
+      float mc[U], lc[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int c = min(c0 + kJoin * u, n - 1);
+        mc[u] = ml[32 * c], lc[u] = ml[32 * c + 1];
+        v[u] = *reinterpret_cast<const f32x4*>(o + (int64_t)c * 16 * HD);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (c0 + kJoin * u >= n) break;
+        const float f = mc[u] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mc[u] - M);
+        L += f * lc[u];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] += f * v[u][i];
+      }
+    }
+  }
+  *reinterpret_cast<f32x4*>(s_y[threadIdx.x]) = f32x4{y[0], y[1], y[2], y[3]};
+  if (ln == 0) s_l[grp] = L;
+  __syncthreads();
+  if (g != 0 || n == 1) return;
+#pragma unroll
+  for (int k = 1; k < kJoin; ++k) {
+    L += s_l[grp + k];
+    const f32x4 v = *reinterpret_cast<const f32x4*>(s_y[threadIdx.x + k * LN]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] += v[i];
   }
   const float inv = 1.f / L;
 #pragma unroll
@@ -343,7 +419,7 @@ void launch_t(const PagedAttnArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((paged_attn_kernel<E4, HD>), dim3((unsigned)(ceil_div(items, kXcds) * kXcds * a.qtiles)), dim3(kThreads), 0, st, a);
   if (a.splits > 1) {
     const int64_t vecs = (int64_t)a.B * a.pg.hkv * a.R * a.grp;
-    hipLaunchKernelGGL((paged_combine_kernel<HD>), dim3((unsigned)ceil_div(vecs * (HD / 4), 256)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((paged_combine_kernel<HD>), dim3((unsigned)ceil_div(vecs * (HD / 4) * kJoin, kThreads)), dim3(kThreads), 0, st, a);
   }
 }
 
@@ -364,8 +440,9 @@ size_t paged_attn_workspace(PagedAttnArgs a, int hd) {
 
 int launch_paged_attn(PagedAttnArgs a, int hd, bool e4, hipStream_t st) {
   attn_splits(&a);
+  a.by_grp = FastDiv(a.grp), a.by_hkv = FastDiv(a.pg.hkv), a.by_b = FastDiv(a.B), a.by_qtiles = FastDiv(a.qtiles);
   const int64_t blocks = (ceil_div((int64_t)a.splits * a.B * a.pg.hkv, kXcds) * kXcds) * a.qtiles;
-  if (blocks >= (int64_t(1) << 31) || (int64_t)a.B * a.R * a.hq * hd / 4 / 256 >= (int64_t(1) << 31))
+  if (blocks >= (int64_t(1) << 31) || (int64_t)a.B * a.R * a.hq * hd / 4 * 4 / 256 >= (int64_t(1) << 31))
     return fail(SDD_EUNSUPPORTED, "%d x %d rows in one call", a.B, a.R);
   prof_begin(PROF_ATTN, st);
   if (e4) {
