@@ -327,9 +327,11 @@ int sdd_paged_attention_workspace_bytes(const sdd_pages* pg, int B, int R, int n
  * host's bound sizes the launch, so that a captured call serves all lengths up
  * to it.  A row that sees nothing (its pages are invalid) gives zeros.  Sums and
  * softmax statistics are fp32 and in a fixed order: results are
- * bit-reproducible and do not depend on the other sequences of the call (they
- * do on R, whose rows share work).  Errors: SDD_EINVAL, SDD_ENOMEM (small
- * workspace), SDD_EUNSUPPORTED. */
+ * bit-reproducible, and a sequence's do not depend on the other sequences of
+ * the call, with one line between two orders of the sums: B * n_kv_heads *
+ * ceil(R * n_q_heads / n_kv_heads / 128) of 160 and more (they do depend on R,
+ * whose rows share work).  Errors: SDD_EINVAL, SDD_ENOMEM (small workspace),
+ * SDD_EUNSUPPORTED. */
 int sdd_paged_attention(const sdd_pages* pg, const int32_t* table, int table_width, const int32_t* len, int B, int R,
                         int n_q_heads, const uint16_t* q, float scale, int max_len, uint16_t* out, int32_t* err,
                         void* ws, size_t ws_bytes, sdd_stream_t stream);

@@ -1386,7 +1386,7 @@ static int paged_layer(CallCtx& cx, int layer, int nb, int R) {
   t.q = a.q_out;
   t.out = reinterpret_cast<uint16_t*>(cx.ws + cx.L.ao);
   t.frag = 1;
-  t.scale = kLog2e / sqrtf((float)c.head_dim);
+  t.set_scale(1.f / sqrtf((float)c.head_dim));
   t.err = kv->err;
   t.part = reinterpret_cast<float*>(pw + paged_ws(kv, nb, R, 0).part);
   return launch_paged_attn(t, c.head_dim, e4, cx.st);

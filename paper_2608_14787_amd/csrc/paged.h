@@ -99,13 +99,20 @@ struct PagedAttnArgs {
   uint16_t* out;        // the same, or fragment-major rows (frag)
   int frag;
   int B, R, hq, grp, max_len;
-  float scale;  // of the scores, times log2(e)
+  // |scale| of the scores, times log2(e) (1 for a scale of 0); the queries' bits are masked and flipped for its sign
+  float scale;
+  uint32_t q_and, q_xor;
+  void set_scale(float x) {
+    scale = x == 0.f ? 1.f : __builtin_fabsf(x) * 1.44269504088896340736f;
+    q_and = x == 0.f ? 0u : ~0u;
+    q_xor = x < 0.f ? 0x80008000u : 0u;
+  }
   int32_t* err;
-  int qtiles, splits, max_splits;
-  FastDiv by_grp, by_hkv, by_b, by_qtiles;  // (set by the launch)
+  int qtiles, splits, max_splits, qpad;
+  int wide;  // the kernel for many query vectors
+  FastDiv by_grp, by_hkv, by_b, by_qtiles, by_qv;  // (set by the launch)
   float* part;  // partial results
 };
-constexpr float kLog2e = 1.44269504088896340736f;
 // Bytes of partial results that a call needs (B, R, hq, grp, max_len and pg.hkv are read).
 size_t paged_attn_workspace(PagedAttnArgs a, int head_dim);
 int launch_paged_attn(PagedAttnArgs a, int head_dim, bool e4, hipStream_t st);

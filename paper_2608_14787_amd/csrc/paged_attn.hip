@@ -5,9 +5,11 @@
 // in one pass with the running maximum m, sum and accumulator in fp32 (exponentials of base 2, scale holding log2 e).  The
 // weights are rounded to bf16 for the second product, as V is held in bf16 or less; their sum takes them before that rounding.
 //
-// A workgroup takes 16 query vectors of one KV head (rows x the heads that share it) over one chunk of the sequence; its
-// four waves take the chunk's 32-position steps round-robin and are joined through LDS in wave order, and the chunks'
-// results by combine_kernel in chunk order.  The cut into chunks depends on the sequence's own length alone.
+// Two kernels.  paged_attn_kernel: a workgroup takes 16 query vectors of one KV head (rows x the heads that share it) over one
+// chunk of the sequence; its four waves take the chunk's 32-position steps round-robin, each step's K and V straight into the
+// wave's registers, and are joined through LDS in wave order.  paged_attn_wide_kernel, for calls with many query vectors: 128
+// of them a workgroup, sharing each step through a ring in LDS.  A third joins the chunks' results in chunk order.  The cut of
+// a sequence into chunks depends on its own length alone.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -19,12 +21,31 @@ namespace sdd {
 namespace {
 
 constexpr int kWaves = 4, kThreads = kWaves * kWave;
-constexpr int kMinChunk = 256;      // positions: two steps a wave
-constexpr int kTargetItems = 512;   // workgroups a sequence is cut into at most
+// A chunk is at least two steps a wave, and a sequence is cut into no more workgroups than kTargetItems.  Measured with chunks
+// of at least 128, 256 and 512 (attention alone): 32 ragged decode sequences 64, 53, 52 us; one of 513 positions 5.1, 5.5, 6.4.
+constexpr int kMinChunk = 256;
+constexpr int kTargetItems = 512;
 
-__host__ __device__ inline int chunk_of(int total, int max_splits) {
+// The many-vector kernel: a workgroup's waves, a tile of 32 query vectors each; the number of such workgroups (before the cut
+// into chunks) from which a call takes it; its chunks and items.  Measured, 64/8 heads of 128, bf16, this kernel against the
+// other, both with the join: eight sequences of 284-3761 positions, 33 rows (192 workgroups) 57 / 76 us; one sequence, 1024
+// rows behind 1024 positions (512) 73 / 127; 256 rows (128) 39 / 28, and behind 8000 positions 114 / 153; 33 rows (24) 18 / 14.
+// Chunks of 256, 512, 768, 1024 with the first of these: 63, 57.5, 57, 61 us (longer ones leave compute units idle, shorter
+// ones write more partial results).
+constexpr int kWideWaves = 4;
+constexpr int kWideBlocks = 160;
+constexpr int kWideChunk = 512, kWideItems = 256;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// The weights' reference m need not be the maximum: it moves, and with it the accumulators, only where a score passes it by
+// kFar (weights up to 2^kFar; their rounding is relative, and sums are fp32).  With 32 query vectors some maximum rises in most
+// steps: rescaled at each rise, a third of the step's vector instructions were the accumulators'.
+constexpr float kFar = 8.f;
+
+__host__ __device__ inline int chunk_of(int total, int max_splits, int wide) {
   const int c = (total + max_splits - 1) / max_splits;
-  return max(kMinChunk, (c + 127) / 128 * 128);
+  return max(wide ? kWideChunk : kMinChunk, (c + 127) / 128 * 128);
 }
 
 struct Seq {
@@ -45,26 +66,42 @@ __device__ inline Seq attn_seq(const PagedAttnArgs& a, int b, bool report) {
   return Seq{ok && fits && p >= 0 ? p : -1, row};
 }
 
-__device__ inline void store_out4(const PagedAttnArgs& a, int b, int r, int h, int HD, int dim, const float* y) {
-  const int row = b * a.R + r;
-  const int64_t at = a.frag ? xfrag_index<uint16_t>(row, h * HD + dim, a.hq * HD / 32) : ((int64_t)row * a.hq + h) * HD + dim;
-  *reinterpret_cast<uint2*>(a.out + at) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+// Partial results: rows of HD values, then a (maximum, sum) pair for each row; row (sequence x KV head, chunk, query vector).
+__host__ __device__ inline int64_t part_rows(const PagedAttnArgs& a) { return (int64_t)a.B * a.pg.hkv * a.splits * a.qpad; }
+__device__ inline int64_t part_row(const PagedAttnArgs& a, int bh, int c, int qv) {
+  return ((int64_t)bh * a.splits + c) * a.qpad + qv;
 }
 
-// Four e4m3 codes of a word to bf16.
-__device__ inline void unpack_e4m3(uint32_t w, bf16x2& lo, bf16x2& hi) {
-  lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.f, false);
-  hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w, 1.f, true);
+__device__ inline int64_t out_index(const PagedAttnArgs& a, int b, int r, int h, int HD, int dim) {
+  const int row = b * a.R + r;
+  return a.frag ? xfrag_index<uint16_t>(row, h * HD + dim, a.hq * HD / 32) : ((int64_t)row * a.hq + h) * HD + dim;
 }
-__device__ inline bf16x8 e4m3_frag(uint32_t x, uint32_t y) {
-  bf16x2 a, b, c, d;
-  unpack_e4m3(x, a, b);
-  unpack_e4m3(y, c, d);
+__device__ inline void store_out1(const PagedAttnArgs& a, int b, int r, int h, int HD, int dim, float y) {
+  a.out[out_index(a, b, r, h, HD, dim)] = f32_to_bf16(y);
+}
+__device__ inline void store_out4(const PagedAttnArgs& a, int b, int r, int h, int HD, int dim, const float* y) {
+  *reinterpret_cast<uint2*>(a.out + out_index(a, b, r, h, HD, dim)) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+}
+
+// Eight e4m3 codes to bf16, times a power of two (exact).
+__device__ inline bf16x8 e4m3_frag(uint32_t x, uint32_t y, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, scale, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)x, scale, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)y, scale, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)y, scale, true);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+// A query fragment as the products take it: scores are scaled by a.scale > 0 alone, so a negative scale's sign is the query's,
+// and a scale of 0 a query of zeros.
+__device__ inline uint4 load_q(const PagedAttnArgs& a, const uint16_t* q) {
+  uint4 v = load16(q);
+  v.x = (v.x & a.q_and) ^ a.q_xor, v.y = (v.y & a.q_and) ^ a.q_xor;
+  v.z = (v.z & a.q_and) ^ a.q_xor, v.w = (v.w & a.q_and) ^ a.q_xor;
+  return v;
 }
 __device__ inline uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-template <bool E4, int HD>
+template <bool E4, int HD, bool ONCE>
 __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a) {
   constexpr int KK = HD / 32, DB = HD / 16;
   constexpr int NK = E4 ? HD / 64 : HD / 32, NV = E4 ? HD / 32 : HD / 16;  // 16-byte loads of a step: 2 NK of K, NV of V
@@ -81,7 +118,7 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const Seq sq = attn_seq(a, b, threadIdx.x == 0 && c == 0 && kvh == 0 && qt == 0);
   if (sq.pos < 0) return;
-  const int total = sq.pos + a.R, chunk = chunk_of(total, a.max_splits), n_chunks = (total + chunk - 1) / chunk;
+  const int total = sq.pos + a.R, chunk = chunk_of(total, a.max_splits, a.wide), n_chunks = (total + chunk - 1) / chunk;
   if (c >= n_chunks) return;
   const int QV = a.R * a.grp, qv = qt * 16 + lane % 16;
   const bool qok = qv < QV;
@@ -101,7 +138,7 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
   uint4 q_frag = make_uint4(0, 0, 0, 0);
   if (wave < KK) {
     const uint16_t* Q = a.q + ((int64_t)(b * a.R + r) * a.hq + kvh * a.grp + hh) * HD;
-    q_frag = load16(Q + (E4 ? 64 * (wave / 2) + 16 * (lane / 16) + 8 * (wave % 2) : 32 * wave + g8));
+    q_frag = load_q(a, Q + (E4 ? 64 * (wave / 2) + 16 * (lane / 16) + 8 * (wave % 2) : 32 * wave + g8));
   }
   bool bad_page = false;
   // Where a step lies: the head's part of its page as a descriptor (one address register for all of a step's loads), the
@@ -130,36 +167,38 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
                  p & ((1 << lg) - 1), ok};
   };
   uint4 kr[2][NK], vr[NV];
-  uint2 ks = {0, 0}, vs = {0, 0};
+  uint8_t ks[2] = {0, 0};  // e4m3: scale byte of the lane's K row of each sub-tile
+  uint2 vs = {0, 0};      // and those of its 8 positions of V
   auto load = [&](const Place& pl, int off) {
-    // (non-temporal: a decode step reads a position once)
-    return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(pl.page, lane * 16, off, kNtCpol));
-  };
-  auto load_scales = [&](const Place& pl, int off) {
-    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-    const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(pl.page, g8, off, 0);
-    return make_uint2(v[0], v[1]);
+    // (ONCE: one query tile, which reads a position once: non-temporal)
+    return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(pl.page, lane * 16, off, ONCE ? kNtCpol : 0));
   };
   auto load_k = [&](const Place& pl) {
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
       for (int j = 0; j < NK; ++j) kr[s][j] = load(pl, pl.in * HD * (E4 ? 1 : 2) + (s * NK + j) * 1024);
-    if constexpr (E4) ks = load_scales(pl, 2 * a.pg.side + pl.in);
+    if constexpr (E4)
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+        ks[s] = __builtin_amdgcn_raw_buffer_load_b8(pl.page, kv_row(lane % 16, s), 2 * a.pg.side + pl.in, 0);
   };
   auto load_v = [&](const Place& pl) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) vr[j] = load(pl, a.pg.side + pl.in * HD * (E4 ? 1 : 2) + j * 1024);
-    if constexpr (E4) vs = load_scales(pl, 2 * a.pg.side + (1 << lg) + pl.in);
+    if constexpr (E4) {
+      const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(pl.page, g8, 2 * a.pg.side + (1 << lg) + pl.in, 0);
+      vs = make_uint2(v[0], v[1]);
+    }
   };
 
   f32x4 o[DB];
-  float m, l;
-  bool wild;
+  float m, l;        // (m: of the scores before the scale)
+  float ref, m_far;  // -m scale (0 for no m), and the score from which m moves
   auto reset = [&]() {
 #pragma unroll
     for (int db = 0; db < DB; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
-    m = -INFINITY, l = 0.f, wild = false;
+    m = -INFINITY, l = 0.f, ref = 0.f, m_far = -INFINITY;
   };
   reset();
   // V operand of 16 dimensions, positions outside `mask` (a bit for each of the lane's 8) zeroed: their weights are 0, and 0
@@ -176,7 +215,7 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
         }
         x &= mx, y &= my;
       }
-      return e4m3_frag(x, y);
+      return e4m3_frag(x, y, 1.f);
     } else {
       uint4 w = vr[db];
       if (mask != 255) {
@@ -208,7 +247,7 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
       for (int t = 0; t < 2; ++t) {
         bf16x8 k;
         if constexpr (E4)
-          k = e4m3_frag(word(kr[t][i / 2], i % 2 * 2), word(kr[t][i / 2], i % 2 * 2 + 1));
+          k = e4m3_frag(word(kr[t][i / 2], i % 2 * 2), word(kr[t][i / 2], i % 2 * 2 + 1), scale_value(ks[t]));
         else
           k = __builtin_bit_cast(bf16x8, kr[t][i]);
         s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q, s[t], 0, 0, 0);
@@ -217,16 +256,13 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
     // s[i / 4][i % 4]: position p + g8 + i, query vector lane % 16
     float sv[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      sv[i] = s[i / 4][i % 4] * a.scale;
-      if constexpr (E4) sv[i] *= scale_value(((i < 4 ? ks.x : ks.y) >> (8 * (i % 4))) & 255);
-    }
+    for (int i = 0; i < 8; ++i) sv[i] = s[i / 4][i % 4];
     // K's registers are free: the next step's loads go out ahead of this one's softmax, V's after its product
     pl = place(p + kStride);
     load_k(pl);
     __builtin_amdgcn_sched_barrier(0);
-    const bool whole = p + 32 <= p_end && ok;  // (the same in every lane: products run with all of them)
-    if (p + 31 > lo || !whole) {
+    const bool inner = p + 31 <= lo && p + 32 <= p_end && ok;  // every query vector sees the whole step
+    if (!inner) {
       const int end = ok ? min(qpos + 1, p_end) : 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) sv[i] = p + g8 + i < end ? sv[i] : -INFINITY;
@@ -236,27 +272,28 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
     for (int i = 1; i < 8; ++i) top = fmaxf(top, sv[i]);
     top = xor16_op(top, [](float x, float y) { return fmaxf(x, y); });
     top = xor32_op(top, [](float x, float y) { return fmaxf(x, y); });
-    const float mn = fmaxf(m, top);
-    if (__any(mn != m)) {
-      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+    if (__any(top * a.scale > m_far)) {
+      const float mn = fmaxf(m, top), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * a.scale);
       l *= f;
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[db] *= f;
       m = mn;
+      ref = m == -INFINITY ? 0.f : -m * a.scale;  // (a hidden score's weight is then exp2(-inf) = 0)
+      m_far = m == -INFINITY ? -INFINITY : kFar - ref;
     }
-    const float ref = m == -INFINITY ? 0.f : m;  // (a hidden score's weight is then exp2(-inf) = 0)
     float e[8], sum = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      e[i] = __builtin_amdgcn_exp2f(sv[i] - ref);
+      e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[i], a.scale, ref));
       sum += e[i];
     }
     l += sum;
     if constexpr (E4) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float x = e[i] * scale_value(((i < 4 ? vs.x : vs.y) >> (8 * (i % 4))) & 255);
-        e[i] = sv[i] == -INFINITY ? 0.f : x;  // (a position that was never written may have any scale byte)
+      for (int i = 0; i < 8; ++i) e[i] *= scale_value(((i < 4 ? vs.x : vs.y) >> (8 * (i % 4))) & 255);
+      if (!inner) {  // (a position that was never written may have any scale byte)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = sv[i] == -INFINITY ? 0.f : e[i];
       }
     }
     const bf16x8 pf = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]),
@@ -271,17 +308,14 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
           if (lane % 16 == q) o[db] = y;  // (a product's columns are independent: the others are not taken)
         }
       }
-    } else if (whole && p + 31 <= lo) {
+    } else if (inner) {
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(db, 255), pf, o[db], 0, 0, 0);
     } else {
       const uint32_t mask = below(p, ok ? p_end : 0);
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        const bf16x8 v = v_frag(db, mask);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) wild |= !__builtin_isfinite((float)v[i]);
-        o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pf, o[db], 0, 0, 0);
+        o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(db, mask), pf, o[db], 0, 0, 0);
       }
     }
   };
@@ -302,13 +336,22 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
   };
   steps(std::false_type{});
   // On the tile's diagonal a position may be hidden from some of the query vectors only.  Where a V value there is not finite,
-  // the zero weight of those vectors has not kept it out: the wave's steps again, each vector's product by itself.
-  if (lo + 1 < tile_end && __any(wild)) {
-    reset();
-    page0 = p_begin >> lg;
-    load_ids();
-    steps(std::true_type{});
+  // the zero weight of those vectors has not kept it out, and their sums are not finite: then the wave's steps again, each
+  // vector's product by itself.
+  if (lo + 1 < tile_end && p_end > lo + 1) {
+    bool wild = false;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) wild |= !__builtin_isfinite(o[db][i]);
+    if (__any(wild)) {
+      reset();
+      page0 = p_begin >> lg;
+      load_ids();
+      steps(std::true_type{});
+    }
   }
+  m *= a.scale;  // (-inf stays: the scale is positive)
   if (a.err && bad_page && lane == 0) atomicOr(a.err, kErrId);
   l = xor16_op(l, [](float x, float y) { return x + y; });
   l = xor32_op(l, [](float x, float y) { return x + y; });
@@ -319,9 +362,9 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
     s_l[wave][lane] = l;
   }
   __syncthreads();
-  const int64_t slot = ((int64_t)(b * hkv + kvh) * a.qtiles + qt) * a.splits + c;
-  float* part_o = a.part + slot * 16 * HD;
-  float* part_ml = a.part + (int64_t)a.B * hkv * a.qtiles * a.splits * 16 * HD + slot * 32;
+  const int64_t at = part_row(a, b * hkv + kvh, c, qt * 16);
+  float* part_o = a.part + at * HD;
+  float* part_ml = a.part + part_rows(a) * HD + at * 2;
   for (int e = threadIdx.x; e < 16 * HD / 4; e += kThreads) {
     const int q = e / (HD / 4), d = e % (HD / 4) * 4;
     if (qt * 16 + q >= QV) continue;
@@ -354,72 +397,514 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
   }
 }
 
-// Joins the chunks of a query vector: kJoin groups of HD / 4 lanes (4 dimensions a lane) take the chunks g, g + kJoin, ... in
-// order, several loads in flight, and are added in order of g.  A workgroup holds kThreads / (kJoin HD / 4) query vectors.
-constexpr int kJoin = 4;
-template <int HD>
-__global__ void __launch_bounds__(kThreads) paged_combine_kernel(PagedAttnArgs a) {
-  constexpr int LN = HD / 4, VEC = kThreads / (LN * kJoin), U = 4;
-  __shared__ __align__(16) float s_y[kThreads][4];
-  __shared__ float s_l[kThreads / LN];
-  const int grp = threadIdx.x / LN, g = grp % kJoin, ln = threadIdx.x % LN, d = 4 * ln, QV = a.R * a.grp;
-  const int64_t idx = (int64_t)blockIdx.x * VEC + grp / kJoin, bh = idx / QV;
-  const int qv = (int)(idx % QV), b = (int)(bh / a.pg.hkv), kvh = (int)(bh % a.pg.hkv);
-  Seq sq{-1, 0};
-  if (b < a.B) sq = attn_seq(a, b, false);
-  const int total = sq.pos + a.R, chunk = chunk_of(total, a.max_splits), n = sq.pos < 0 ? 1 : (total + chunk - 1) / chunk;
-  float y[4] = {0.f, 0.f, 0.f, 0.f}, L = 0.f;
-  if (n > 1) {
-    const int64_t slot = (bh * a.qtiles + qv / 16) * a.splits;
-    const float* o = a.part + (slot * 16 + qv % 16) * HD + d;
-    const float* ml = a.part + (int64_t)a.B * a.pg.hkv * a.qtiles * a.splits * 16 * HD + (slot * 16 + qv % 16) * 2;
-    float M = -INFINITY;
-    for (int c = ln; c < n; c += LN) M = fmaxf(M, ml[32 * c]);
+// ---- many query vectors ---------------------------------------------------------------------------------
+//
+// A workgroup takes NW tiles of 32 query vectors of one KV head, a wave each (queries and accumulators in registers), over one
+// chunk.  The steps of K and V pass through a ring in LDS, loaded there directly (no registers, several steps in flight) and
+// read by every wave; e4m3 operands are converted on their way from LDS to the products.  S^T = K Q^T and O^T = V^T P^T by
+// 32x32x16 products: a lane holds 16 scores of one query vector, which are its operand of the second product as they stand
+// (the stored order of K's rows sees to that).
+
+// N reads of 16 (8) bytes a lane from addr + off(i), and their wait, in one block: the compiler would hold every LDS read back
+// until all direct loads into LDS, those of later steps too, have landed.
+template <int N, int DIV, int HI, int LO>  // off(i) = i / DIV * HI + i % DIV * LO
+__device__ inline void lds_read16(u32x4* f, uint32_t addr) {
+  constexpr auto off = [](int i) { return i / DIV * HI + i % DIV * LO; };
+  static_assert(N == 2 || N == 4 || N == 8, "reads of a block");
+  if constexpr (N == 2) {
+    asm volatile("ds_read_b128 %0, %2 offset:%3\n\tds_read_b128 %1, %2 offset:%4\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(f[0]), "=&v"(f[1]) : "v"(addr), "i"(off(0)), "i"(off(1)) : "memory");
+  } else if constexpr (N == 4) {
+    asm volatile("ds_read_b128 %0, %4 offset:%5\n\tds_read_b128 %1, %4 offset:%6\n\tds_read_b128 %2, %4 offset:%7\n\t"
+                 "ds_read_b128 %3, %4 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
+                 : "v"(addr), "i"(off(0)), "i"(off(1)), "i"(off(2)), "i"(off(3)) : "memory");
+  } else {
+    asm volatile("ds_read_b128 %0, %8 offset:%9\n\tds_read_b128 %1, %8 offset:%10\n\tds_read_b128 %2, %8 offset:%11\n\t"
+                 "ds_read_b128 %3, %8 offset:%12\n\tds_read_b128 %4, %8 offset:%13\n\tds_read_b128 %5, %8 offset:%14\n\t"
+                 "ds_read_b128 %6, %8 offset:%15\n\tds_read_b128 %7, %8 offset:%16\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3]), "=&v"(f[4]), "=&v"(f[5]), "=&v"(f[6]), "=&v"(f[7])
+                 : "v"(addr), "i"(off(0)), "i"(off(1)), "i"(off(2)), "i"(off(3)), "i"(off(4)), "i"(off(5)), "i"(off(6)), "i"(off(7))
+                 : "memory");
+  }
+}
+template <int N, int STEP>
+__device__ inline void lds_read8(u32x2* f, uint32_t addr) {
+  static_assert(N == 4 || N == 8, "reads of a block");
+  if constexpr (N == 4) {
+    asm volatile("ds_read_b64 %0, %4\n\tds_read_b64 %1, %4 offset:%5\n\tds_read_b64 %2, %4 offset:%6\n\t"
+                 "ds_read_b64 %3, %4 offset:%7\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
+                 : "v"(addr), "i"(STEP), "i"(2 * STEP), "i"(3 * STEP) : "memory");
+  } else {
+    asm volatile("ds_read_b64 %0, %8\n\tds_read_b64 %1, %8 offset:%9\n\tds_read_b64 %2, %8 offset:%10\n\t"
+                 "ds_read_b64 %3, %8 offset:%11\n\tds_read_b64 %4, %8 offset:%12\n\tds_read_b64 %5, %8 offset:%13\n\t"
+                 "ds_read_b64 %6, %8 offset:%14\n\tds_read_b64 %7, %8 offset:%15\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3]), "=&v"(f[4]), "=&v"(f[5]), "=&v"(f[6]), "=&v"(f[7])
+                 : "v"(addr), "i"(STEP), "i"(2 * STEP), "i"(3 * STEP), "i"(4 * STEP), "i"(5 * STEP), "i"(6 * STEP), "i"(7 * STEP)
+                 : "memory");
+  }
+}
+
+// An e4m3 step's K operands (N reads of 16 bytes, 512 apart) and scale bytes, as above.
+template <int N>
+__device__ inline void lds_read_e4(u32x4* k, u32x2* sb, uint32_t ak, uint32_t aks, uint32_t avs) {
+  static_assert(N == 2 || N == 4, "reads of a block");
+  uint32_t ks;
+  if constexpr (N == 2) {
+    asm volatile("ds_read_u8 %2, %6\n\tds_read_b128 %0, %5\n\tds_read_b128 %1, %5 offset:512\n\tds_read_b64 %3, %7\n\t"
+                 "ds_read_b64 %4, %7 offset:16\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(k[0]), "=&v"(k[1]), "=&v"(ks), "=&v"(sb[1]), "=&v"(sb[2]) : "v"(ak), "v"(aks), "v"(avs) : "memory");
+  } else {
+    asm volatile("ds_read_u8 %4, %8\n\tds_read_b128 %0, %7\n\tds_read_b128 %1, %7 offset:512\n\tds_read_b128 %2, %7 offset:1024\n\t"
+                 "ds_read_b128 %3, %7 offset:1536\n\tds_read_b64 %5, %9\n\tds_read_b64 %6, %9 offset:16\n\ts_waitcnt lgkmcnt(0)"
+                 : "=&v"(k[0]), "=&v"(k[1]), "=&v"(k[2]), "=&v"(k[3]), "=&v"(ks), "=&v"(sb[1]), "=&v"(sb[2])
+                 : "v"(ak), "v"(aks), "v"(avs) : "memory");
+  }
+  sb[0][0] = ks;
+}
+
+// The 32 query vectors from q0 over positions [p_begin, p_end), one after the other and position by position: what a wave whose
+// products met a non-finite V on the diagonal computes instead.  A lane holds HD / 64 dimensions.
+template <bool E4, int HD>
+__device__ inline void wide_one_by_one(const PagedAttnArgs& a, const Seq& sq, int b, int kvh, int q0, int c, int p_begin, int p_end,
+                                       bool whole) {
+  constexpr int N = HD / 64;
+  const int lane = threadIdx.x % kWave, d0 = N * lane, lg = a.pg.log_page;
+  auto value = [&](const char* side, int off) {
+    if constexpr (E4)
+      return (float)e4m3_frag(*reinterpret_cast<const uint8_t*>(side + off), 0, 1.f)[0];
+    else
+      return bf16_to_f32(*reinterpret_cast<const uint16_t*>(side + off));
+  };
+#pragma unroll 1
+  for (int qv = q0; qv < min(q0 + 32, a.R * a.grp); ++qv) {
+    const int r = a.by_grp.div(qv), hh = qv - r * a.grp;
+    const uint16_t* Q = a.q + ((int64_t)(b * a.R + r) * a.hq + kvh * a.grp + hh) * HD + d0;
+    float q[N], y[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int k = 1; k < LN; k *= 2) M = fmaxf(M, __shfl_xor(M, k));
-    for (int c0 = g; c0 < n; c0 += kJoin * U) {
-      f32x4 v[U];
-      float mc[U], lc[U];
+    for (int i = 0; i < N; ++i) q[i] = bf16_to_f32((uint16_t)((Q[i] & a.q_and) ^ (a.q_xor & 0x8000u)));
+#pragma unroll 1
+    for (int p = p_begin; p < min(p_end, sq.pos + r + 1); ++p) {
+      const int id = a.pg.table[(int64_t)sq.row * a.pg.width + (p >> lg)], in = p & ((1 << lg) - 1);
+      if ((unsigned)id >= (unsigned)a.pg.n_pages) continue;
+      const char* k = page_head(a.pg, id, kvh);
+      float s = 0.f;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int c = min(c0 + kJoin * u, n - 1);
-        mc[u] = ml[32 * c], lc[u] = ml[32 * c + 1];
-        v[u] = *reinterpret_cast<const f32x4*>(o + (int64_t)c * 16 * HD);
+      for (int i = 0; i < N; ++i) s += q[i] * value(k, page_k_offset<E4, HD>(in, d0 + i));
+      s = wave_sum(s) * a.scale;
+      float vs = 1.f;
+      if constexpr (E4) {
+        s *= scale_value((uint8_t)k[2 * a.pg.side + in]);
+        vs = scale_value((uint8_t)k[2 * a.pg.side + (1 << lg) + in]);
       }
+      const float mn = fmaxf(m, s), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+      const float w = __builtin_amdgcn_exp2f(s - (mn == -INFINITY ? 0.f : mn));
+      l = l * f + w;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (c0 + kJoin * u >= n) break;
-        const float f = mc[u] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mc[u] - M);
-        L += f * lc[u];
+      for (int i = 0; i < N; ++i) y[i] = y[i] * f + w * (vs * value(k + a.pg.side, page_v_offset<E4, HD>(in, d0 + i)));
+      m = mn;
+    }
+    if (whole) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] += f * v[u][i];
+      for (int i = 0; i < N; ++i) store_out1(a, b, r, kvh * a.grp + hh, HD, d0 + i, l == 0.f ? 0.f : y[i] / l);
+    } else {
+      const int64_t row = part_row(a, b * a.pg.hkv + kvh, c, qv);
+#pragma unroll
+      for (int i = 0; i < N; ++i) a.part[row * HD + d0 + i] = y[i];
+      if (lane == 0) {
+        a.part[part_rows(a) * HD + row * 2] = m;
+        a.part[part_rows(a) * HD + row * 2 + 1] = l;
       }
     }
   }
-  *reinterpret_cast<f32x4*>(s_y[threadIdx.x]) = f32x4{y[0], y[1], y[2], y[3]};
-  if (ln == 0) s_l[grp] = L;
-  __syncthreads();
-  if (g != 0 || n == 1) return;
+}
+
+template <bool E4, int HD>
+__global__ void __launch_bounds__(kWideWaves * kWave, E4 ? 2 : 3) paged_attn_wide_kernel(PagedAttnArgs a) {
+  constexpr int NW = kWideWaves;
+  constexpr int KS = HD / 16, DB = HD / 32;   // products of a tile and step: KS for the scores, 2 DB for the values
+  constexpr int NB = (E4 ? 2 : 4) * HD / 32;  // 1 KiB blocks of a step, K's then V's
+  constexpr int L = NB / NW + (E4 ? 1 : 0);   // loads that a wave issues for a step (e4m3: its own copy of the scale bytes)
+  constexpr int kStage = NB * 1024 + (E4 ? NW * 256 : 0);
+  constexpr int RS = E4 ? 5 : 3;              // ring stages: RS - 1 steps in flight, of 8 or 16 KiB
+  static_assert(NB % NW == 0, "a step's blocks over the waves");
+  __shared__ __align__(16) char s_ring[RS * kStage];
+  touch_kernargs<PagedAttnArgs>();
+  const int hkv = a.pg.hkv;
+  const int low = blockIdx.x % kXcds, rest = blockIdx.x / kXcds;
+  const int group = a.by_qtiles.div(rest), qb = a.qtiles - 1 - (rest - group * a.qtiles), item = group * kXcds + low;
+  if (item >= a.splits * a.B * hkv) return;
+  const int bc = a.by_hkv.div(item), kvh = item - bc * hkv, c = a.by_b.div(bc), b = bc - c * a.B;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, half = lane / 32;
+  const Seq sq = attn_seq(a, b, threadIdx.x == 0 && c == 0 && kvh == 0 && qb == 0);
+  if (sq.pos < 0) return;
+  const int total = sq.pos + a.R, chunk = chunk_of(total, a.max_splits, a.wide), n_chunks = (total + chunk - 1) / chunk;
+  if (c >= n_chunks) return;
+  const int QV = a.R * a.grp, q_block = qb * NW * 32, q0 = q_block + wave * 32, qv = q0 + lane % 32;
+  const int block_end = __builtin_amdgcn_readfirstlane(sq.pos + min(a.R - 1, a.by_grp.div(q_block + NW * 32 - 1)) + 1);
+  const int p_begin = c * chunk, p_end = min(block_end, p_begin + chunk);
+  // the lane's query's position (-1: none), the tile's first position, the one past its last (0: no queries)
+  const bool qok = qv < QV;
+  const int r = qok ? a.by_grp.div(qv) : 0, hh = qok ? qv - r * a.grp : 0;
+  const int qpos = qok ? sq.pos + r : -1;
+  const int lo = __builtin_amdgcn_readfirstlane(q0 + 31 < QV ? sq.pos + a.by_grp.div(q0) : -1);
+  const int tile_end = __builtin_amdgcn_readfirstlane(q0 < QV ? sq.pos + min(a.R - 1, a.by_grp.div(q0 + 31)) + 1 : 0);
+  const int lg = a.pg.log_page;
+  int page0 = p_begin >> lg, ids = 0;  // the chunk's page ids, 64 at a time across the lanes
+  auto load_ids = [&]() { ids = a.pg.table[(int64_t)sq.row * a.pg.width + min(page0 + lane, a.pg.width - 1)]; };
+  load_ids();
+  bf16x8 qf[KS];  // fragment i: the dimensions of the i-th K operand
+  {
+    const uint16_t* Q = a.q + ((int64_t)(b * a.R + r) * a.hq + kvh * a.grp + hh) * HD;
+#pragma unroll
+    for (int i = 0; i < KS; ++i)
+      qf[i] = __builtin_bit_cast(bf16x8, load_q(a, Q + (E4 ? 64 * (i / 4) + 32 * (i / 2 % 2) + 16 * half + 8 * (i % 2) : 16 * i + 8 * half)));
+  }
+  bool bad_page = false;
+  int p_load = p_begin, slot = 0;  // next step to load, its byte offset in the ring
+  uint32_t ok_bits = 0;            // whether the pages of the steps in flight exist, the oldest in bit RS - 2
+  // the page of the next step: its head's bytes, their number (0 for a missing page)
+  char* page_at = nullptr;
+  int page_bytes = 0;
+  const int in_mask = (1 << lg) - 1;
+  auto turn_page = [&]() {
+    const int i = min(p_load, max(p_end - 1, p_begin)) >> lg;
+    int id;
+    if (i - page0 < kWave) {
+      id = __builtin_amdgcn_readlane(ids, i - page0);
+    } else {  // (read here as well, so that only this path waits for the load)
+      page0 += kWave;
+      load_ids();
+      id = __builtin_amdgcn_readlane(ids, i - page0);
+    }
+    const bool ok = (unsigned)id < (unsigned)a.pg.n_pages;
+    bad_page |= !ok && p_load < p_end;
+    page_at = page_head(a.pg, ok ? id : 0, kvh);
+    page_bytes = ok ? a.pg.head_bytes : 0;
+  };
+  auto issue = [&]() {
+    const int in = p_load & in_mask, at = in * HD * (E4 ? 1 : 2);
+    if (in == 0) turn_page();
+    ok_bits = ok_bits << 1 | (page_bytes ? 1u : 0u);
+    // (past the end, and for a missing page, loads of no memory: the count in flight stays the same)
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(page_at, 0, p_load < p_end ? page_bytes : 0, kBufferRsrcWord3);
+    char* st = s_ring + slot;
+#pragma unroll
+    for (int j = 0; j < NB / NW; ++j) {
+      const int blk = wave + NW * j;
+      load_lds16<0>(rs, st + blk * 1024, lane * 16, blk < NB / 2 ? at + blk * 1024 : a.pg.side + at + (blk - NB / 2) * 1024);
+    }
+    if constexpr (E4)  // 16 lanes of 4 bytes: K's 32 scale bytes, V's
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)(st + NB * 1024 + wave * 256), 4,
+                                               lane < 16 ? lane % 8 * 4 + (lane / 8 << lg) : 0x7ffffff0, 2 * a.pg.side + in, 0, 0);
+    p_load += 32;
+    slot = slot + kStage == RS * kStage ? 0 : slot + kStage;
+  };
+
+  const uint32_t ring = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(s_ring);
+  const int rho = lane % 16, b16 = lane % 32 / 16;
+  const uint32_t rd_k = ring + b16 * (NB / 4) * 1024 + (16 * half + rho) * 16;
+  const uint32_t rd_v = ring + NB / 2 * 1024 + (E4 ? (16 * half + rho) * 16 + 8 * b16 : b16 * 1024 + (16 * half + rho) * 16);
+  const uint32_t rd_ks = ring + NB * 1024 + wave * 256 + kv_row(rho, b16), rd_vs = ring + NB * 1024 + wave * 256 + 32 + 8 * half;
+  f32x16 o[DB];
+  float m = -INFINITY, l = 0.f;           // (m: of the scores before the scale)
+  float ref = 0.f, m_far = -INFINITY;     // -m scale (0 for no m), and the score from which m moves
+  {
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+    turn_page();
+#pragma unroll
+    for (int i = 0; i < RS - 1; ++i) issue();
+    uint32_t so = 0;  // this step's byte offset in the ring
+    auto next_step = [&]() {
+      __builtin_amdgcn_s_waitcnt(wait_vmcnt((RS - 2) * L));
+      phase_barrier();  // the step is whole, and the slot of the step before it has been read by every wave
+      issue();
+    };
+    // Step p, at so in the ring.  INNER: every query vector sees the whole of it.
+    auto step = [&](auto inner_c, int p, bool ok) {
+      constexpr bool inner = decltype(inner_c)::value;
+      const uint32_t at_step = so;
+      f32x16 s;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = 0.f;
+      float vs[E4 ? 16 : 1];
+      auto at = [&](int i) { return 16 * (i / 4 % 2) + 8 * half + 4 * (i / 8) + i % 4; };  // position of s[i]
+      if constexpr (E4) {
+        u32x4 kr[KS / 2];
+        u32x2 sb[3];  // scale bytes: of the lane's K row, V's of positions 8 half .. and 16 + 8 half ..
+        lds_read_e4<KS / 2>(kr, sb, rd_k + at_step, rd_ks + at_step, rd_vs + at_step);
+        const float ks = scale_value((int)sb[0][0]);
+#pragma unroll
+        for (int i = 0; i < KS; ++i)
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(e4m3_frag(kr[i / 2][i % 2 * 2], kr[i / 2][i % 2 * 2 + 1], ks), qf[i], s, 0, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)  // byte 4 (i / 8) + i % 4 of the eight from 16 (i / 4 % 2) + 8 half
+          vs[i] = scale_value((sb[1 + i / 4 % 2][i / 8] >> (8 * (i % 4))) & 255);
+      } else {
+#pragma unroll
+        for (int h = 0; h < KS; h += 4) {
+          u32x4 kr[4];
+          lds_read16<4, 4, 0, 512>(kr, rd_k + at_step + h * 512);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[i]), qf[h + i], s, 0, 0, 0);
+        }
+      }
+      float sv[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sv[i] = s[i];
+      if constexpr (!inner) {
+        const int e = ok ? min(qpos + 1, p_end) : 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sv[i] = p + at(i) < e ? sv[i] : -INFINITY;
+      }
+      float top = sv[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, sv[i]);
+      top = xor32_op(top, [](float x, float y) { return fmaxf(x, y); });
+      if (__any(top * a.scale > m_far)) {
+        const float mn = fmaxf(m, top);
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * a.scale);
+        l *= f;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[db][i] *= f;
+        m = mn;
+        ref = m == -INFINITY ? 0.f : -m * a.scale;
+        m_far = m == -INFINITY ? -INFINITY : kFar - ref;
+      }
+      float e[16], sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[i], a.scale, ref));
+        sum += e[i];
+      }
+      l += sum;
+      if constexpr (E4) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) e[i] *= vs[i];
+        if constexpr (!inner) {  // (a position that was never written may have any scale byte)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) e[i] = sv[i] == -INFINITY ? 0.f : e[i];
+        }
+      }
+      bf16x8 pf[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)  // positions 16 h + 8 half .. + 7: registers 4 h .. and 8 + 4 h ..
+        pf[h] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16x2(e[4 * h], e[4 * h + 1]), pack_bf16x2(e[4 * h + 2], e[4 * h + 3]),
+                                                      pack_bf16x2(e[8 + 4 * h], e[9 + 4 * h]),
+                                                      pack_bf16x2(e[10 + 4 * h], e[11 + 4 * h])));
+      // V operands, 64 dimensions at a time: operand 2 db + h holds dimension 32 db + lane % 32, positions 16 h + 8 half .. + 7
+#pragma unroll
+      for (int g = 0; g < DB; g += 2) {
+        bf16x8 v[4];
+        if constexpr (E4) {
+          u32x2 vr[4];
+          lds_read8<4, 512>(vr, rd_v + at_step + g * 1024);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = e4m3_frag(vr[i][0], vr[i][1], 1.f);
+        } else {
+          u32x4 vr[4];
+          lds_read16<4, 2, 2048, 512>(vr, rd_v + at_step + g * 2048);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(bf16x8, vr[i]);
+        }
+        if constexpr (!inner) {  // positions from p_end on zeroed: their weights are 0, and 0 times a stale non-finite value would not be
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int n = (ok ? p_end : 0) - (p + 16 * (i % 2) + 8 * half);
+            u32x4 w = __builtin_bit_cast(u32x4, v[i]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] &= (2 * k < n ? 0xffffu : 0u) | (2 * k + 1 < n ? 0xffff0000u : 0u);
+            v[i] = __builtin_bit_cast(bf16x8, w);
+          }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int db = 0; db < 2; ++db) o[g + db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[2 * db + h], pf[h], o[g + db], 0, 0, 0);
+      }
+    };
+    int p = p_begin;
+    // the steps that every query vector sees whole, up to a missing page; then the others (one loop after the other: as the two
+    // sides of a branch in one loop they would each copy the accumulators)
+    const int p_inner = min(min(lo - 31, p_end - 32), tile_end - 1);
+#pragma unroll 1
+    for (; p <= p_inner && (ok_bits >> (RS - 2) & 1); p += 32) {
+      next_step();
+      step(std::true_type{}, p, true);
+      so = so + kStage == (uint32_t)(RS * kStage) ? 0 : so + kStage;
+    }
+#pragma unroll 1
+    for (; p < min(p_end, tile_end); p += 32) {
+      const bool ok = ok_bits >> (RS - 2) & 1;
+      next_step();
+      step(std::false_type{}, p, ok);
+      so = so + kStage == (uint32_t)(RS * kStage) ? 0 : so + kStage;
+    }
+    for (; p < p_end; p += 32) next_step();  // (steps behind the tile's last position: the other waves')
+    __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));  // (the loads past the end: they clear LDS)
+  }
+  if (a.err && bad_page && threadIdx.x == 0) atomicOr(a.err, kErrId);
+  const float lsum = xor32_op(l, [](float x, float y) { return x + y; });
+  // On the diagonal a position may be hidden from some of the query vectors only.  Where a V value there is not finite, the zero
+  // weight of those vectors has not kept it out, and their sums are not finite: then the wave's vectors one by one.
+  if (p_end > (lo < 0 ? sq.pos : lo) + 1) {
+    bool wild = false;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) wild |= !__builtin_isfinite(o[db][i]);
+    if (__any(wild)) {
+      wide_one_by_one<E4, HD>(a, sq, b, kvh, q0, c, p_begin, p_end, n_chunks == 1);
+      return;
+    }
+  }
+  if (!qok) return;
+  const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
+  const int64_t row = part_row(a, b * hkv + kvh, c, qv);
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {  // dimensions 32 db + 8 i + 4 half .. + 3
+      const int d = 32 * db + 8 * i + 4 * half;
+      float y[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y[k] = o[db][4 * i + k];
+      if (n_chunks == 1) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) y[k] = lsum == 0.f ? 0.f : y[k] * inv;
+        store_out4(a, b, r, kvh * a.grp + hh, HD, d, y);
+      } else {
+        *reinterpret_cast<f32x4*>(a.part + row * HD + d) = f32x4{y[0], y[1], y[2], y[3]};
+      }
+    }
+  if (n_chunks > 1 && half == 0) {
+    float* ml = a.part + part_rows(a) * HD + row * 2;
+    ml[0] = m * a.scale;
+    ml[1] = lsum;
+  }
+}
+
+// Joins the chunks of a query vector, 4 dimensions a lane: four sums, of the chunks c = g mod 4 in order, added in order of g.
+// A call whose sequences have few chunks takes one group of HD / 4 lanes for all four (SMALL: up to kSmallJoin chunks, all of a
+// vector's loads in flight at once); others a group for each.  The sums are the same.
+constexpr int kJoin = 4, kSmallJoin = 16;
+template <int HD, bool SMALL>
+__global__ void __launch_bounds__(kThreads) paged_combine_kernel(PagedAttnArgs a) {
+  constexpr int LN = HD / 4, VEC = kThreads / (SMALL ? LN : LN * kJoin);
+  __shared__ __align__(16) float s_y[SMALL ? 1 : kThreads][4];
+  __shared__ float s_l[kThreads / LN];
+  const int grp = threadIdx.x / LN, ln = threadIdx.x % LN, d = 4 * ln, QV = a.R * a.grp;
+  const int idx = (int)blockIdx.x * VEC + (SMALL ? grp : grp / kJoin);
+  const int bh = a.by_qv.div(idx), qv = idx - bh * QV, b = a.by_hkv.div(bh), kvh = bh - b * a.pg.hkv;
+  int n = 1;
+  if (b < a.B) {
+    int p = a.rows ? a.rows[(int64_t)b * a.R].pos : a.len[b];
+    const bool ok = (!a.rows || a.rows[(int64_t)b * a.R].valid) && p >= 0 && (int64_t)p + a.R <= a.max_len;
+    const int total = p + a.R;
+    if (ok) n = (total + chunk_of(total, a.max_splits, a.wide) - 1) / chunk_of(total, a.max_splits, a.wide);
+  }
+  const int64_t at = part_row(a, bh, 0, qv), stride = a.qpad;  // (of a chunk)
+  const float* o = a.part + at * HD + d;
+  const float* ml = a.part + part_rows(a) * HD + at * 2;
+  f32x4 y[kJoin];
+  float L[kJoin], M = -INFINITY;
+#pragma unroll
+  for (int g = 0; g < kJoin; ++g) y[g] = f32x4{0.f, 0.f, 0.f, 0.f}, L[g] = 0.f;
+  auto add = [&](int g, float mc, float lc, const f32x4& v) {
+    const float f = mc == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mc - M);  // (no maximum: a sum of 0, or of NaN scores)
+    L[g] += f * lc;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[g][i] += f * v[i];
+  };
+  if constexpr (SMALL) {
+    if (n == 1) return;
+    constexpr int U = 8;
+    float2 p[kSmallJoin];
+    f32x4 v[U];
+#pragma unroll
+    for (int c = 0; c < kSmallJoin; ++c) p[c] = *reinterpret_cast<const float2*>(ml + 2 * stride * min(c, n - 1));
+#pragma unroll
+    for (int c = 0; c < U; ++c) v[c] = *reinterpret_cast<const f32x4*>(o + stride * min(c, n - 1) * HD);
+#pragma unroll
+    for (int c = 0; c < kSmallJoin; ++c) M = fmaxf(M, p[c].x);
+#pragma unroll
+    for (int c = 0; c < U; ++c)
+      if (c < n) add(c % kJoin, p[c].x, p[c].y, v[c]);
+    if (n > U) {
+#pragma unroll
+      for (int c = 0; c < U; ++c) v[c] = *reinterpret_cast<const f32x4*>(o + stride * min(U + c, n - 1) * HD);
+#pragma unroll
+      for (int c = 0; c < U; ++c)
+        if (U + c < n) add(c % kJoin, p[U + c].x, p[U + c].y, v[c]);
+    }
+  } else {
+    constexpr int U = 8;
+    const int g = grp % kJoin;
+    if (n > 1) {
+      for (int c = ln; c < n; c += LN) M = fmaxf(M, ml[2 * stride * c]);
+#pragma unroll
+      for (int k = 1; k < LN; k *= 2) M = fmaxf(M, __shfl_xor(M, k));
+      for (int c0 = g; c0 < n; c0 += kJoin * U) {
+        f32x4 v[U];
+        float2 p[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int c = min(c0 + kJoin * u, n - 1);
+          p[u] = *reinterpret_cast<const float2*>(ml + 2 * stride * c);
+          v[u] = *reinterpret_cast<const f32x4*>(o + stride * c * HD);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (c0 + kJoin * u < n) add(0, p[u].x, p[u].y, v[u]);
+      }
+    }
+    *reinterpret_cast<f32x4*>(s_y[threadIdx.x]) = y[0];
+    if (ln == 0) s_l[grp] = L[0];
+    __syncthreads();
+    if (g != 0 || n == 1) return;
+#pragma unroll
+    for (int k = 1; k < kJoin; ++k) {
+      L[k] = s_l[grp + k];
+      y[k] = *reinterpret_cast<const f32x4*>(s_y[threadIdx.x + k * LN]);
+    }
+  }
 #pragma unroll
   for (int k = 1; k < kJoin; ++k) {
-    L += s_l[grp + k];
-    const f32x4 v = *reinterpret_cast<const f32x4*>(s_y[threadIdx.x + k * LN]);
+    L[0] += L[k];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] += v[i];
+    for (int i = 0; i < 4; ++i) y[0][i] += y[k][i];
   }
-  const float inv = 1.f / L;
+  const float inv = 1.f / L[0];
+  float out[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) y[i] = L == 0.f ? 0.f : y[i] * inv;
-  store_out4(a, b, qv / a.grp, kvh * a.grp + qv % a.grp, HD, d, y);
+  for (int i = 0; i < 4; ++i) out[i] = L[0] == 0.f ? 0.f : y[0][i] * inv;
+  const int r = a.by_grp.div(qv);
+  store_out4(a, b, r, kvh * a.grp + qv - r * a.grp, HD, d, out);
 }
 
 template <bool E4, int HD>
 void launch_t(const PagedAttnArgs& a, hipStream_t st) {
   const int64_t items = (int64_t)a.splits * a.B * a.pg.hkv;
-  hipLaunchKernelGGL((paged_attn_kernel<E4, HD>), dim3((unsigned)(ceil_div(items, kXcds) * kXcds * a.qtiles)), dim3(kThreads), 0, st, a);
+  const dim3 grid((unsigned)(ceil_div(items, kXcds) * kXcds * a.qtiles));
+  if (a.wide)
+    hipLaunchKernelGGL((paged_attn_wide_kernel<E4, HD>), grid, dim3(kWideWaves * kWave), 0, st, a);
+  else if (a.qtiles == 1)
+    hipLaunchKernelGGL((paged_attn_kernel<E4, HD, true>), grid, dim3(kThreads), 0, st, a);
+  else
+    hipLaunchKernelGGL((paged_attn_kernel<E4, HD, false>), grid, dim3(kThreads), 0, st, a);
   if (a.splits > 1) {
     const int64_t vecs = (int64_t)a.B * a.pg.hkv * a.R * a.grp;
-    hipLaunchKernelGGL((paged_combine_kernel<HD>), dim3((unsigned)ceil_div(vecs * (HD / 4) * kJoin, kThreads)), dim3(kThreads), 0, st, a);
+    if (a.splits <= kSmallJoin)
+      hipLaunchKernelGGL((paged_combine_kernel<HD, true>), dim3((unsigned)ceil_div(vecs * (HD / 4), kThreads)), dim3(kThreads), 0, st, a);
+    else
+      hipLaunchKernelGGL((paged_combine_kernel<HD, false>), dim3((unsigned)ceil_div(vecs * (HD / 4) * kJoin, kThreads)), dim3(kThreads), 0, st, a);
   }
 }
 
@@ -427,20 +912,25 @@ void launch_t(const PagedAttnArgs& a, hipStream_t st) {
 
 // The cut of a call: chunks per sequence at most, and those that a sequence of max_len positions has.
 static void attn_splits(PagedAttnArgs* a) {
-  a->qtiles = (int)ceil_div((int64_t)a->R * a->grp, 16);
-  a->max_splits = std::max(1, kTargetItems / std::max(1, std::min(kTargetItems, a->pg.hkv * a->qtiles)));
-  a->splits = std::min(a->max_splits, (int)ceil_div(a->max_len, kMinChunk));
+  const int QV = a->R * a->grp;
+  const int64_t blocks = (int64_t)a->B * a->pg.hkv * ceil_div(QV, 32 * kWideWaves);
+  a->wide = QV > 16 && blocks >= kWideBlocks;
+  a->qtiles = (int)(a->wide ? ceil_div(QV, 32 * kWideWaves) : ceil_div(QV, 16));
+  a->qpad = (int)align_up(QV, 16);
+  const int target = a->wide ? kWideItems : kTargetItems;
+  a->max_splits = std::max(1, target / std::max(1, std::min(target, a->pg.hkv * a->qtiles)));
+  a->splits = std::min(a->max_splits, (int)ceil_div(a->max_len, a->wide ? kWideChunk : kMinChunk));
 }
 
 size_t paged_attn_workspace(PagedAttnArgs a, int hd) {
   attn_splits(&a);
   if (a.splits == 1) return 0;
-  return (size_t)a.B * a.pg.hkv * a.qtiles * a.splits * 16 * (hd + 2) * 4;
+  return (size_t)part_rows(a) * (hd + 2) * 4;
 }
 
 int launch_paged_attn(PagedAttnArgs a, int hd, bool e4, hipStream_t st) {
   attn_splits(&a);
-  a.by_grp = FastDiv(a.grp), a.by_hkv = FastDiv(a.pg.hkv), a.by_b = FastDiv(a.B), a.by_qtiles = FastDiv(a.qtiles);
+  a.by_grp = FastDiv(a.grp), a.by_hkv = FastDiv(a.pg.hkv), a.by_b = FastDiv(a.B), a.by_qtiles = FastDiv(a.qtiles), a.by_qv = FastDiv(a.R * a.grp);
   const int64_t blocks = (ceil_div((int64_t)a.splits * a.B * a.pg.hkv, kXcds) * kXcds) * a.qtiles;
   if (blocks >= (int64_t(1) << 31) || (int64_t)a.B * a.R * a.hq * hd / 4 * 4 / 256 >= (int64_t(1) << 31))
     return fail(SDD_EUNSUPPORTED, "%d x %d rows in one call", a.B, a.R);
@@ -504,7 +994,7 @@ extern "C" int sdd_paged_attention(const sdd_pages* pg, const int32_t* table, in
   a.q = q;
   a.out = out;
   a.err = err;
-  a.scale = scale * kLog2e;
+  a.set_scale(scale);
   a.part = reinterpret_cast<float*>(ws);
   return launch_paged_attn(a, pg->head_dim, pg->dtype == SDD_E4M3, reinterpret_cast<hipStream_t>(stream));
 }
