@@ -10,7 +10,15 @@
 // wave's first vectors: at least n tokens reach it.
 // Rows are cut into C chunks of whole 16-byte vectors (C from the row count and V alone); a row's last workgroup to
 // finish joins the chunks' records in chunk order, so results do not depend on the order of arrival.
+//
+// Bound: the arithmetic, close to the memory.  A bf16 logit costs 11 instructions of which the exponential counts
+// four times; 528 rows of 151936 (160 MB, 22.6 us at the copy's 7.1 TB/s) take 35 us without alternatives, 43 with one, 45
+// with 5, 55 with 20; one row of 152064 floats takes 5.1 and 9.7 with 20.  The time above that of no alternatives goes to
+// the sorts (a fixed cost of a workgroup) and to the tokens that pass: so few workgroups with long chunks, 2048 at
+// most.  528 rows, 20 alternatives: 55 us in 1584 workgroups, 62 in 3696, 93 in 8448.  With two vectors in flight instead of
+// four the same rows take 65 (the first threshold comes from half as many tokens); one row of 4096: 12 instead of 6.
 #include <algorithm>
+#include <type_traits>
 
 #include "sdd_internal.h"
 
@@ -93,6 +101,22 @@ __device__ inline uint64_t reversed(uint64_t v) {  // lane l gets lane 63 - l's
   return xor_lane64<32>(xor_lane64<16>((uint64_t)(uint32_t)dpp_i<kDppMirror>((int)(v >> 32)) << 32 | (uint32_t)dpp_i<kDppMirror>((int)v)));
 }
 
+// The same for 32-bit values.
+template <int J, int K>
+__device__ inline void sort_step32(uint32_t& v) {
+  const uint32_t o = (uint32_t)xor_lane<J>((int)v);
+  const int lane = threadIdx.x % kWave;
+  v = ((lane & J) == 0) == ((lane & K) == 0) ? max(v, o) : min(v, o);
+}
+__device__ inline void sort64_32(uint32_t& v) {
+  sort_step32<1, 2>(v);
+  sort_step32<2, 4>(v), sort_step32<1, 4>(v);
+  sort_step32<4, 8>(v), sort_step32<2, 8>(v), sort_step32<1, 8>(v);
+  sort_step32<8, 16>(v), sort_step32<4, 16>(v), sort_step32<2, 16>(v), sort_step32<1, 16>(v);
+  sort_step32<16, 32>(v), sort_step32<8, 32>(v), sort_step32<4, 32>(v), sort_step32<2, 32>(v), sort_step32<1, 32>(v);
+  sort_step32<32, 64>(v), sort_step32<16, 64>(v), sort_step32<8, 64>(v), sort_step32<4, 64>(v), sort_step32<2, 64>(v), sort_step32<1, 64>(v);
+}
+
 __device__ inline void wave_sync() {  // LDS accesses of one wave stay in program order
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
@@ -103,6 +127,7 @@ struct Best {
   uint64_t best, thr;  // thr: only keys above it count
   float thr_f;         // its logit
   int cnt;
+  bool held;      // best holds keys
   uint64_t* buf;  // LDS, 128 keys
 };
 __device__ inline void set_thr(Best& b, uint64_t thr) {
@@ -119,9 +144,14 @@ __device__ inline void flush(Best& b, int n) {
   wave_sync();
   b.cnt = max(0, b.cnt - kWave);
   sort64(v);
-  v = reversed(v);
-  b.best = v > b.best ? v : b.best;
-  merge64(b.best);
+  if (b.held) {
+    v = reversed(v);
+    b.best = v > b.best ? v : b.best;
+    merge64(b.best);
+  } else {
+    b.best = v;
+    b.held = true;
+  }
   const uint64_t t = lane_key(b.best, n - 1);
   if (t > b.thr) set_thr(b, t);
 }
@@ -159,18 +189,14 @@ __device__ inline Stats join_wave(Stats a) {
   return a;
 }
 
-// Wave 0 writes a row's results from its statistics and sorted keys.
-template <typename T>
-__device__ inline void write_row(const Job& j, int row, const T* z, const Stats& st, uint64_t best) {
+// Wave 0 writes a row's results from its statistics, its token's logit and its sorted keys.
+__device__ inline void write_row(const Job& j, int row, int token, float zt, const Stats& st, uint64_t best) {
   const int lane = threadIdx.x % kWave;
   // no distribution: a NaN or +inf among the logits, or none above -inf
   const bool bad = !(st.s > 0.f && st.s < INFINITY && st.m < INFINITY);
   const float nan = __builtin_nanf(""), ls = __logf(st.s);
   if (lane == 0) {
-    if (j.tokens) {
-      const int t = j.tokens[row];
-      j.logprob[row] = bad || (unsigned)t >= (unsigned)j.V ? nan : (Elem<T>::to_f32(z[t]) - st.m) - ls;
-    }
+    if (j.tokens) j.logprob[row] = bad || (unsigned)token >= (unsigned)j.V ? nan : (zt - st.m) - ls;
     if (j.entropy) j.entropy[row] = bad ? nan : fmaxf(ls - st.t / st.s, 0.f);
   }
   if (lane < j.n_top) {
@@ -180,56 +206,88 @@ __device__ inline void write_row(const Job& j, int row, const T* z, const Stats&
   }
 }
 
-template <typename T, bool TOP>
+// VEC elements from p, which need only be aligned as an element is (this GPU's global loads need no more).
+template <typename T, int VEC>
+__device__ inline uint4 load_any(const T* p) {
+  if constexpr (VEC == 1) {
+    return make_uint4(__builtin_bit_cast(uint32_t, Elem<T>::to_f32(*p)), 0, 0, 0);
+  } else {
+    typedef u32x4 any2 __attribute__((aligned(2)));
+    typedef u32x4 any4 __attribute__((aligned(4)));
+    const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const std::conditional_t<sizeof(T) == 2, any2, any4>*>(p));
+    return make_uint4(v.x, v.y, v.z, v.w);
+  }
+}
+
+template <typename T, bool TOP, int VEC>  // VEC: 16 bytes' elements, or 1 for rows of fewer
 __global__ void __launch_bounds__(kThreads) logprobs_kernel(Job j) {
-  constexpr int VEC = 16 / (int)sizeof(T);
   __shared__ uint64_t s_buf[TOP ? kWaves : 1][TOP ? 2 * kWave : 1];
+  __shared__ uint32_t s_first[TOP ? kWaves : 1][TOP ? kWave : 1];
   __shared__ Stats s_st[kWaves];
   __shared__ int s_flag;
+  touch_kernargs<Job>();
   const int row = blockIdx.x / j.C, c = blockIdx.x % j.C;
   const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
   const T* z = reinterpret_cast<const T*>(j.z) + (int64_t)(row / j.R) * j.seq_stride + (int64_t)(row % j.R) * j.V;
-  // vectors lie on 16-byte borders: the row's first and last may hold fewer of its elements
-  const int shift = (int)((uintptr_t)z % 16 / sizeof(T));
-  const int v_end = min((j.V + shift + VEC - 1) / VEC, (c + 1) * j.chunk);
+  int token = -1;
+  float zt = 0.f;
+  if (j.tokens) {
+    token = j.tokens[row];
+    zt = Elem<T>::to_f32(z[min(max(token, 0), j.V - 1)]);
+  }
+  const int v_end = min((j.V + VEC - 1) / VEC, (c + 1) * j.chunk);
   Stats st{-INFINITY, 0.f, 0.f};
   Best b;
   if constexpr (TOP) {
     b.best = 0;
     b.cnt = 0;
+    b.held = false;
     b.buf = s_buf[wave];
     set_thr(b, kFloor);
   }
-  bool first = true;
-  for (int v0 = c * j.chunk; v0 < v_end; v0 += kUnroll * kThreads) {
-    float x[kUnroll][VEC];
+  const int first = c * j.chunk;
+  auto step = [&](auto unroll, int v0) {
+    constexpr int U = decltype(unroll)::value;  // vectors of a thread
+    // (the row's last vector begins early enough to end with the row, threads past the chunk take it too: every load is in the
+    // row, none is conditional; what is not a thread's own is set to -inf)
+    uint4 raw[U];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int v = v0 + u * kThreads + (int)threadIdx.x, e0 = v * VEC - shift;
-      if (v < v_end && e0 >= 0 && e0 + VEC <= j.V) {
-        unpack16(load_nt16(z + e0), x[u], T());
-      } else {
+    for (int u = 0; u < U; ++u)
+      raw[u] = load_any<T, VEC>(z + min((v0 + u * kThreads + (int)threadIdx.x) * VEC, j.V - VEC));
+    float x[U][VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) x[u][e] = v < v_end && e0 + e >= 0 && e0 + e < j.V ? Elem<T>::to_f32(z[e0 + e]) : -INFINITY;
+    for (int u = 0; u < U; ++u) {
+      if constexpr (VEC == 1)
+        x[u][0] = __builtin_bit_cast(float, raw[u].x);
+      else
+        unpack16(raw[u], x[u], T());
+    }
+    const int v1 = v0 + U * kThreads;
+    if (v1 > v_end || (int64_t)v1 * VEC > j.V) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int v = v0 + u * kThreads + (int)threadIdx.x, own = v < v_end ? v * VEC - min(v * VEC, j.V - VEC) : VEC;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[u][e] = e >= own ? x[u][e] : -INFINITY;
       }
     }
-    float hi[kUnroll], top = -INFINITY;
+    float hi[U], top = -INFINITY;
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
+    for (int u = 0; u < U; ++u) {
       hi[u] = x[u][0];
 #pragma unroll
       for (int e = 1; e < VEC; ++e) hi[u] = fmaxf(hi[u], x[u][e]);
       top = fmaxf(top, hi[u]);
     }
-    if (top > st.m) {
-      const float d = st.m == -INFINITY ? 0.f : st.m - top, f = __expf(d);
+    if (__any(top > st.m)) {
+      const float mn = fmaxf(st.m, top), d = st.m == -INFINITY ? 0.f : st.m - mn, f = __expf(d);
       st.t = f * (st.t + st.s * fmaxf(d, -1e4f));
       st.s *= f;
-      st.m = top;
+      st.m = mn;
     }
     const float ref = st.m == -INFINITY ? 0.f : st.m;
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
+    for (int u = 0; u < U; ++u) {
       float s = 0.f, t = 0.f;
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
@@ -241,17 +299,20 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(Job j) {
       st.t += t;
     }
     if constexpr (TOP) {
-      if (first) {
-        first = false;
-        uint64_t v = (uint64_t)ordered(top) << 32;
-        sort64(v);
-        const uint64_t t = lane_key(v, j.n_top - 1);
+      if (v0 == first) {
+        s_first[wave][lane] = ordered(top);
+        __syncthreads();
+        uint32_t v = s_first[0][lane];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) v = max(v, s_first[w][lane]);
+        sort64_32(v);
+        const uint64_t t = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)v, j.n_top - 1) << 32;
         if (t > kFloor) set_thr(b, t - 1);  // (any index at that logit passes)
       }
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
+      for (int u = 0; u < U; ++u) {
         if (!__builtin_amdgcn_ballot_w64(hi[u] >= b.thr_f)) continue;
-        const int e0 = (v0 + u * kThreads + (int)threadIdx.x) * VEC - shift;
+        const int e0 = min((v0 + u * kThreads + (int)threadIdx.x) * VEC, j.V - VEC);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
           if (!__builtin_amdgcn_ballot_w64(x[u][e] >= b.thr_f)) continue;
@@ -260,7 +321,11 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(Job j) {
         }
       }
     }
-  }
+  };
+  // (one vector a thread or less at the end: not a step of four)
+  int v0 = first;
+  for (; v0 + kThreads < v_end; v0 += kUnroll * kThreads) step(std::integral_constant<int, kUnroll>(), v0);
+  if (v0 < v_end) step(std::integral_constant<int, 1>(), v0);
   if constexpr (TOP) {
     if (b.cnt > 0) flush(b, j.n_top);
     wave_sync();
@@ -282,7 +347,7 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(Job j) {
       }
     }
     if (j.C == 1) {
-      write_row<T>(j, row, z, st, best);
+      write_row(j, row, token, zt, st, best);
     } else {
       const int64_t at = (int64_t)row * j.C + c;
       if (lane == 0) {
@@ -296,30 +361,47 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(Job j) {
   }
   if (j.C == 1) return;
   if (!arrive_last(j.counters + row * kCntStride, j.C, &s_flag) || wave != 0) return;
-  // this row's chunks, lane l chunk l's statistics
+  // this row's chunks, lane l chunk l's statistics and first keys
   const int64_t r0 = (int64_t)row * j.C;
   Stats p{-INFINITY, 0.f, 0.f};
-  if (lane < j.C) p = Stats{ld_coherent(j.recs + 4 * (r0 + lane)), ld_coherent(j.recs + 4 * (r0 + lane) + 1), ld_coherent(j.recs + 4 * (r0 + lane) + 2)};
+  constexpr int kAhead = 4;  // keys of a chunk that are loaded at once
+  uint64_t head[kAhead] = {0, 0, 0, 0};
+  if (lane < j.C) {
+    p = Stats{ld_coherent(j.recs + 4 * (r0 + lane)), ld_coherent(j.recs + 4 * (r0 + lane) + 1), ld_coherent(j.recs + 4 * (r0 + lane) + 2)};
+    if constexpr (TOP)
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) head[i] = ld_coherent(j.keys + (r0 + lane) * j.n_top + min(i, j.n_top - 1));
+  }
   p = join_wave(p);
   if constexpr (TOP) {
     b.best = 0;
     b.cnt = 0;
+    b.held = false;
     set_thr(b, kFloor);
-    // n chunks or more: the n-th largest of their best keys is reached by n keys at least
-    uint64_t head = lane < j.C ? ld_coherent(j.keys + (r0 + lane) * j.n_top) : 0, v = head;
-    sort64(v);
-    const uint64_t t = lane_key(v, j.n_top - 1);
+    // n chunks or more: the n-th largest of their best logits is reached by n keys at least
+    uint32_t v = (uint32_t)(head[0] >> 32);
+    sort64_32(v);
+    const uint64_t t = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)v, j.n_top - 1) << 32;
     if (t > kFloor) set_thr(b, t - 1);
-    for (int i = 0; i < j.n_top; ++i) {
-      const bool pass = lane < j.C && head > b.thr && head > kFloor;
-      if (!__builtin_amdgcn_ballot_w64(pass)) break;  // (lists are sorted)
-      push(b, head, pass, j.n_top);
-      if (i + 1 < j.n_top && lane < j.C) head = ld_coherent(j.keys + (r0 + lane) * j.n_top + i + 1);
+    // (lists are sorted)
+    bool more = true;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (more && i < j.n_top) {
+        const bool pass = lane < j.C && head[i] > b.thr && head[i] > kFloor;
+        more = __builtin_amdgcn_ballot_w64(pass) != 0;
+        push(b, head[i], pass, j.n_top);
+      }
+    for (int i = kAhead; more && i < j.n_top; ++i) {
+      const uint64_t k = lane < j.C ? ld_coherent(j.keys + (r0 + lane) * j.n_top + i) : 0;
+      const bool pass = k > b.thr && k > kFloor;
+      more = __builtin_amdgcn_ballot_w64(pass) != 0;
+      push(b, k, pass, j.n_top);
     }
     if (b.cnt > 0) flush(b, j.n_top);
     best = b.best;
   }
-  write_row<T>(j, row, z, p, best);
+  write_row(j, row, token, zt, p, best);
 }
 
 // Chunks of a row: as many as fill the device once, none under 4 vectors a thread, at most a wave's lanes.
@@ -335,16 +417,19 @@ size_t workspace(int64_t rows, int n_top) {
 
 template <typename T>
 int launch(Job j, int64_t rows, hipStream_t st) {
-  const int64_t vectors = ceil_div((int64_t)j.V + 16 / sizeof(T) - 1, 16 / sizeof(T));  // of a row at any alignment
+  constexpr int VEC = 16 / (int)sizeof(T);
+  const int64_t vectors = j.V < VEC ? j.V : ceil_div((int64_t)j.V, VEC);
   j.C = chunks_for(rows, vectors);
   j.chunk = (int)ceil_div(vectors, j.C);
   j.C = (int)ceil_div(vectors, j.chunk);
   const dim3 grid((unsigned)(rows * j.C));
   prof_begin(PROF_LOGP, st);
-  if (j.n_top > 0)
-    hipLaunchKernelGGL((logprobs_kernel<T, true>), grid, dim3(kThreads), 0, st, j);
+  if (j.V < VEC)
+    hipLaunchKernelGGL((logprobs_kernel<T, true, 1>), grid, dim3(kThreads), 0, st, j);
+  else if (j.n_top > 0)
+    hipLaunchKernelGGL((logprobs_kernel<T, true, VEC>), grid, dim3(kThreads), 0, st, j);
   else
-    hipLaunchKernelGGL((logprobs_kernel<T, false>), grid, dim3(kThreads), 0, st, j);
+    hipLaunchKernelGGL((logprobs_kernel<T, false, VEC>), grid, dim3(kThreads), 0, st, j);
   prof_end(PROF_LOGP, st);
   return check_launch("logprobs_kernel");
 }
