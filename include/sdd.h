@@ -313,9 +313,10 @@ int sdd_paged_append(const sdd_pages* pg, const int32_t* table, int table_width,
                      const float* k_gain, float eps, const float* rope, int max_pos, uint16_t* q_out, int32_t* err,
                      sdd_stream_t stream);
 
-/* Workspace of sdd_paged_attention for calls of at most max_len positions a
- * sequence (0: none is needed).  It needs no initialization and carries nothing
- * from one call to the next. */
+/* Workspace of sdd_paged_attention for calls of at most B sequences, R rows and
+ * max_len positions a sequence (0: none is needed).  It needs no initialization
+ * and carries nothing from one call to the next; calls that may run at the same
+ * time need one each. */
 int sdd_paged_attention_workspace_bytes(const sdd_pages* pg, int B, int R, int n_q_heads, int max_len, size_t* bytes);
 
 /* Causal attention of R rows (their own K/V appended before) of each of B
@@ -327,10 +328,10 @@ int sdd_paged_attention_workspace_bytes(const sdd_pages* pg, int B, int R, int n
  * host's bound sizes the launch, so that a captured call serves all lengths up
  * to it.  A row that sees nothing (its pages are invalid) gives zeros.  Sums and
  * softmax statistics are fp32 and in a fixed order: results are
- * bit-reproducible, and a sequence's do not depend on the other sequences of
- * the call, with one line between two orders of the sums: B * n_kv_heads *
- * ceil(R * n_q_heads / n_kv_heads / 128) of 160 and more (they do depend on R,
- * whose rows share work).  Errors: SDD_EINVAL, SDD_ENOMEM (small workspace),
+ * bit-reproducible and do not depend on what the call's other sequences hold;
+ * below a B * n_kv_heads * ceil(R * n_q_heads / n_kv_heads / 128) of 160 not on B
+ * either (from there B decides into how many parts a sequence's sums are cut;
+ * R, whose rows share work, always counts).  Errors: SDD_EINVAL, SDD_ENOMEM (small workspace),
  * SDD_EUNSUPPORTED. */
 int sdd_paged_attention(const sdd_pages* pg, const int32_t* table, int table_width, const int32_t* len, int B, int R,
                         int n_q_heads, const uint16_t* q, float scale, int max_len, uint16_t* out, int32_t* err,

@@ -1323,25 +1323,15 @@ static PagedWs paged_ws(const sdd_kv* kv, int nb, int R, size_t part_bytes) {
   p.total = align_up(p.part + part_bytes, 256);
   return p;
 }
-// Partial results of nb blocks of R rows; of nb blocks of up to R rows (fewer rows may be cut into more chunks).
+// Partial results of nb blocks of up to R rows.
 static size_t paged_part(const sdd_kv* kv, int nb, int R) {
   return paged_attn_workspace(paged_attn_shape(kv, nb, R), kv->m->cfg.head_dim);
 }
-static size_t paged_part_upto(const sdd_kv* kv, int nb, int R) {
-  size_t most = 0;
-  for (int r = 1; r <= R; ++r) {
-    const size_t n = paged_part(kv, nb, r);
-    if (n == 0) break;  // blocks of this many rows are not cut, nor are larger ones
-    most = std::max(most, n);
-  }
-  return most;
-}
-// What a call of nb blocks of R rows needs, and a prefill whose chunks are of at most R rows; 0 for a contiguous cache.
+// What a call of nb blocks of up to R rows needs; 0 for a contiguous cache.
 static size_t paged_bytes(const sdd_kv* kv, int nb, int R) { return kv->page_size ? paged_ws(kv, nb, R, paged_part(kv, nb, R)).total : 0; }
-static size_t paged_chunk_bytes(const sdd_kv* kv, int R) { return kv->page_size ? paged_ws(kv, 1, R, paged_part_upto(kv, 1, R)).total : 0; }
 // What a prefill's chunks of at most R rows leave of a workspace for their layout: a paged cache's part sits at its end.
 static size_t prefill_room(const sdd_kv* kv, int R, size_t bytes) {
-  const size_t p = paged_chunk_bytes(kv, R);
+  const size_t p = paged_bytes(kv, 1, R);
   return p == 0 ? bytes : p < bytes ? (bytes - p) / 256 * 256 : 0;
 }
 static sdd_pages kv_pages(const sdd_kv* kv, int layer) {
@@ -1876,7 +1866,7 @@ extern "C" int sdd_kv_workspace_bytes(const sdd_kv* kv, int max_rows, size_t* by
   size_t paged = 0;
   if (kv->page_size) {
     size_t part = 0;  // the largest partial results of any nb blocks of R rows, nb R <= max_rows
-    for (int nb = 1; nb <= std::min(kv->max_batch, max_rows); ++nb) part = std::max(part, paged_part_upto(kv, nb, max_rows / nb));
+    for (int nb = 1; nb <= std::min(kv->max_batch, max_rows); ++nb) part = std::max(part, paged_part(kv, nb, max_rows / nb));
     paged = paged_ws(kv, 1, max_rows, part).total + 256;
   }
   *bytes = ws_layout(kv->m, max_rows).total + paged;

@@ -31,10 +31,12 @@ constexpr int kTargetItems = 512;
 // other, both with the join: eight sequences of 284-3761 positions, 33 rows (192 workgroups) 57 / 76 us; one sequence, 1024
 // rows behind 1024 positions (512) 73 / 127; 256 rows (128) 39 / 28, and behind 8000 positions 114 / 153; 33 rows (24) 18 / 14.
 // Chunks of 256, 512, 768, 1024 with the first of these: 63, 57.5, 57, 61 us (longer ones leave compute units idle, shorter
-// ones write more partial results).
+// ones write more partial results).  A call has kWideItems workgroups at most: with many sequences partial results would cost
+// more than they give (64 sequences, 33 rows: 279 us, and 366 where a sequence's chunks did not depend on the batch), with one
+// sequence 512 fill the device (kWideFew; 1024 workgroups of 1024 rows behind 1024 positions: 102 instead of 69 us).
 constexpr int kWideWaves = 4;
 constexpr int kWideBlocks = 160;
-constexpr int kWideChunk = 512, kWideItems = 256;
+constexpr int kWideChunk = 512, kWideItems = 2048, kWideFew = 4;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
@@ -917,15 +919,23 @@ static void attn_splits(PagedAttnArgs* a) {
   a->wide = QV > 16 && blocks >= kWideBlocks;
   a->qtiles = (int)(a->wide ? ceil_div(QV, 32 * kWideWaves) : ceil_div(QV, 16));
   a->qpad = (int)align_up(QV, 16);
-  const int target = a->wide ? kWideItems : kTargetItems;
-  a->max_splits = std::max(1, target / std::max(1, std::min(target, a->pg.hkv * a->qtiles)));
+  const int64_t items = a->wide ? kWideItems / std::max(a->B, kWideFew) : kTargetItems;
+  a->max_splits = (int)std::max<int64_t>(1, items / ((int64_t)a->pg.hkv * a->qtiles));
   a->splits = std::min(a->max_splits, (int)ceil_div(a->max_len, a->wide ? kWideChunk : kMinChunk));
 }
 
+// Enough for a call of a->B sequences, a->R rows and a->max_len positions and for each with fewer of any of them, whichever
+// kernel takes it and however it is cut: where there is more than one chunk, kTargetItems workgroups of 16 vectors a sequence,
+// or kWideItems of 128 a call, are not passed, and no more chunks than kSizeStep positions each.
 size_t paged_attn_workspace(PagedAttnArgs a, int hd) {
+  constexpr int kSizeStep = 128;
+  static_assert(kSizeStep <= kMinChunk && kSizeStep <= kWideChunk, "");
+  if (a.max_len <= kSizeStep) return 0;
   attn_splits(&a);
-  if (a.splits == 1) return 0;
-  return (size_t)part_rows(a) * (hd + 2) * 4;
+  const int64_t most = (int64_t)a.B * a.pg.hkv * ceil_div(a.max_len, kSizeStep) * a.qpad;
+  int64_t rows = std::min(most, (int64_t)a.B * kTargetItems * 16);
+  if (a.wide) rows = std::max(rows, std::min(most, (int64_t)kWideItems * 32 * kWideWaves));
+  return (size_t)rows * (hd + 2) * 4;
 }
 
 int launch_paged_attn(PagedAttnArgs a, int hd, bool e4, hipStream_t st) {
