@@ -7,6 +7,7 @@ missing or no gfx950 GPU is present, calls raise.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 
 import torch
@@ -122,9 +123,24 @@ def _ptr(t):
     return None if t is None else C.c_void_p(t.data_ptr())
 
 
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
 def _stream(stream=None):
     s = stream if stream is not None else torch.cuda.current_stream()
     return C.c_void_p(s.cuda_stream)
+
+
+def _here(stream, *tensors):
+    """Raw handle of the stream to launch on; the tensors (None: absent) must be on the current device, whose kernels read
+    them."""
+    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else 0
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"tensors must be on the current device cuda:{dev}, got one on {t.device}")
+    # (the handle alone: torch.cuda.current_stream makes a Stream object, 2.7 us of a call's 14)
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 def _need(cond: bool, msg: str):
@@ -241,24 +257,30 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, n_t
 
     Returns (logprob, entropy) fp32 [B, R] (logprob None without tokens) and, with n_top, (top int32, top_logprob
     fp32) [B, R, n_top] as well; `out` gives the tensors to write into, in that order."""
-    B, R, V = logits.shape
     _rows(logits, "logits")
-    _i32(tokens, "tokens", allow_none=True)
-    _need(tokens is None or tokens.numel() == B * R, "tokens must be [B, R]")
+    B, R, V = logits.shape
+    n = B * R
+    if tokens is not None:
+        _i32(tokens, "tokens")
+        _need(tokens.numel() == n, "tokens must be [B, R]")
     if ws is None:
-        ws = logprobs_workspace(B * R, V, n_top, logits.device)
+        ws = logprobs_workspace(n, V, n_top, logits.device)
     if out is None:
-        new = lambda *shape, dtype=torch.float32: torch.empty(*shape, dtype=dtype, device=logits.device)
-        out = (new(B, R) if tokens is not None else None, new(B, R))
+        dev, f32 = logits.device, torch.float32
+        out = (None if tokens is None else torch.empty((B, R), dtype=f32, device=dev), torch.empty((B, R), dtype=f32, device=dev))
         if n_top:
-            out += (new(B, R, n_top, dtype=torch.int32), new(B, R, n_top))
-    lp, ent, top, top_lp = tuple(out) + (None,) * (4 - len(out))
-    for t, nm, n in ((lp, "logprob", B * R), (ent, "entropy", B * R), (top_lp, "top_logprob", B * R * n_top)):
-        _need(t is None or (t.dtype == torch.float32 and t.is_contiguous() and t.numel() == n), f"{nm} must be contiguous fp32, {n} values")
-    _i32(top, "top", allow_none=n_top == 0)
-    _need(top is None or top.numel() == B * R * n_top, "top must be [B, R, n_top]")
-    _check(lib().sdd_token_logprobs(_ptr(logits), _dtype_code(logits), logits.stride(0), B, R, V, _ptr(tokens), n_top,
-                                    _ptr(lp), _ptr(ent), _ptr(top), _ptr(top_lp), _ptr(ws), ws.numel(), _stream(stream)))
+            out += (torch.empty((B, R, n_top), dtype=torch.int32, device=dev), torch.empty((B, R, n_top), dtype=f32, device=dev))
+        lp, ent, top, top_lp = out if n_top else out + (None, None)
+    else:
+        lp, ent, top, top_lp = tuple(out) + (None,) * (4 - len(out))
+        for t, nm, k in ((lp, "logprob", n), (ent, "entropy", n), (top_lp, "top_logprob", n * n_top)):
+            _need(t is None or (t.dtype == torch.float32 and t.is_contiguous() and t.numel() == k), f"{nm} must be contiguous fp32, {k} values")
+        _i32(top, "top", allow_none=n_top == 0)
+        _need(top is None or top.numel() == n * n_top, "top must be [B, R, n_top]")
+    _need(ws.is_contiguous(), "ws must be contiguous")
+    st = _here(stream, logits, tokens, lp, ent, top, top_lp, ws)
+    _check(lib().sdd_token_logprobs(_addr(logits), _dtype_code(logits), logits.stride(0), B, R, V, _addr(tokens), n_top,
+                                    _addr(lp), _addr(ent), _addr(top), _addr(top_lp), _addr(ws), ws.nbytes, st))
     return out
 
 
@@ -368,6 +390,7 @@ class PagePool:
         _need(buf.is_contiguous() and buf.numel() * buf.element_size() >= n, f"buf must be contiguous and hold {n} bytes")
         self.buf = buf
         self.desc.pages = buf.data_ptr()
+        self._desc = C.byref(self.desc)
 
     def _seqs(self, table, lens, rows):
         _i32(table, "table")
@@ -377,23 +400,29 @@ class PagePool:
     def append(self, qkv: torch.Tensor, n_q_heads: int, table: torch.Tensor, lens: torch.Tensor, *, q_norm=None, k_norm=None,
                eps: float = 1e-6, rope: torch.Tensor | None = None, q_out=None, err=None, stream=None) -> torch.Tensor:
         """sdd_paged_append of qkv [B, R, (n_q_heads + 2 n_kv_heads) * head_dim]; returns q bf16 [B, R, n_q_heads, head_dim]."""
+        _need(qkv.dim() == 3, "qkv must be [B, R, (n_q_heads + 2 n_kv_heads) * head_dim]")
         B, R, n = qkv.shape
+        hd = self.head_dim
         self._seqs(table, lens, B)
-        _need(n == (n_q_heads + 2 * self.n_kv_heads) * self.head_dim, "qkv must be [B, R, (n_q_heads + 2 n_kv_heads) * head_dim]")
-        _need(qkv.stride(2) == 1 and (B == 1 or R == 1 or qkv.stride(0) == R * qkv.stride(1)), "qkv rows must be evenly spaced")
+        s0, s1, s2 = qkv.stride()
+        _need(n == (n_q_heads + 2 * self.n_kv_heads) * hd, "qkv must be [B, R, (n_q_heads + 2 n_kv_heads) * head_dim]")
+        _need(s2 == 1 and (B == 1 or R == 1 or s0 == R * s1), "qkv rows must be evenly spaced")
         for t, nm in ((q_norm, "q_norm"), (k_norm, "k_norm")):
-            _need(t is None or (t.dtype == torch.float32 and t.is_contiguous() and t.numel() == self.head_dim), f"{nm} must be fp32 [head_dim]")
-        _need(rope is None or (rope.dtype == torch.float32 and rope.is_contiguous() and rope.shape[1:] == (self.head_dim // 2, 2)),
-              "rope must be contiguous fp32 [max_pos, head_dim / 2, 2]")
+            if t is not None and not (t.dtype == torch.float32 and t.is_contiguous() and t.numel() == hd):
+                raise ValueError(f"{nm} must be fp32 [head_dim]")
+        if rope is not None:
+            _need(rope.dtype == torch.float32 and rope.is_contiguous() and rope.dim() == 3 and rope.shape[1:] == (hd // 2, 2),
+                  "rope must be contiguous fp32 [max_pos, head_dim / 2, 2]")
         _i32(err, "err", allow_none=True)
         if q_out is None:
-            q_out = torch.empty((B, R, n_q_heads, self.head_dim), dtype=torch.bfloat16, device=qkv.device)
-        _need(q_out.dtype == torch.bfloat16 and q_out.is_contiguous() and q_out.numel() == B * R * n_q_heads * self.head_dim,
-              "q_out must be contiguous bf16 [B, R, n_q_heads, head_dim]")
-        _check(lib().sdd_paged_append(C.byref(self.desc), _ptr(table), table.shape[1], _ptr(lens), B, R, n_q_heads, _ptr(qkv),
-                                      _dtype_code(qkv), qkv.stride(1) if R > 1 else qkv.stride(0) if B > 1 else n,
-                                      _ptr(q_norm), _ptr(k_norm), eps, _ptr(rope), 0 if rope is None else rope.shape[0],
-                                      _ptr(q_out), _ptr(err), _stream(stream)))
+            q_out = torch.empty((B, R, n_q_heads, hd), dtype=torch.bfloat16, device=qkv.device)
+        else:
+            _need(q_out.dtype == torch.bfloat16 and q_out.is_contiguous() and q_out.numel() == B * R * n_q_heads * hd,
+                  "q_out must be contiguous bf16 [B, R, n_q_heads, head_dim]")
+        st = _here(stream, self.buf, table, lens, qkv, q_norm, k_norm, rope, q_out, err)
+        _check(lib().sdd_paged_append(self._desc, _addr(table), table.shape[1], _addr(lens), B, R, n_q_heads, _addr(qkv),
+                                      _dtype_code(qkv), s1 if R > 1 else s0 if B > 1 else n, _addr(q_norm), _addr(k_norm), eps,
+                                      _addr(rope), 0 if rope is None else rope.shape[0], _addr(q_out), _addr(err), st))
         return q_out
 
     def attention_workspace(self, B: int, R: int, n_q_heads: int, max_len: int) -> torch.Tensor:
@@ -404,35 +433,42 @@ class PagePool:
                   scale: float | None = None, out=None, ws=None, err=None, stream=None) -> torch.Tensor:
         """sdd_paged_attention of q bf16 [B, R, n_q_heads, head_dim] (rows at lens .. lens + R - 1, appended before); same
         shape returned.  max_len bounds lens + R (default: what the table can hold); scale defaults to head_dim^-1/2."""
+        _need(q.dim() == 4 and q.dtype == torch.bfloat16 and q.is_contiguous() and q.shape[3] == self.head_dim,
+              "q must be contiguous bf16 [B, R, n_q_heads, head_dim]")
         B, R, H, hd = q.shape
         self._seqs(table, lens, B)
-        _need(q.dtype == torch.bfloat16 and q.is_contiguous() and hd == self.head_dim, "q must be contiguous bf16 [B, R, n_q_heads, head_dim]")
         max_len = max_len or table.shape[1] * self.page_size
         if ws is None:
             ws = self.attention_workspace(B, R, H, max_len)
         if out is None:
             out = torch.empty_like(q)
-        _need(out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == q.numel(), "out must be contiguous bf16 like q")
+        else:
+            _need(out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == q.numel(), "out must be contiguous bf16 like q")
+        _need(ws.is_contiguous(), "ws must be contiguous")
         _i32(err, "err", allow_none=True)
-        _check(lib().sdd_paged_attention(C.byref(self.desc), _ptr(table), table.shape[1], _ptr(lens), B, R, H, _ptr(q),
-                                         hd ** -0.5 if scale is None else scale, max_len, _ptr(out), _ptr(err), _ptr(ws),
-                                         ws.numel(), _stream(stream)))
+        st = _here(stream, self.buf, table, lens, q, out, err, ws)
+        _check(lib().sdd_paged_attention(self._desc, _addr(table), table.shape[1], _addr(lens), B, R, H, _addr(q),
+                                         hd ** -0.5 if scale is None else scale, max_len, _addr(out), _addr(err), _addr(ws),
+                                         ws.nbytes, st))
         return out
 
     def read(self, table: torch.Tensor, start: torch.Tensor, n: int, *, out=None, err=None, stream=None):
         """sdd_paged_read of positions start .. start + n - 1: (k, v) bf16 [B, n, n_kv_heads, head_dim]."""
         B = start.numel()
         self._seqs(table, start, B)
+        shape = (B, n, self.n_kv_heads, self.head_dim)
         if out is None:
-            shape = (B, n, self.n_kv_heads, self.head_dim)
-            out = tuple(torch.empty(shape, dtype=torch.bfloat16, device=self.buf.device) for _ in range(2))
-        for t in out:
-            _need(t.dtype == torch.bfloat16 and t.is_contiguous() and t.numel() == B * n * self.n_kv_heads * self.head_dim,
-                  "k and v must be contiguous bf16 [B, n, n_kv_heads, head_dim]")
+            k = torch.empty(shape, dtype=torch.bfloat16, device=self.buf.device)
+            v = torch.empty_like(k)
+        else:
+            k, v = out
+            for t in (k, v):
+                _need(t.dtype == torch.bfloat16 and t.is_contiguous() and t.numel() == math.prod(shape),
+                      "k and v must be contiguous bf16 [B, n, n_kv_heads, head_dim]")
         _i32(err, "err", allow_none=True)
-        _check(lib().sdd_paged_read(C.byref(self.desc), _ptr(table), table.shape[1], _ptr(start), B, n, _ptr(out[0]),
-                                    _ptr(out[1]), _ptr(err), _stream(stream)))
-        return tuple(out)
+        st = _here(stream, self.buf, table, start, k, v, err)
+        _check(lib().sdd_paged_read(self._desc, _addr(table), table.shape[1], _addr(start), B, n, _addr(k), _addr(v), _addr(err), st))
+        return k, v
 
 
 # ---- decoder ------------------------------------------------------------------------------
