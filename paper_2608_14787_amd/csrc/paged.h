@@ -108,7 +108,7 @@ struct PagedAttnArgs {
     q_xor = x < 0.f ? 0x80008000u : 0u;
   }
   int32_t* err;
-  int qtiles, splits, max_splits, qpad;
+  int qtiles, splits, max_splits, whole, qpad;
   int wide;  // the kernel for many query vectors
   FastDiv by_grp, by_hkv, by_b, by_qtiles, by_qv;  // (set by the launch)
   float* part;  // partial results

@@ -25,6 +25,11 @@ constexpr int kWaves = 4, kThreads = kWaves * kWave;
 // of at least 128, 256 and 512 (attention alone): 32 ragged decode sequences 64, 53, 52 us; one of 513 positions 5.1, 5.5, 6.4.
 constexpr int kMinChunk = 256;
 constexpr int kTargetItems = 512;
+// A short sequence is one chunk, so that its parts need no second kernel to join them: up to kWhole positions, or kWholeMany
+// where its heads and rows are kManyItems workgroups as it is.  Measured, 64/8 heads, bf16, one chunk against several and
+// the join: one row, 300 positions 5.8 / 8.1 us, 700 7.5 / 8.2, 1000 8.6 / 8.3, 1300 12.0 / 8.6; 33 rows (136 workgroups), 1300
+// 11.6 / 14.6, 1600 12.8 / 15.5, and from e4m3 pages 15.0 / 15.1, 2000 17.3 / 16.2.
+constexpr int kWhole = 768, kWholeMany = 1536, kManyItems = 64;
 
 // The many-vector kernel: a workgroup's waves, a tile of 32 query vectors each; the number of such workgroups (before the cut
 // into chunks) from which a call takes it; its chunks and items.  Measured, 64/8 heads of 128, bf16, this kernel against the
@@ -45,9 +50,11 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // steps: rescaled at each rise, a third of the step's vector instructions were the accumulators'.
 constexpr float kFar = 8.f;
 
-__host__ __device__ inline int chunk_of(int total, int max_splits, int wide) {
-  const int c = (total + max_splits - 1) / max_splits;
-  return max(wide ? kWideChunk : kMinChunk, (c + 127) / 128 * 128);
+// Positions of a chunk of a sequence of total positions; a.whole of them and fewer are not cut.
+__host__ __device__ inline int chunk_of(const PagedAttnArgs& a, int total) {
+  if (total <= a.whole) return a.whole;
+  const int c = (total + a.max_splits - 1) / a.max_splits;
+  return max(a.wide ? kWideChunk : kMinChunk, (c + 127) / 128 * 128);
 }
 
 struct Seq {
@@ -120,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const Seq sq = attn_seq(a, b, threadIdx.x == 0 && c == 0 && kvh == 0 && qt == 0);
   if (sq.pos < 0) return;
-  const int total = sq.pos + a.R, chunk = chunk_of(total, a.max_splits, a.wide), n_chunks = (total + chunk - 1) / chunk;
+  const int total = sq.pos + a.R, chunk = chunk_of(a, total), n_chunks = (total + chunk - 1) / chunk;
   if (c >= n_chunks) return;
   const int QV = a.R * a.grp, qv = qt * 16 + lane % 16;
   const bool qok = qv < QV;
@@ -541,7 +548,7 @@ __global__ void __launch_bounds__(kWideWaves * kWave, E4 ? 2 : 3) paged_attn_wid
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, half = lane / 32;
   const Seq sq = attn_seq(a, b, threadIdx.x == 0 && c == 0 && kvh == 0 && qb == 0);
   if (sq.pos < 0) return;
-  const int total = sq.pos + a.R, chunk = chunk_of(total, a.max_splits, a.wide), n_chunks = (total + chunk - 1) / chunk;
+  const int total = sq.pos + a.R, chunk = chunk_of(a, total), n_chunks = (total + chunk - 1) / chunk;
   if (c >= n_chunks) return;
   const int QV = a.R * a.grp, q_block = qb * NW * 32, q0 = q_block + wave * 32, qv = q0 + lane % 32;
   const int block_end = __builtin_amdgcn_readfirstlane(sq.pos + min(a.R - 1, a.by_grp.div(q_block + NW * 32 - 1)) + 1);
@@ -810,7 +817,7 @@ __global__ void __launch_bounds__(kThreads) paged_combine_kernel(PagedAttnArgs a
     int p = a.rows ? a.rows[(int64_t)b * a.R].pos : a.len[b];
     const bool ok = (!a.rows || a.rows[(int64_t)b * a.R].valid) && p >= 0 && (int64_t)p + a.R <= a.max_len;
     const int total = p + a.R;
-    if (ok) n = (total + chunk_of(total, a.max_splits, a.wide) - 1) / chunk_of(total, a.max_splits, a.wide);
+    if (ok) n = (total + chunk_of(a, total) - 1) / chunk_of(a, total);
   }
   const int64_t at = part_row(a, bh, 0, qv), stride = a.qpad;  // (of a chunk)
   const float* o = a.part + at * HD + d;
@@ -921,7 +928,8 @@ static void attn_splits(PagedAttnArgs* a) {
   a->qpad = (int)align_up(QV, 16);
   const int64_t items = a->wide ? kWideItems / std::max(a->B, kWideFew) : kTargetItems;
   a->max_splits = (int)std::max<int64_t>(1, items / ((int64_t)a->pg.hkv * a->qtiles));
-  a->splits = std::min(a->max_splits, (int)ceil_div(a->max_len, a->wide ? kWideChunk : kMinChunk));
+  a->whole = a->wide ? kWideChunk : a->pg.hkv * a->qtiles >= kManyItems ? kWholeMany : kWhole;
+  a->splits = a->max_len <= a->whole ? 1 : std::min(a->max_splits, (int)ceil_div(a->max_len, a->wide ? kWideChunk : kMinChunk));
 }
 
 // Enough for a call of a->B sequences, a->R rows and a->max_len positions and for each with fewer of any of them, whichever

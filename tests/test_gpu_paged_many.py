@@ -190,3 +190,46 @@ def test_a_workspace_serves_smaller_calls(S):  # noqa: F811
                 for m in (1, 129, 257, 513, n // 2, n):
                     if b <= B and r <= R:
                         assert size(b, r, m) <= most, (B, R, n, b, r, m)
+
+
+# ---- few rows, sequences that are cut --------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("R", [1, 33])
+def test_peaks_in_different_parts(S, dtype, R):  # noqa: F811
+    hq, hkv, hd, at = 8, 2, 64, [2500, 767, 768, 1600]
+    c, k, v = fill(S, dtype, hkv, hd, 32, R, at, spread=8.0)
+    q = (20 * randn(5, 4, R, hq, hd)).to(torch.bfloat16)
+    for scale in (1.0, 0.0, -0.5):
+        check_attention(S, c, k, v, q, at, scale=scale)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("hq, hkv, R", [(16, 2, 1), (64, 8, 33)])
+def test_lengths_around_the_cut(S, dtype, hq, hkv, R):  # noqa: F811
+    at = [n - R for n in (255, 256, 257, 767, 768, 769, 1535, 1536, 1537, 2049)]
+    for b in range(0, 10, 5):  # (five at a time: few workgroups)
+        c, k, v = fill(S, dtype, hkv, 128, 64, R, at[b:b + 5])
+        q = (2 * randn(9, 5, R, hq, 128)).to(torch.bfloat16)
+        check_attention(S, c, k, v, q, at[b:b + 5])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("where", ["k", "v"])
+def test_nan_in_one_part(S, dtype, where):  # noqa: F811
+    """A NaN in a part that every row sees reaches all rows of its head, one on the diagonal those behind it."""
+    hq, hkv, hd, R, at = 8, 2, 64, 3, 1500
+    for spoilt, first in ((100, 0), (at + 1, 1)):
+        c = Cache(S, dtype, hkv, hd, 32, [at + R])
+        k, v = randn(1, 1, at + R, hkv, hd), randn(2, 1, at + R, hkv, hd)
+        (k if where == "k" else v)[0, spoilt, 1, 5] = math.nan
+        k, v = c.put(k, v, [0])
+        q = randn(3, 1, R, hq, hd).to(torch.bfloat16)
+        got = c.pool.attention(q.cuda(), c.table, i32([at]))[0].cpu().double()
+        want, tol = ref.attention(q[0].double(), k[0], v[0], at, hd ** -0.5)
+        clean = torch.ones(R, hq, dtype=torch.bool)
+        clean[first:, 4:] = False
+        assert ((got - want).abs() <= tol)[clean].all()
+        dims = slice(5, 6) if where == "v" and dtype == "bf16" else slice(None)
+        assert torch.isnan(got[first:, 4:, dims]).all()
