@@ -86,6 +86,7 @@ struct AppendArgs {
   int n_qk;       // workgroups of the q/k part
   int per_wave;   // head sets that a wave takes one after the other
   int v_groups;   // 8-position groups that R rows can touch
+  FastDiv by_waves, by_r, by_hkv, by_groups;  // (set by the launch; by_waves: waves of a row)
 };
 
 int launch_paged_append(AppendArgs a, int head_dim, bool e4, bool f32, hipStream_t st);

@@ -3,7 +3,9 @@
 //
 // Both are streams: a row's (n_q + 2 n_kv) heads are read once, q is written once and K/V once in the cache's type; the
 // rotation's cosines and sines are read from a table (angles in 64 bits when it is made: in 32 bits, position 10^5 would be
-// off by 4e-3 rad at the first frequency).
+// off by 4e-3 rad at the first frequency).  Bound: the memory.  64/8 heads of 128: 4095 rows appended (168 MB, norms and
+// rotation) 38 us, 4.4 TB/s where a copy of torch's runs at 4.9; eight prefixes of 4001 positions read from e4m3 pages (197 MB)
+// 36 us, 5.5 TB/s, from bf16 (262 MB) 50; one row appended 4.4 us, read 3.2.
 #include <algorithm>
 #include <cmath>
 
@@ -79,6 +81,12 @@ __device__ inline void load8(const char* base, int64_t i, float* y) {
   }
 }
 
+// 16 bytes that are read once
+__device__ inline uint4 load_nt(const void* p) {
+  const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+
 // Four values already within +-448 to their nearest e4m3 codes (ties to even), value i in byte i.
 __device__ inline uint32_t pack_e4m3x4(float a, float b, float c, float d) {
   int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
@@ -118,11 +126,24 @@ __global__ void __launch_bounds__(256) append_kernel(AppendArgs a) {
   const int H = a.hq + a.pg.hkv;
   if ((int)blockIdx.x < a.n_qk) {
     constexpr int LN = HD / 16, HS = kWave / LN;  // heads of a set: one wave's
-    const int sets = (H + HS - 1) / HS, waves = (sets + a.per_wave - 1) / a.per_wave;
-    const int64_t item = (int64_t)blockIdx.x * 4 + wave;
-    const int64_t m = item / waves;
-    if (m >= (int64_t)a.B * a.R) return;
-    const int b = (int)(m / a.R), r = (int)(m % a.R), s0 = (int)(item % waves) * a.per_wave;
+    const int sets = (H + HS - 1) / HS;
+    const int item = __builtin_amdgcn_readfirstlane((int)blockIdx.x * 4 + wave);
+    const int row = a.by_waves.div(item);
+    if (row >= a.B * a.R) return;
+    const int64_t m = row;
+    const int b = a.by_r.div(row), r = row - b * a.R, s0 = (item - row * (int)a.by_waves.d) * a.per_wave, s1 = min(sets, s0 + a.per_wave);
+    // (raw elements of the set after the one at work, so that its loads run meanwhile)
+    constexpr int NV = sizeof(T) / 2;
+    uint4 raw[2][NV];
+    auto load_set = [&](int s) {
+      const int h = min(s * HS + lane / LN, H - 1);
+      const T* x = reinterpret_cast<const T*>(a.qkv) + m * a.row_stride + (int64_t)h * HD + 8 * (lane % LN);
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) raw[j][i] = load_nt(x + j * (HD / 2) + i * 16 / (int)sizeof(T));
+    };
+    load_set(s0);
     const Start st = append_start(a, b, lane == 0 && s0 == 0);
     if (st.pos < 0) return;
     const int64_t pos = st.pos + r;
@@ -138,23 +159,22 @@ __global__ void __launch_bounds__(256) append_kernel(AppendArgs a) {
     }
     const int page = page_of(a.pg, st.row, pos, lane == 0 && s0 == 0 ? a.err : nullptr);
     const int in_page = (int)(pos & ((1 << a.pg.log_page) - 1));
-    for (int s = s0; s < min(sets, s0 + a.per_wave); ++s) {
+    for (int s = s0; s < s1; ++s) {
       const int h = s * HS + lane / LN;
-      const bool on = h < H;
+      const bool on = h < H;  // (lanes past the last head work on it too and store nothing)
       const bool is_q = h < a.hq;
       float y[16];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) y[i] = 0.f;
-      if (on) {
-        load8<T>(a.qkv, m * a.row_stride + (int64_t)h * HD + d, y);
-        load8<T>(a.qkv, m * a.row_stride + (int64_t)h * HD + d + HD / 2, y + 8);
-      }
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < NV; ++i) unpack16(raw[j][i], y + 8 * j + i * 16 / (int)sizeof(T), T());
+      load_set(min(s + 1, s1 - 1));
       const float* gain = is_q ? a.q_gain : a.k_gain;
       float ss = 0.f;
 #pragma unroll
       for (int i = 0; i < 16; ++i) ss = __builtin_fmaf(y[i], y[i], ss);
       ss = lanes_op<LN>(ss, add);
-      if (gain && on) {
+      if (gain) {
         const float inv = 1.f / sqrtf(ss / (float)HD + a.eps);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -210,10 +230,9 @@ __global__ void __launch_bounds__(256) append_kernel(AppendArgs a) {
   }
   // v: an item is (sequence, group of 8 positions, head), LN lanes of 8 dimensions each
   constexpr int LN = HD / 8, IT = kWave / LN;
-  const int64_t item = ((int64_t)(blockIdx.x - a.n_qk) * 4 + wave) * IT + lane / LN;
-  const int h = (int)(item % a.pg.hkv);
-  const int64_t bg = item / a.pg.hkv;
-  const int b = (int)(bg / a.v_groups), grp = (int)(bg % a.v_groups), d = 8 * (lane % LN);
+  const int item = (((int)blockIdx.x - a.n_qk) * 4 + wave) * IT + lane / LN;
+  const int bg = a.by_hkv.div(item), h = item - bg * a.pg.hkv;
+  const int b = a.by_groups.div(bg), grp = bg - b * a.v_groups, d = 8 * (lane % LN);
   Start st{-1, 0};
   if (b < a.B) st = append_start(a, b, false);
   const int64_t g0 = st.pos / 8 * 8 + 8 * (int64_t)grp;  // the group's first position
@@ -410,15 +429,18 @@ void launch_append_t(const AppendArgs& a, int hd, int blocks, hipStream_t st) {
 int launch_paged_append(AppendArgs a, int hd, bool e4, bool f32, hipStream_t st) {
   const int H = a.hq + a.pg.hkv, hs = kWave / (hd / 16), sets = (int)ceil_div(H, hs);
   const int64_t rows = (int64_t)a.B * a.R;
-  // one set of heads per wave while the waves are few (latency), all of a row's with many rows (the table's and the gains'
-  // loads then serve them all)
-  a.per_wave = rows * sets <= 8192 ? 1 : sets;
+  // one set of heads per wave while the waves are few (latency); three, the table's loads serving them all, up to what fills
+  // the device; all of a row's beyond.  Measured, 64/8 heads of 128 (9 sets), bf16, sets a wave 1, 3, 9: 264 rows 6.8, 5.7, 6.6 us;
+  // 1024 rows 15.1, 15.2, 17.6 (e4m3 pages 15.3, 11.8, 16.9); 4095 rows 48, 40, 38
+  a.per_wave = rows * sets <= 1024 ? 1 : std::min(sets, rows <= 2560 ? 3 : sets);
   const int64_t waves = rows * ceil_div(sets, a.per_wave);
   a.v_groups = (int)((a.R + 14) / 8);
   const int64_t v_items = (int64_t)a.B * a.v_groups * a.pg.hkv, per = kWave / (hd / 8);
   const int64_t nqk = ceil_div(waves, 4), nv = ceil_div(v_items, 4 * per);
-  if (nqk + nv >= (int64_t(1) << 31)) return fail(SDD_EUNSUPPORTED, "%lld rows in one call", (long long)rows);
+  if (std::max(4 * nqk, nv * 4 * per) >= (int64_t(1) << 31)) return fail(SDD_EUNSUPPORTED, "%lld rows in one call", (long long)rows);
   a.n_qk = (int)nqk;
+  a.by_waves = FastDiv((uint32_t)ceil_div(sets, a.per_wave)), a.by_r = FastDiv(a.R);
+  a.by_hkv = FastDiv(a.pg.hkv), a.by_groups = FastDiv(a.v_groups);
   const int blocks = (int)(nqk + nv);
   prof_begin(PROF_PAGES, st);
   if (f32) {
