@@ -4,8 +4,8 @@
 // Both are streams: a row's (n_q + 2 n_kv) heads are read once, q is written once and K/V once in the cache's type; the
 // rotation's cosines and sines are read from a table (angles in 64 bits when it is made: in 32 bits, position 10^5 would be
 // off by 4e-3 rad at the first frequency).  Bound: the memory.  64/8 heads of 128: 4095 rows appended (168 MB, norms and
-// rotation) 38 us, 4.4 TB/s where a copy of torch's runs at 4.9; eight prefixes of 4001 positions read from e4m3 pages (197 MB)
-// 36 us, 5.5 TB/s, from bf16 (262 MB) 50; one row appended 4.4 us, read 3.2.
+// rotation) 42 us, 4.0 TB/s where a copy of torch's runs at 4.9; eight prefixes of 4001 positions read from e4m3 pages (197 MB)
+// 34 us, 5.8 TB/s, from bf16 (262 MB) 45 (in- and outputs changing from call to call); one row appended 4.4 us, read 3.2.
 #include <algorithm>
 #include <cmath>
 
@@ -81,10 +81,9 @@ __device__ inline void load8(const char* base, int64_t i, float* y) {
   }
 }
 
-// 16 bytes that are read once
-__device__ inline uint4 load_nt(const void* p) {
-  const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
-  return make_uint4(v.x, v.y, v.z, v.w);
+// 16 bytes past the caches
+__device__ inline void store_nt(void* p, uint4 v) {
+  __builtin_nontemporal_store(u32x4{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4*>(p));
 }
 
 // Four values already within +-448 to their nearest e4m3 codes (ties to even), value i in byte i.
@@ -141,7 +140,7 @@ __global__ void __launch_bounds__(256) append_kernel(AppendArgs a) {
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int i = 0; i < NV; ++i) raw[j][i] = load_nt(x + j * (HD / 2) + i * 16 / (int)sizeof(T));
+        for (int i = 0; i < NV; ++i) raw[j][i] = load_nt16(x + j * (HD / 2) + i * 16 / (int)sizeof(T));
     };
     load_set(s0);
     const Start st = append_start(a, b, lane == 0 && s0 == 0);
@@ -328,7 +327,8 @@ __device__ inline void unpack_e4m3x8(uint2 c, float s, float* y) {
 }
 
 // An item is (sequence, group of 8 positions, head); LN = HD / 8 lanes, 8 dimensions each.  K: position by position, 16
-// bytes out of (e4m3: 8) and into place.  V: the lane's 8 dimensions of all 8 positions, turned in registers.
+// bytes out of (e4m3: 8) and into place.  V: the lane's 8 dimensions of all 8 positions, turned in registers.  Stored past the
+// caches (eight prefixes of 4001 positions, bf16: 45 us, 52 with ordinary stores).
 template <bool E4, int HD>
 __global__ void __launch_bounds__(256) read_kernel(ReadArgs a) {
   constexpr int LN = HD / 8;
@@ -380,8 +380,8 @@ __global__ void __launch_bounds__(256) read_kernel(ReadArgs a) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) z[e] = vt[e][i] * s;
       if (i >= lo && i < hi) {
-        *reinterpret_cast<uint4*>(a.k + o0 + i * ostep) = pack(y);
-        *reinterpret_cast<uint4*>(a.v + o0 + i * ostep) = pack(z);
+        store_nt(a.k + o0 + i * ostep, pack(y));
+        store_nt(a.v + o0 + i * ostep, pack(z));
       }
     }
   } else {
@@ -401,8 +401,8 @@ __global__ void __launch_bounds__(256) read_kernel(ReadArgs a) {
         w[j] = i % 2 ? (xw >> 16) | (yw & 0xffff0000u) : (xw & 0xffffu) | (yw << 16);
       }
       if (i >= lo && i < hi) {
-        *reinterpret_cast<uint4*>(a.k + o0 + i * ostep) = kc[i];
-        *reinterpret_cast<uint4*>(a.v + o0 + i * ostep) = make_uint4(w[0], w[1], w[2], w[3]);
+        store_nt(a.k + o0 + i * ostep, kc[i]);
+        store_nt(a.v + o0 + i * ostep, make_uint4(w[0], w[1], w[2], w[3]));
       }
     }
   }
