@@ -619,146 +619,144 @@ __global__ void __launch_bounds__(kWideWaves * kWave, E4 ? 2 : 3) paged_attn_wid
   f32x16 o[DB];
   float m = -INFINITY, l = 0.f;           // (m: of the scores before the scale)
   float ref = 0.f, m_far = -INFINITY;     // -m scale (0 for no m), and the score from which m moves
-  {
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+  for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
-    turn_page();
+    for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+  turn_page();
 #pragma unroll
-    for (int i = 0; i < RS - 1; ++i) issue();
-    uint32_t so = 0;  // this step's byte offset in the ring
-    auto next_step = [&]() {
-      __builtin_amdgcn_s_waitcnt(wait_vmcnt((RS - 2) * L));
-      phase_barrier();  // the step is whole, and the slot of the step before it has been read by every wave
-      issue();
-    };
-    // Step p, at so in the ring.  INNER: every query vector sees the whole of it.
-    auto step = [&](auto inner_c, int p, bool ok) {
-      constexpr bool inner = decltype(inner_c)::value;
-      const uint32_t at_step = so;
-      f32x16 s;
+  for (int i = 0; i < RS - 1; ++i) issue();
+  uint32_t so = 0;  // this step's byte offset in the ring
+  auto next_step = [&]() {
+    __builtin_amdgcn_s_waitcnt(wait_vmcnt((RS - 2) * L));
+    phase_barrier();  // the step is whole, and the slot of the step before it has been read by every wave
+    issue();
+  };
+  // Step p, at so in the ring.  INNER: every query vector sees the whole of it.
+  auto step = [&](auto inner_c, int p, bool ok) {
+    constexpr bool inner = decltype(inner_c)::value;
+    const uint32_t at_step = so;
+    f32x16 s;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 0.f;
-      float vs[E4 ? 16 : 1];
-      auto at = [&](int i) { return 16 * (i / 4 % 2) + 8 * half + 4 * (i / 8) + i % 4; };  // position of s[i]
+    for (int i = 0; i < 16; ++i) s[i] = 0.f;
+    float vs[E4 ? 16 : 1];
+    auto at = [&](int i) { return 16 * (i / 4 % 2) + 8 * half + 4 * (i / 8) + i % 4; };  // position of s[i]
+    if constexpr (E4) {
+      u32x4 kr[KS / 2];
+      u32x2 sb[3];  // scale bytes: of the lane's K row, V's of positions 8 half .. and 16 + 8 half ..
+      lds_read_e4<KS / 2>(kr, sb, rd_k + at_step, rd_ks + at_step, rd_vs + at_step);
+      const float ks = scale_value((int)sb[0][0]);
+#pragma unroll
+      for (int i = 0; i < KS; ++i)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(e4m3_frag(kr[i / 2][i % 2 * 2], kr[i / 2][i % 2 * 2 + 1], ks), qf[i], s, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)  // byte 4 (i / 8) + i % 4 of the eight from 16 (i / 4 % 2) + 8 half
+        vs[i] = scale_value((sb[1 + i / 4 % 2][i / 8] >> (8 * (i % 4))) & 255);
+    } else {
+#pragma unroll
+      for (int h = 0; h < KS; h += 4) {
+        u32x4 kr[4];
+        lds_read16<4, 4, 0, 512>(kr, rd_k + at_step + h * 512);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[i]), qf[h + i], s, 0, 0, 0);
+      }
+    }
+    float sv[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sv[i] = s[i];
+    if constexpr (!inner) {
+      const int e = ok ? min(qpos + 1, p_end) : 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sv[i] = p + at(i) < e ? sv[i] : -INFINITY;
+    }
+    float top = sv[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, sv[i]);
+    top = xor32_op(top, [](float x, float y) { return fmaxf(x, y); });
+    if (__any(top * a.scale > m_far)) {
+      const float mn = fmaxf(m, top);
+      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * a.scale);
+      l *= f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] *= f;
+      m = mn;
+      ref = m == -INFINITY ? 0.f : -m * a.scale;
+      m_far = m == -INFINITY ? -INFINITY : kFar - ref;
+    }
+    float e[16], sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[i], a.scale, ref));
+      sum += e[i];
+    }
+    l += sum;
+    if constexpr (E4) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) e[i] *= vs[i];
+      if constexpr (!inner) {  // (a position that was never written may have any scale byte)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) e[i] = sv[i] == -INFINITY ? 0.f : e[i];
+      }
+    }
+    bf16x8 pf[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)  // positions 16 h + 8 half .. + 7: registers 4 h .. and 8 + 4 h ..
+      pf[h] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16x2(e[4 * h], e[4 * h + 1]), pack_bf16x2(e[4 * h + 2], e[4 * h + 3]),
+                                                    pack_bf16x2(e[8 + 4 * h], e[9 + 4 * h]),
+                                                    pack_bf16x2(e[10 + 4 * h], e[11 + 4 * h])));
+    // V operands, 64 dimensions at a time: operand 2 db + h holds dimension 32 db + lane % 32, positions 16 h + 8 half .. + 7
+#pragma unroll
+    for (int g = 0; g < DB; g += 2) {
+      bf16x8 v[4];
       if constexpr (E4) {
-        u32x4 kr[KS / 2];
-        u32x2 sb[3];  // scale bytes: of the lane's K row, V's of positions 8 half .. and 16 + 8 half ..
-        lds_read_e4<KS / 2>(kr, sb, rd_k + at_step, rd_ks + at_step, rd_vs + at_step);
-        const float ks = scale_value((int)sb[0][0]);
+        u32x2 vr[4];
+        lds_read8<4, 512>(vr, rd_v + at_step + g * 1024);
 #pragma unroll
-        for (int i = 0; i < KS; ++i)
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(e4m3_frag(kr[i / 2][i % 2 * 2], kr[i / 2][i % 2 * 2 + 1], ks), qf[i], s, 0, 0, 0);
-#pragma unroll
-        for (int i = 0; i < 16; ++i)  // byte 4 (i / 8) + i % 4 of the eight from 16 (i / 4 % 2) + 8 half
-          vs[i] = scale_value((sb[1 + i / 4 % 2][i / 8] >> (8 * (i % 4))) & 255);
+        for (int i = 0; i < 4; ++i) v[i] = e4m3_frag(vr[i][0], vr[i][1], 1.f);
       } else {
+        u32x4 vr[4];
+        lds_read16<4, 2, 2048, 512>(vr, rd_v + at_step + g * 2048);
 #pragma unroll
-        for (int h = 0; h < KS; h += 4) {
-          u32x4 kr[4];
-          lds_read16<4, 4, 0, 512>(kr, rd_k + at_step + h * 512);
+        for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(bf16x8, vr[i]);
+      }
+      if constexpr (!inner) {  // positions from p_end on zeroed: their weights are 0, and 0 times a stale non-finite value would not be
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[i]), qf[h + i], s, 0, 0, 0);
+        for (int i = 0; i < 4; ++i) {
+          const int n = (ok ? p_end : 0) - (p + 16 * (i % 2) + 8 * half);
+          u32x4 w = __builtin_bit_cast(u32x4, v[i]);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) w[k] &= (2 * k < n ? 0xffffu : 0u) | (2 * k + 1 < n ? 0xffff0000u : 0u);
+          v[i] = __builtin_bit_cast(bf16x8, w);
         }
       }
-      float sv[16];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sv[i] = s[i];
-      if constexpr (!inner) {
-        const int e = ok ? min(qpos + 1, p_end) : 0;
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sv[i] = p + at(i) < e ? sv[i] : -INFINITY;
-      }
-      float top = sv[0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, sv[i]);
-      top = xor32_op(top, [](float x, float y) { return fmaxf(x, y); });
-      if (__any(top * a.scale > m_far)) {
-        const float mn = fmaxf(m, top);
-        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * a.scale);
-        l *= f;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[db][i] *= f;
-        m = mn;
-        ref = m == -INFINITY ? 0.f : -m * a.scale;
-        m_far = m == -INFINITY ? -INFINITY : kFar - ref;
-      }
-      float e[16], sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(sv[i], a.scale, ref));
-        sum += e[i];
-      }
-      l += sum;
-      if constexpr (E4) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) e[i] *= vs[i];
-        if constexpr (!inner) {  // (a position that was never written may have any scale byte)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) e[i] = sv[i] == -INFINITY ? 0.f : e[i];
-        }
-      }
-      bf16x8 pf[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h)  // positions 16 h + 8 half .. + 7: registers 4 h .. and 8 + 4 h ..
-        pf[h] = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16x2(e[4 * h], e[4 * h + 1]), pack_bf16x2(e[4 * h + 2], e[4 * h + 3]),
-                                                      pack_bf16x2(e[8 + 4 * h], e[9 + 4 * h]),
-                                                      pack_bf16x2(e[10 + 4 * h], e[11 + 4 * h])));
-      // V operands, 64 dimensions at a time: operand 2 db + h holds dimension 32 db + lane % 32, positions 16 h + 8 half .. + 7
-#pragma unroll
-      for (int g = 0; g < DB; g += 2) {
-        bf16x8 v[4];
-        if constexpr (E4) {
-          u32x2 vr[4];
-          lds_read8<4, 512>(vr, rd_v + at_step + g * 1024);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = e4m3_frag(vr[i][0], vr[i][1], 1.f);
-        } else {
-          u32x4 vr[4];
-          lds_read16<4, 2, 2048, 512>(vr, rd_v + at_step + g * 2048);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(bf16x8, vr[i]);
-        }
-        if constexpr (!inner) {  // positions from p_end on zeroed: their weights are 0, and 0 times a stale non-finite value would not be
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int n = (ok ? p_end : 0) - (p + 16 * (i % 2) + 8 * half);
-            u32x4 w = __builtin_bit_cast(u32x4, v[i]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] &= (2 * k < n ? 0xffffu : 0u) | (2 * k + 1 < n ? 0xffff0000u : 0u);
-            v[i] = __builtin_bit_cast(bf16x8, w);
-          }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int db = 0; db < 2; ++db) o[g + db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[2 * db + h], pf[h], o[g + db], 0, 0, 0);
-      }
-    };
-    int p = p_begin;
-    // the steps that every query vector sees whole, up to a missing page; then the others (one loop after the other: as the two
-    // sides of a branch in one loop they would each copy the accumulators)
-    const int p_inner = min(min(lo - 31, p_end - 32), tile_end - 1);
-#pragma unroll 1
-    for (; p <= p_inner && (ok_bits >> (RS - 2) & 1); p += 32) {
-      next_step();
-      step(std::true_type{}, p, true);
-      so = so + kStage == (uint32_t)(RS * kStage) ? 0 : so + kStage;
+        for (int db = 0; db < 2; ++db) o[g + db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[2 * db + h], pf[h], o[g + db], 0, 0, 0);
     }
+  };
+  int p = p_begin;
+  // the steps that every query vector sees whole, up to a missing page; then the others (one loop after the other: as the two
+  // sides of a branch in one loop they would each copy the accumulators)
+  const int p_inner = min(min(lo - 31, p_end - 32), tile_end - 1);
 #pragma unroll 1
-    for (; p < min(p_end, tile_end); p += 32) {
-      const bool ok = ok_bits >> (RS - 2) & 1;
-      next_step();
-      step(std::false_type{}, p, ok);
-      so = so + kStage == (uint32_t)(RS * kStage) ? 0 : so + kStage;
-    }
-    for (; p < p_end; p += 32) next_step();  // (steps behind the tile's last position: the other waves')
-    __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));  // (the loads past the end: they clear LDS)
+  for (; p <= p_inner && (ok_bits >> (RS - 2) & 1); p += 32) {
+    next_step();
+    step(std::true_type{}, p, true);
+    so = so + kStage == (uint32_t)(RS * kStage) ? 0 : so + kStage;
   }
+#pragma unroll 1
+  for (; p < min(p_end, tile_end); p += 32) {
+    const bool ok = ok_bits >> (RS - 2) & 1;
+    next_step();
+    step(std::false_type{}, p, ok);
+    so = so + kStage == (uint32_t)(RS * kStage) ? 0 : so + kStage;
+  }
+  for (; p < p_end; p += 32) next_step();  // (steps behind the tile's last position: the other waves')
+  __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));  // (the loads past the end: they clear LDS)
   if (a.err && bad_page && threadIdx.x == 0) atomicOr(a.err, kErrId);
   const float lsum = xor32_op(l, [](float x, float y) { return x + y; });
   // On the diagonal a position may be hidden from some of the query vectors only.  Where a V value there is not finite, the zero
