@@ -238,8 +238,9 @@ int sdd_kv_commit(sdd_kv* kv, const int32_t* seq_ids, int n_seq, const int32_t* 
  * of every KV head; the pages of a sequence, in any order and anywhere in the
  * pool, are the entries of its row of a block table (device int32
  * [B][table_width]): position p lies in page table[b][p / page_size].  Several
- * sequences may hold the same page (a common prefix); rows appended to it by
- * more than one of them in one call leave one of the values, any of them.
+ * sequences may hold the same page (a common prefix, to be read): a position
+ * that more than one of them appends to in one call, or a page named twice in
+ * a row of the table, ends up as any mix of what they wrote there.
  * Stored order, for callers that move pages themselves: head h of page p starts
  * at byte (p * n_kv_heads + h) * head_bytes with K (page_size * head_dim
  * elements), V (as many) and, for SDD_E4M3, page_size scale bytes of K and of V
@@ -272,7 +273,8 @@ int sdd_rope_table(float* table, int max_pos, int head_dim, float theta, sdd_str
  * fit (past table_width pages, the rotation table, or max_len), which sets bit0
  * of the sticky error word err (device int32, caller-zeroed; may be NULL).  A
  * page id outside [0, n_pages) sets bit2 and is never followed: nothing is
- * written there, attention does not see its positions, and reads give zeros. */
+ * written there, attention does not see its positions, and reads give zeros.
+ * Outputs and workspaces overlap no other argument. */
 
 /* A decoder's KV cache in pages, for bf16 models: one pool of n_pages pages a
  * layer, page ids meaning the same page in each of them, and one block table
@@ -284,8 +286,9 @@ int sdd_rope_table(float* table, int max_pos, int head_dim, float theta, sdd_str
  * missing ones (ids outside [0, n_pages)) set sticky bit2 and are not seen.
  * Results equal the contiguous cache's up to rounding: q, k and v pass through
  * fp32 rows, norms and rotation being a launch of their own (sdd_paged_append),
- * and the attention (sdd_paged_attention) adds in its own order; SDD_E4M3 pages
- * round K and V to 8 bits besides.  Errors: SDD_EINVAL, SDD_ENOMEM,
+ * and the attention (sdd_paged_attention) adds in its own order, which with
+ * many query vectors counts the call's sequences too; SDD_E4M3 pages round K
+ * and V to 8 bits besides.  Errors: SDD_EINVAL, SDD_ENOMEM,
  * SDD_EUNSUPPORTED (fp32 model). */
 int sdd_paged_kv_bytes(const sdd_model_config* cfg, int max_batch, int max_len, int page_size, int dtype, int n_pages,
                        size_t* bytes);

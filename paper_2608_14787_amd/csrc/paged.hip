@@ -483,7 +483,7 @@ static int pool_args(const sdd_pages* pg, const int32_t* table, int width, const
   if (rc) return rc;
   SDD_REQUIRE(pg->pages && table && len, "NULL pointer");
   SDD_REQUIRE((uintptr_t)pg->pages % 256 == 0, "pages must be 256-byte aligned");
-  SDD_REQUIRE(B > 0 && R > 0 && R <= (1 << 24) && width > 0, "bad shape B=%d rows=%d table_width=%d", B, R, width);
+  SDD_REQUIRE(B > 0 && R > 0 && R <= (1 << 24) && (int64_t)B * R <= (1 << 30) && width > 0, "bad shape B=%d rows=%d table_width=%d", B, R, width);
   d->table = table;
   d->width = width;
   return SDD_OK;

@@ -926,7 +926,7 @@ static void attn_splits(PagedAttnArgs* a) {
   a->qpad = (int)align_up(QV, 16);
   const int64_t items = a->wide ? kWideItems / std::max(a->B, kWideFew) : kTargetItems;
   a->max_splits = (int)std::max<int64_t>(1, items / ((int64_t)a->pg.hkv * a->qtiles));
-  a->whole = a->wide ? kWideChunk : a->pg.hkv * a->qtiles >= kManyItems ? kWholeMany : kWhole;
+  a->whole = a->wide ? kWideChunk : (int64_t)a->pg.hkv * a->qtiles >= kManyItems ? kWholeMany : kWhole;
   a->splits = a->max_len <= a->whole ? 1 : std::min(a->max_splits, (int)ceil_div(a->max_len, a->wide ? kWideChunk : kMinChunk));
 }
 
@@ -938,9 +938,9 @@ size_t paged_attn_workspace(PagedAttnArgs a, int hd) {
   static_assert(kSizeStep <= kMinChunk && kSizeStep <= kWideChunk, "");
   if (a.max_len <= kSizeStep) return 0;
   attn_splits(&a);
-  const int64_t most = (int64_t)a.B * a.pg.hkv * ceil_div(a.max_len, kSizeStep) * a.qpad;
-  int64_t rows = std::min(most, (int64_t)a.B * kTargetItems * 16);
-  if (a.wide) rows = std::max(rows, std::min(most, (int64_t)kWideItems * 32 * kWideWaves));
+  const int64_t most = a.pg.hkv * ceil_div(a.max_len, kSizeStep) * a.qpad, call = kWideItems * 32 * kWideWaves;  // (below 2^61)
+  int64_t rows = a.B * std::min<int64_t>(most, kTargetItems * 16);
+  if (a.wide) rows = std::max(rows, std::min(a.B * std::min(most, call), call));
   return (size_t)rows * (hd + 2) * 4;
 }
 
@@ -948,7 +948,7 @@ int launch_paged_attn(PagedAttnArgs a, int hd, bool e4, hipStream_t st) {
   attn_splits(&a);
   a.by_grp = FastDiv(a.grp), a.by_hkv = FastDiv(a.pg.hkv), a.by_b = FastDiv(a.B), a.by_qtiles = FastDiv(a.qtiles), a.by_qv = FastDiv(a.R * a.grp);
   const int64_t blocks = (ceil_div((int64_t)a.splits * a.B * a.pg.hkv, kXcds) * kXcds) * a.qtiles;
-  if (blocks >= (int64_t(1) << 31) || (int64_t)a.B * a.R * a.hq * hd / 4 * 4 / 256 >= (int64_t(1) << 31))
+  if (blocks >= (int64_t(1) << 31) || (int64_t)a.B * a.R * a.hq >= (int64_t(1) << 31))  // (the join's index is of 32 bits)
     return fail(SDD_EUNSUPPORTED, "%d x %d rows in one call", a.B, a.R);
   prof_begin(PROF_ATTN, st);
   if (e4) {

@@ -132,15 +132,14 @@ def _stream(stream=None):
     return C.c_void_p(s.cuda_stream)
 
 
-def _here(stream, *tensors):
-    """Raw handle of the stream to launch on; the tensors (None: absent) must be on the current device, whose kernels read
-    them."""
+def _here(*tensors):
+    """Raw handle of the current stream; the tensors (None: absent) must be on the current device, whose kernels read them."""
     dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else 0
     for t in tensors:
         if t is not None and t.get_device() != dev:
             raise ValueError(f"tensors must be on the current device cuda:{dev}, got one on {t.device}")
     # (the handle alone: torch.cuda.current_stream makes a Stream object, 2.7 us of a call's 14)
-    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(dev)
 
 
 def _need(cond: bool, msg: str):
@@ -257,6 +256,9 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, n_t
 
     Returns (logprob, entropy) fp32 [B, R] (logprob None without tokens) and, with n_top, (top int32, top_logprob
     fp32) [B, R, n_top] as well; `out` gives the tensors to write into, in that order."""
+    if stream is not None:  # (what the call makes is that stream's)
+        with torch.cuda.stream(stream):
+            return token_logprobs(logits, tokens, n_top, ws=ws, out=out)
     _rows(logits, "logits")
     B, R, V = logits.shape
     n = B * R
@@ -278,7 +280,7 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, n_t
         _i32(top, "top", allow_none=n_top == 0)
         _need(top is None or top.numel() == n * n_top, "top must be [B, R, n_top]")
     _need(ws.is_contiguous(), "ws must be contiguous")
-    st = _here(stream, logits, tokens, lp, ent, top, top_lp, ws)
+    st = _here(logits, tokens, lp, ent, top, top_lp, ws)
     _check(lib().sdd_token_logprobs(_addr(logits), _dtype_code(logits), logits.stride(0), B, R, V, _addr(tokens), n_top,
                                     _addr(lp), _addr(ent), _addr(top), _addr(top_lp), _addr(ws), ws.nbytes, st))
     return out
@@ -368,8 +370,11 @@ class PagesDesc(C.Structure):
 
 def rope_table(max_pos: int, head_dim: int, theta: float, device="cuda", stream=None) -> torch.Tensor:
     """Rotation table fp32 [max_pos, head_dim / 2, 2] (cos, sin)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return rope_table(max_pos, head_dim, theta, device)
     t = torch.empty((max_pos, head_dim // 2, 2), dtype=torch.float32, device=device)
-    _check(lib().sdd_rope_table(_ptr(t), max_pos, head_dim, theta, _stream(stream)))
+    _check(lib().sdd_rope_table(_addr(t), max_pos, head_dim, theta, _here(t)))
     return t
 
 
@@ -377,7 +382,8 @@ class PagePool:
     """One layer's pages of KV cache (sdd_pages) in a torch-owned device buffer; dtype "bf16" or "e4m3".
 
     Sequences are rows of a block table int32 [B, width] of page ids; lens int32 [B] is each sequence's cached length
-    before the call (negative: a padded slot, left alone).  err: an int32 tensor of one sticky error word, or None."""
+    before the call (negative: a padded slot, left alone).  err: an int32 tensor of one sticky error word, or None.  Calls with
+    `stream` run on it, and the tensors that they make belong to it."""
 
     def __init__(self, n_pages: int, n_kv_heads: int, head_dim: int, page_size: int = 64, dtype: str = "bf16",
                  device="cuda", buf: torch.Tensor | None = None):
@@ -400,6 +406,9 @@ class PagePool:
     def append(self, qkv: torch.Tensor, n_q_heads: int, table: torch.Tensor, lens: torch.Tensor, *, q_norm=None, k_norm=None,
                eps: float = 1e-6, rope: torch.Tensor | None = None, q_out=None, err=None, stream=None) -> torch.Tensor:
         """sdd_paged_append of qkv [B, R, (n_q_heads + 2 n_kv_heads) * head_dim]; returns q bf16 [B, R, n_q_heads, head_dim]."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.append(qkv, n_q_heads, table, lens, q_norm=q_norm, k_norm=k_norm, eps=eps, rope=rope, q_out=q_out, err=err)
         _need(qkv.dim() == 3, "qkv must be [B, R, (n_q_heads + 2 n_kv_heads) * head_dim]")
         B, R, n = qkv.shape
         hd = self.head_dim
@@ -419,7 +428,7 @@ class PagePool:
         else:
             _need(q_out.dtype == torch.bfloat16 and q_out.is_contiguous() and q_out.numel() == B * R * n_q_heads * hd,
                   "q_out must be contiguous bf16 [B, R, n_q_heads, head_dim]")
-        st = _here(stream, self.buf, table, lens, qkv, q_norm, k_norm, rope, q_out, err)
+        st = _here(self.buf, table, lens, qkv, q_norm, k_norm, rope, q_out, err)
         _check(lib().sdd_paged_append(self._desc, _addr(table), table.shape[1], _addr(lens), B, R, n_q_heads, _addr(qkv),
                                       _dtype_code(qkv), s1 if R > 1 else s0 if B > 1 else n, _addr(q_norm), _addr(k_norm), eps,
                                       _addr(rope), 0 if rope is None else rope.shape[0], _addr(q_out), _addr(err), st))
@@ -433,6 +442,9 @@ class PagePool:
                   scale: float | None = None, out=None, ws=None, err=None, stream=None) -> torch.Tensor:
         """sdd_paged_attention of q bf16 [B, R, n_q_heads, head_dim] (rows at lens .. lens + R - 1, appended before); same
         shape returned.  max_len bounds lens + R (default: what the table can hold); scale defaults to head_dim^-1/2."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.attention(q, table, lens, max_len=max_len, scale=scale, out=out, ws=ws, err=err)
         _need(q.dim() == 4 and q.dtype == torch.bfloat16 and q.is_contiguous() and q.shape[3] == self.head_dim,
               "q must be contiguous bf16 [B, R, n_q_heads, head_dim]")
         B, R, H, hd = q.shape
@@ -446,7 +458,7 @@ class PagePool:
             _need(out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == q.numel(), "out must be contiguous bf16 like q")
         _need(ws.is_contiguous(), "ws must be contiguous")
         _i32(err, "err", allow_none=True)
-        st = _here(stream, self.buf, table, lens, q, out, err, ws)
+        st = _here(self.buf, table, lens, q, out, err, ws)
         _check(lib().sdd_paged_attention(self._desc, _addr(table), table.shape[1], _addr(lens), B, R, H, _addr(q),
                                          hd ** -0.5 if scale is None else scale, max_len, _addr(out), _addr(err), _addr(ws),
                                          ws.nbytes, st))
@@ -454,6 +466,9 @@ class PagePool:
 
     def read(self, table: torch.Tensor, start: torch.Tensor, n: int, *, out=None, err=None, stream=None):
         """sdd_paged_read of positions start .. start + n - 1: (k, v) bf16 [B, n, n_kv_heads, head_dim]."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.read(table, start, n, out=out, err=err)
         B = start.numel()
         self._seqs(table, start, B)
         shape = (B, n, self.n_kv_heads, self.head_dim)
@@ -466,7 +481,7 @@ class PagePool:
                 _need(t.dtype == torch.bfloat16 and t.is_contiguous() and t.numel() == math.prod(shape),
                       "k and v must be contiguous bf16 [B, n, n_kv_heads, head_dim]")
         _i32(err, "err", allow_none=True)
-        st = _here(stream, self.buf, table, start, k, v, err)
+        st = _here(self.buf, table, start, k, v, err)
         _check(lib().sdd_paged_read(self._desc, _addr(table), table.shape[1], _addr(start), B, n, _addr(k), _addr(v), _addr(err), st))
         return k, v
 
@@ -612,6 +627,7 @@ class PagedKVCache(KVCache):
 
     def assign(self, seq: int, positions: int):
         """Gives sequence seq the pages that `positions` positions need (those it holds stay); raises when none are free."""
+        _need(0 <= seq < self.max_batch, f"bad seq {seq}")
         have, want = len(self.held[seq]), -(-positions // self.page_size)
         _need(positions <= self.max_len, f"{positions} positions exceed max_len {self.max_len}")
         if want <= have:
@@ -624,6 +640,7 @@ class PagedKVCache(KVCache):
 
     def release(self, seq: int):
         """Takes all pages back from sequence seq."""
+        _need(0 <= seq < self.max_batch, f"bad seq {seq}")
         self.free += reversed(self.held[seq])
         self.held[seq] = []
         self.table[seq] = -1

@@ -233,3 +233,62 @@ def test_nan_in_one_part(S, dtype, where):  # noqa: F811
         assert ((got - want).abs() <= tol)[clean].all()
         dims = slice(5, 6) if where == "v" and dtype == "bf16" else slice(None)
         assert torch.isnan(got[first:, 4:, dims]).all()
+
+
+# ---- streams and devices ---------------------------------------------------------------------------------
+
+
+def test_tensors_made_on_another_stream_are_its_own(S):  # noqa: F811
+    """Outputs and workspaces that calls on a busy stream make are not handed out again before that stream is done with them."""
+    hq, hkv, hd, at = 8, 2, 128, [2000, 20]
+    c, k, v = fill(S, "bf16", hkv, hd, 64, 1, at)
+    q, lens = randn(4, 2, 1, hq, hd).to(torch.bfloat16).cuda(), i32(at)
+    z, tok = randn(5, 2, 3, 5000).float().cuda(), i32([[1, 2, 3], [4, 5, 4999]])
+    rows = randn(6, 2, 1, (hq + 2 * hkv) * hd).to(torch.bfloat16).cuda()
+    want = (c.pool.attention(q, c.table, lens), *c.pool.read(c.table, i32([0, 0]), 20), *S.token_logprobs(z, tok, 5),
+            S.rope_table(64, hd, 1e4))
+    start, side, slow = i32([0, 0]), torch.cuda.Stream(), torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(8):
+            slow = slow @ slow * 1e-3
+    got = (c.pool.attention(q, c.table, lens, stream=side), *c.pool.read(c.table, start, 20, stream=side),
+           *S.token_logprobs(z, tok, 5, stream=side), S.rope_table(64, hd, 1e4, stream=side))
+    qo = c.pool.append(rows, hq, c.table, i32([-1, -1]), stream=side)
+    junk = [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in (1 << 12, 1 << 14, 1 << 16, 1 << 18, 1 << 20) for _ in range(4)]
+    torch.cuda.synchronize()
+    assert qo.shape == (2, 1, hq, hd) and len(junk) == 20
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+
+
+def test_two_calls_at_once(S):  # noqa: F811
+    """Calls on two streams over one pool, each with a workspace of its own."""
+    hq, hkv, hd, R, at = 64, 8, 128, 33, [700, 3, 260, 0, 1900, 41, 513]
+    c, k, v = fill(S, "bf16", hkv, hd, 64, R, at)
+    q = randn(4, 7, R, hq, hd).to(torch.bfloat16).cuda()
+    q1 = q[:, :1].contiguous()
+    lens, many, one = i32(at), c.pool.attention(q, c.table, i32(at)), c.pool.attention(q1, c.table, i32(at))
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = [(c.pool.attention(q, c.table, lens, stream=a), c.pool.attention(q1, c.table, lens, stream=b)) for _ in range(8)]
+    torch.cuda.synchronize()
+    for x, y in got:
+        assert torch.equal(x, many) and torch.equal(y, one)
+
+
+def test_tensors_off_the_device_are_refused(S):  # noqa: F811
+    c, k, v = fill(S, "bf16", 2, 64, 32, 1, [40])
+    q = randn(4, 1, 1, 4, 64).to(torch.bfloat16)
+    good, lens = q.cuda(), i32([40])
+    for args in ((q, c.table, lens), (good, c.table.cpu(), lens), (good, c.table, lens.cpu())):
+        with pytest.raises(ValueError, match="device"):
+            c.pool.attention(*args)
+    with pytest.raises(ValueError, match="device"):
+        c.pool.attention(good, c.table, lens, out=torch.empty_like(q))
+    with pytest.raises(ValueError, match="device"):
+        c.pool.read(c.table.cpu(), i32([0]), 3)
+    with pytest.raises(ValueError, match="device"):
+        c.pool.append(torch.zeros(1, 1, 8 * 64, dtype=torch.bfloat16), 4, c.table, lens)
+    with pytest.raises(ValueError, match="device"):
+        S.token_logprobs(torch.zeros(1, 2, 8).cuda(), torch.zeros(1, 2, dtype=torch.int32))

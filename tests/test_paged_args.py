@@ -138,3 +138,21 @@ def test_binding_refusals(S):  # noqa: F811
     with pytest.raises(ValueError):
         S.token_logprobs(torch.zeros(1, 8, 2).transpose(1, 2))
     assert os.path.exists(S.LIB_PATH)
+
+
+@pytest.mark.parametrize("B, n", [(2 ** 31 - 1, 1 << 24), (1 << 30, 3), (65, 1 << 24)])
+def test_more_positions_than_an_index_holds(S, B, n):  # noqa: F811
+    d = pages(S)
+    assert S.lib().sdd_paged_read(C.byref(d), A, 4, A, B, n, A, A, None, None) == S.EINVAL
+    assert append(S, B=B, R=n) == S.EINVAL
+
+
+def test_attention_workspace_of_extreme_shapes(S):  # noqa: F811
+    """Sizes stay in range where the product of all factors would pass 64 bits."""
+    out = C.c_size_t()
+    hkv = 1024
+    big = pages(S, hkv=hkv)
+    size = S.lib().sdd_paged_attention_workspace_bytes
+    for B, R, hq in ((1 << 24, 1, hkv), (1, 1 << 20, hkv), (1 << 12, 1 << 12, 64 * hkv)):
+        assert size(C.byref(big), B, R, hq, 1 << 30, C.byref(out)) == S.OK
+        assert 0 < out.value <= B * 512 * 16 * 130 * 4 + 2048 * 128 * 130 * 4
