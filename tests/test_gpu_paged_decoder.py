@@ -217,3 +217,67 @@ def test_refusals(S):
     with pytest.raises(S.SDDError) as e:
         S.PagedKVCache(tiny, 1, 100, 4)
     assert e.value.code == S.EUNSUPPORTED
+
+
+MANY = {"hd64": W.ModelShape(2, 512, 16, 8, 64, 1024, 2048, 1e-6, 1e6, True, "bf16"),
+        "hd128": W.ModelShape(2, 512, 16, 8, 128, 1088, 2176, 1e-6, 1e6, False, "bf16")}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("name", list(MANY))
+def test_many_query_vectors(S, name, dtype):
+    """Calls that take the attention kernel of many query vectors (20 x 8 and 21 x 8 workgroups of 128): a batch of 20 sequences,
+    and a prompt's chunk of 1300 rows, against the contiguous cache and against the sequences one by one."""
+    shape = MANY[name]
+    m = S.Model(shape)
+    m.init_random(12, W.WEIGHT_SIGMA)
+    n, R, V = 20, 33, shape.vocab
+    assert n * 8 * -(-R * 2 // 128) >= 160 and 8 * -(-1300 * 2 // 128) >= 160
+    tol = TOL if dtype == "bf16" else TOL + 2.0 ** -3  # (8-bit K and V, as above)
+    lens = [3 + 31 * s for s in range(n)]
+    kv, cv = S.PagedKVCache(m, n, 1400, 600, 32, dtype), S.KVCache(m, n, 1400)
+    ws = kv.workspace(1400)
+    for s in range(n):
+        kv.assign(s, lens[s] + R)
+        for c in (kv, cv):
+            c.prefill(s, to_dev_i32(W.prompt(s, lens[s], V)), ws)
+    drafts = W.prompt(51, n * (R - 1), V).reshape(n, R - 1)
+    both = verify(kv, list(range(n)), drafts, V, ws)
+    assert torch.equal(both, verify(kv, list(range(n)), drafts, V, ws))
+    plain = verify(cv, list(range(n)), drafts, V, ws)
+    ok, rel = row_tol_ok(both.flatten(0, 1).cpu().numpy(), plain.flatten(0, 1).cpu().numpy(), tol)
+    assert ok.all(), rel.max()
+    for s in (0, 7, 19):
+        one = verify(kv, [s], drafts[s:s + 1], V, ws)[0].cpu().numpy()
+        ok, rel = row_tol_ok(both[s].cpu().numpy(), one, TOL)
+        assert ok.all(), (s, rel.max())
+    for s in range(1, n):
+        kv.release(s)
+    kv.assign(0, 1301 + R)
+    toks = to_dev_i32(W.prompt(77, 1301, V))
+    for c in (kv, cv):
+        c.prefill(0, toks, ws)
+    got, want = (verify(c, [0], drafts[:1], V, ws)[0].cpu().numpy() for c in (kv, cv))
+    ok, rel = row_tol_ok(got, want, tol)
+    assert ok.all(), rel.max()
+    assert kv.state()[2] == 0 and cv.state()[2] == 0
+
+
+def test_a_batch_with_a_refused_sequence(S):
+    """A sequence without room among many: reported, its rows' attention left alone, the others' results as without it."""
+    shape = MANY["hd64"]
+    m = S.Model(shape)
+    m.init_random(13, W.WEIGHT_SIGMA)
+    n, R, V = 20, 33, shape.vocab
+    kv = S.PagedKVCache(m, n, 128, 70, 32, "bf16")
+    ws = kv.workspace(n * R)
+    for s in range(n):
+        kv.assign(s, 96)
+        kv.prefill(s, to_dev_i32(W.prompt(s, 60, V)), ws)
+    drafts = W.prompt(52, n * (R - 1), V).reshape(n, R - 1)
+    want = verify(kv, list(range(n)), drafts, V, ws)
+    kv.commit(to_dev_i32([5]), to_dev_i32([50]), to_dev_i32([1]))  # 110 positions: 33 more pass max_len
+    got = verify(kv, list(range(n)), drafts, V, ws)
+    rest = [s for s in range(n) if s != 5]
+    assert kv.state()[2] & 1
+    assert torch.equal(got[rest], want[rest])
