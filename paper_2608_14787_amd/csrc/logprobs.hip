@@ -13,10 +13,11 @@
 //
 // Bound: the arithmetic, close to the memory.  A bf16 logit costs 11 instructions of which the exponential counts
 // four times; 528 rows of 151936 (160 MB, 22.6 us at the copy's 7.1 TB/s) take 35 us without alternatives, 43 with one, 45
-// with 5, 55 with 20; one row of 152064 floats takes 5.1 and 9.7 with 20.  The time above that of no alternatives goes to
-// the sorts (a fixed cost of a workgroup) and to the tokens that pass: so few workgroups with long chunks, 2048 at
-// most.  528 rows, 20 alternatives: 55 us in 1584 workgroups, 62 in 3696, 93 in 8448.  With two vectors in flight instead of
-// four the same rows take 65 (the first threshold comes from half as many tokens); one row of 4096: 12 instead of 6.
+// with 5, 50 with 20 (57 where each token that passed was picked out of its vector at once); one row of 152064 floats takes 5.0
+// and 9.5 with 20.  The time above that of no alternatives goes to the sorts (a fixed cost of a workgroup) and to the tokens
+// that pass: so few workgroups with long chunks, 2048 at most.  528 rows, 20 alternatives: in 3696 workgroups 7 us more than in
+// 1584, in 8448 38.  With two vectors in flight instead of four the same rows take 9 us more (the first threshold comes from
+// half as many tokens), one row of 4096 twice as long.
 #include <algorithm>
 #include <type_traits>
 
@@ -155,11 +156,13 @@ __device__ inline void flush(Best& b, int n) {
   const uint64_t t = lane_key(b.best, n - 1);
   if (t > b.thr) set_thr(b, t);
 }
+__device__ inline int lanes_below(uint64_t mask) {  // lanes of the mask before this one
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
 __device__ inline void push(Best& b, uint64_t key, bool pass, int n) {
   const uint64_t mask = __builtin_amdgcn_ballot_w64(pass);
   if (mask == 0) return;
-  const int at = __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
-  if (pass) b.buf[b.cnt + at] = key;
+  if (pass) b.buf[b.cnt + lanes_below(mask)] = key;
   b.cnt += __builtin_popcountll(mask);
   if (b.cnt >= kWave) flush(b, n);
 }
@@ -219,6 +222,22 @@ __device__ inline uint4 load_any(const T* p) {
   }
 }
 
+// A vector's 16 bytes again from its values (which are the type's own).
+__device__ inline uint4 repack(const float (&x)[8], uint16_t) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, x[2 * i]) >> 16 | (__builtin_bit_cast(uint32_t, x[2 * i + 1]) & 0xffff0000u);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ inline uint4 repack(const float (&x)[4], float) {
+  return make_uint4(__builtin_bit_cast(uint32_t, x[0]), __builtin_bit_cast(uint32_t, x[1]), __builtin_bit_cast(uint32_t, x[2]),
+                    __builtin_bit_cast(uint32_t, x[3]));
+}
+template <typename T>
+__device__ inline uint4 repack(const float (&x)[1], T) {
+  return make_uint4(__builtin_bit_cast(uint32_t, x[0]), 0, 0, 0);
+}
+
 template <typename T, bool TOP, int VEC>  // VEC: 16 bytes' elements, or 1 for rows of fewer
 __global__ void __launch_bounds__(kThreads) logprobs_kernel(Job j) {
   __shared__ uint64_t s_buf[TOP ? kWaves : 1][TOP ? 2 * kWave : 1];
@@ -245,6 +264,20 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(Job j) {
     b.buf = s_buf[wave];
     set_thr(b, kFloor);
   }
+  // A vector with a logit that may count is put aside whole; kGroup of them are opened at once, a lane a logit.
+  constexpr int kGroup = kWave / VEC;
+  __shared__ uint4 s_vec[TOP ? kWaves : 1][TOP ? kWave + kGroup : 1];
+  __shared__ int s_at[TOP ? kWaves : 1][TOP ? kWave + kGroup : 1];  // its first index
+  int n_vec = 0;
+  auto open_vectors = [&](int at, int n) {
+    wave_sync();
+    using E = std::conditional_t<VEC == 1, float, T>;
+    const int i = lane / VEC, e = lane % VEC, in = at + min(i, n - 1);
+    const float x = Elem<E>::to_f32(reinterpret_cast<const E*>(&s_vec[wave][in])[e]);
+    const uint64_t key = make_key(x, s_at[wave][in] + e);
+    push(b, key, i < n && key > b.thr && x > -INFINITY, j.n_top);
+    wave_sync();
+  };
   const int first = c * j.chunk;
   auto step = [&](auto unroll, int v0) {
     constexpr int U = decltype(unroll)::value;  // vectors of a thread
@@ -311,13 +344,17 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(Job j) {
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        if (!__builtin_amdgcn_ballot_w64(hi[u] >= b.thr_f)) continue;
-        const int e0 = min((v0 + u * kThreads + (int)threadIdx.x) * VEC, j.V - VEC);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          if (!__builtin_amdgcn_ballot_w64(x[u][e] >= b.thr_f)) continue;
-          const uint64_t key = make_key(x[u][e], e0 + e);
-          push(b, key, key > b.thr && x[u][e] > -INFINITY, j.n_top);
+        const uint64_t mask = __builtin_amdgcn_ballot_w64(hi[u] >= b.thr_f);
+        if (!mask) continue;
+        if (hi[u] >= b.thr_f) {
+          const int at = n_vec + lanes_below(mask);
+          s_vec[wave][at] = repack(x[u], T());
+          s_at[wave][at] = min((v0 + u * kThreads + (int)threadIdx.x) * VEC, j.V - VEC);
+        }
+        n_vec += __builtin_popcountll(mask);
+        while (n_vec >= kGroup) {
+          n_vec -= kGroup;
+          open_vectors(n_vec, kGroup);
         }
       }
     }
@@ -327,6 +364,7 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(Job j) {
   for (; v0 + kThreads < v_end; v0 += kUnroll * kThreads) step(std::integral_constant<int, kUnroll>(), v0);
   if (v0 < v_end) step(std::integral_constant<int, 1>(), v0);
   if constexpr (TOP) {
+    if (n_vec > 0) open_vectors(0, n_vec);
     if (b.cnt > 0) flush(b, j.n_top);
     wave_sync();
     b.buf[lane] = b.best;
