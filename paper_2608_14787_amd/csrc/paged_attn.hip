@@ -9,7 +9,12 @@
 // chunk of the sequence; its four waves take the chunk's 32-position steps round-robin, each step's K and V straight into the
 // wave's registers, and are joined through LDS in wave order.  paged_attn_wide_kernel, for calls with many query vectors: 128
 // of them a workgroup, sharing each step through a ring in LDS.  A third joins the chunks' results in chunk order.  The cut of
-// a sequence into chunks depends on its own length alone.
+// a sequence into chunks depends on its own length and the call's shape, not on what the others hold.
+//
+// Bound, for 64/8 heads of 128: with few rows the stream of K and V (32 ragged sequences in bf16 52 us, 5.5 TB/s; 229000
+// positions in e4m3 80 us, 5.9 TB/s) or, short, the chain of page id, loads, products and joins (one row, 513 positions 6.7 us);
+// with many the softmax's instructions beside the products (1024 rows behind 1055 positions 64 us, 0.82 PFLOP/s; 4096 rows
+// from 0 on 277, 1.0 PFLOP/s).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -412,47 +417,25 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
 // chunk.  The steps of K and V pass through a ring in LDS, loaded there directly (no registers, several steps in flight) and
 // read by every wave; e4m3 operands are converted on their way from LDS to the products.  S^T = K Q^T and O^T = V^T P^T by
 // 32x32x16 products: a lane holds 16 scores of one query vector, which are its operand of the second product as they stand
-// (the stored order of K's rows sees to that).
+// (the stored order of K's rows sees to that).  At 168 registers three workgroups share a compute unit (e4m3 keeps four values of
+// its end in scratch for that: eight sequences of 33 rows 71 us, 75 with two workgroups), and 36 or 48 KiB of LDS each.
 
-// N reads of 16 (8) bytes a lane from addr + off(i), and their wait, in one block: the compiler would hold every LDS read back
+// Four reads of 16 (8) bytes a lane from addr + off(i), and their wait, in one block: the compiler would hold every LDS read back
 // until all direct loads into LDS, those of later steps too, have landed.
-template <int N, int DIV, int HI, int LO>  // off(i) = i / DIV * HI + i % DIV * LO
+template <int DIV, int HI, int LO>  // off(i) = i / DIV * HI + i % DIV * LO
 __device__ inline void lds_read16(u32x4* f, uint32_t addr) {
   constexpr auto off = [](int i) { return i / DIV * HI + i % DIV * LO; };
-  static_assert(N == 2 || N == 4 || N == 8, "reads of a block");
-  if constexpr (N == 2) {
-    asm volatile("ds_read_b128 %0, %2 offset:%3\n\tds_read_b128 %1, %2 offset:%4\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&v"(f[0]), "=&v"(f[1]) : "v"(addr), "i"(off(0)), "i"(off(1)) : "memory");
-  } else if constexpr (N == 4) {
-    asm volatile("ds_read_b128 %0, %4 offset:%5\n\tds_read_b128 %1, %4 offset:%6\n\tds_read_b128 %2, %4 offset:%7\n\t"
-                 "ds_read_b128 %3, %4 offset:%8\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
-                 : "v"(addr), "i"(off(0)), "i"(off(1)), "i"(off(2)), "i"(off(3)) : "memory");
-  } else {
-    asm volatile("ds_read_b128 %0, %8 offset:%9\n\tds_read_b128 %1, %8 offset:%10\n\tds_read_b128 %2, %8 offset:%11\n\t"
-                 "ds_read_b128 %3, %8 offset:%12\n\tds_read_b128 %4, %8 offset:%13\n\tds_read_b128 %5, %8 offset:%14\n\t"
-                 "ds_read_b128 %6, %8 offset:%15\n\tds_read_b128 %7, %8 offset:%16\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3]), "=&v"(f[4]), "=&v"(f[5]), "=&v"(f[6]), "=&v"(f[7])
-                 : "v"(addr), "i"(off(0)), "i"(off(1)), "i"(off(2)), "i"(off(3)), "i"(off(4)), "i"(off(5)), "i"(off(6)), "i"(off(7))
-                 : "memory");
-  }
+  asm volatile("ds_read_b128 %0, %4 offset:%5\n\tds_read_b128 %1, %4 offset:%6\n\tds_read_b128 %2, %4 offset:%7\n\t"
+               "ds_read_b128 %3, %4 offset:%8\n\ts_waitcnt lgkmcnt(0)"
+               : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
+               : "v"(addr), "i"(off(0)), "i"(off(1)), "i"(off(2)), "i"(off(3)) : "memory");
 }
-template <int N, int STEP>
+template <int STEP>
 __device__ inline void lds_read8(u32x2* f, uint32_t addr) {
-  static_assert(N == 4 || N == 8, "reads of a block");
-  if constexpr (N == 4) {
-    asm volatile("ds_read_b64 %0, %4\n\tds_read_b64 %1, %4 offset:%5\n\tds_read_b64 %2, %4 offset:%6\n\t"
-                 "ds_read_b64 %3, %4 offset:%7\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
-                 : "v"(addr), "i"(STEP), "i"(2 * STEP), "i"(3 * STEP) : "memory");
-  } else {
-    asm volatile("ds_read_b64 %0, %8\n\tds_read_b64 %1, %8 offset:%9\n\tds_read_b64 %2, %8 offset:%10\n\t"
-                 "ds_read_b64 %3, %8 offset:%11\n\tds_read_b64 %4, %8 offset:%12\n\tds_read_b64 %5, %8 offset:%13\n\t"
-                 "ds_read_b64 %6, %8 offset:%14\n\tds_read_b64 %7, %8 offset:%15\n\ts_waitcnt lgkmcnt(0)"
-                 : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3]), "=&v"(f[4]), "=&v"(f[5]), "=&v"(f[6]), "=&v"(f[7])
-                 : "v"(addr), "i"(STEP), "i"(2 * STEP), "i"(3 * STEP), "i"(4 * STEP), "i"(5 * STEP), "i"(6 * STEP), "i"(7 * STEP)
-                 : "memory");
-  }
+  asm volatile("ds_read_b64 %0, %4\n\tds_read_b64 %1, %4 offset:%5\n\tds_read_b64 %2, %4 offset:%6\n\t"
+               "ds_read_b64 %3, %4 offset:%7\n\ts_waitcnt lgkmcnt(0)"
+               : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
+               : "v"(addr), "i"(STEP), "i"(2 * STEP), "i"(3 * STEP) : "memory");
 }
 
 // An e4m3 step's K operands (N reads of 16 bytes, 512 apart) and scale bytes, as above.
@@ -530,13 +513,13 @@ __device__ inline void wide_one_by_one(const PagedAttnArgs& a, const Seq& sq, in
 }
 
 template <bool E4, int HD>
-__global__ void __launch_bounds__(kWideWaves * kWave, E4 ? 2 : 3) paged_attn_wide_kernel(PagedAttnArgs a) {
+__global__ void __launch_bounds__(kWideWaves * kWave, 3) paged_attn_wide_kernel(PagedAttnArgs a) {
   constexpr int NW = kWideWaves;
   constexpr int KS = HD / 16, DB = HD / 32;   // products of a tile and step: KS for the scores, 2 DB for the values
   constexpr int NB = (E4 ? 2 : 4) * HD / 32;  // 1 KiB blocks of a step, K's then V's
   constexpr int L = NB / NW + (E4 ? 1 : 0);   // loads that a wave issues for a step (e4m3: its own copy of the scale bytes)
   constexpr int kStage = NB * 1024 + (E4 ? NW * 256 : 0);
-  constexpr int RS = E4 ? 5 : 3;              // ring stages: RS - 1 steps in flight, of 8 or 16 KiB
+  constexpr int RS = E4 ? 4 : 3;              // ring stages: RS - 1 steps in flight, of 8 or 16 KiB
   static_assert(NB % NW == 0, "a step's blocks over the waves");
   __shared__ __align__(16) char s_ring[RS * kStage];
   touch_kernargs<PagedAttnArgs>();
@@ -639,24 +622,22 @@ __global__ void __launch_bounds__(kWideWaves * kWave, E4 ? 2 : 3) paged_attn_wid
     f32x16 s;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = 0.f;
-    float vs[E4 ? 16 : 1];
+    u32x2 vs[2] = {u32x2{0, 0}, u32x2{0, 0}};  // e4m3: V's scale bytes of positions 8 half .. and 16 + 8 half ..
     auto at = [&](int i) { return 16 * (i / 4 % 2) + 8 * half + 4 * (i / 8) + i % 4; };  // position of s[i]
     if constexpr (E4) {
       u32x4 kr[KS / 2];
-      u32x2 sb[3];  // scale bytes: of the lane's K row, V's of positions 8 half .. and 16 + 8 half ..
+      u32x2 sb[3];  // scale bytes: of the lane's K row, V's
       lds_read_e4<KS / 2>(kr, sb, rd_k + at_step, rd_ks + at_step, rd_vs + at_step);
       const float ks = scale_value((int)sb[0][0]);
 #pragma unroll
       for (int i = 0; i < KS; ++i)
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(e4m3_frag(kr[i / 2][i % 2 * 2], kr[i / 2][i % 2 * 2 + 1], ks), qf[i], s, 0, 0, 0);
-#pragma unroll
-      for (int i = 0; i < 16; ++i)  // byte 4 (i / 8) + i % 4 of the eight from 16 (i / 4 % 2) + 8 half
-        vs[i] = scale_value((sb[1 + i / 4 % 2][i / 8] >> (8 * (i % 4))) & 255);
+      vs[0] = sb[1], vs[1] = sb[2];
     } else {
 #pragma unroll
       for (int h = 0; h < KS; h += 4) {
         u32x4 kr[4];
-        lds_read16<4, 4, 0, 512>(kr, rd_k + at_step + h * 512);
+        lds_read16<4, 0, 512>(kr, rd_k + at_step + h * 512);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kr[i]), qf[h + i], s, 0, 0, 0);
@@ -695,7 +676,8 @@ __global__ void __launch_bounds__(kWideWaves * kWave, E4 ? 2 : 3) paged_attn_wid
     l += sum;
     if constexpr (E4) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) e[i] *= vs[i];
+      for (int i = 0; i < 16; ++i)  // byte 4 (i / 8) + i % 4 of the eight from 16 (i / 4 % 2) + 8 half
+        e[i] *= scale_value((vs[i / 4 % 2][i / 8] >> (8 * (i % 4))) & 255);
       if constexpr (!inner) {  // (a position that was never written may have any scale byte)
 #pragma unroll
         for (int i = 0; i < 16; ++i) e[i] = sv[i] == -INFINITY ? 0.f : e[i];
@@ -713,12 +695,12 @@ __global__ void __launch_bounds__(kWideWaves * kWave, E4 ? 2 : 3) paged_attn_wid
       bf16x8 v[4];
       if constexpr (E4) {
         u32x2 vr[4];
-        lds_read8<4, 512>(vr, rd_v + at_step + g * 1024);
+        lds_read8<512>(vr, rd_v + at_step + g * 1024);
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = e4m3_frag(vr[i][0], vr[i][1], 1.f);
       } else {
         u32x4 vr[4];
-        lds_read16<4, 2, 2048, 512>(vr, rd_v + at_step + g * 2048);
+        lds_read16<2, 2048, 512>(vr, rd_v + at_step + g * 2048);
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(bf16x8, vr[i]);
       }
