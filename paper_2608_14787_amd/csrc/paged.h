@@ -109,9 +109,15 @@ struct PagedAttnArgs {
     q_xor = x < 0.f ? 0x80008000u : 0u;
   }
   int32_t* err;
-  int qtiles, splits, max_splits, whole, qpad;
-  int wide;  // the kernel for many query vectors
-  FastDiv by_grp, by_hkv, by_b, by_qtiles, by_qv;  // (set by the launch)
+  // The cut of a call for each of the kernels: blocks of query vectors, chunks that a sequence of max_len positions has, chunks
+  // at most and positions of one at least, positions up to which a sequence is not cut.
+  struct Cut {
+    int qtiles, splits, max_splits, min_chunk, whole;
+    FastDiv by_qtiles;  // (set by the launch, as those below)
+  } few, many;
+  int many_from;     // positions from which a sequence is the many-vector kernel's
+  int splits, qpad;  // of a sequence's partial results: chunks, and query vectors of one
+  FastDiv by_grp, by_hkv, by_b, by_qv;
   float* part;  // partial results
 };
 // Bytes of partial results that a call needs (B, R, hq, grp, max_len and pg.hkv are read).

@@ -47,6 +47,12 @@ constexpr int kWhole = 768, kWholeMany = 1536, kManyItems = 64;
 constexpr int kWideWaves = 4;
 constexpr int kWideBlocks = 160;
 constexpr int kWideChunk = 512, kWideItems = 2048, kWideFew = 4;
+// Below kWideBlocks the two cross where a sequence is long: both are launched, and a sequence's positions say whose it is.
+// Measured, one sequence, this kernel against the other: 256 rows of 28/4 heads (1792 vectors), behind 1000 positions 28.5 / 26,
+// 8000 59 / 138; 400 rows behind 4000 57 / 107; 256 rows of 64/8 (2048) 38 / 27 and 101 / 154, from e4m3 pages 41 / 26 and 116 /
+// 142; 65 rows (520) 27 / 13 and 47 / 68; 128 rows (1024) behind 3000 38 / 33.5, 8000 57 / 79, from e4m3 pages 66 / 77.
+constexpr int kManyVectors = 1536, kManyFrom = 2560;
+constexpr int kSomeVectors = 512, kSomeFrom = 6144;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
@@ -55,11 +61,11 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 // steps: rescaled at each rise, a third of the step's vector instructions were the accumulators'.
 constexpr float kFar = 8.f;
 
-// Positions of a chunk of a sequence of total positions; a.whole of them and fewer are not cut.
-__host__ __device__ inline int chunk_of(const PagedAttnArgs& a, int total) {
-  if (total <= a.whole) return a.whole;
-  const int c = (total + a.max_splits - 1) / a.max_splits;
-  return max(a.wide ? kWideChunk : kMinChunk, (c + 127) / 128 * 128);
+// Positions of a chunk of a sequence of total positions.
+__host__ __device__ inline int chunk_of(const PagedAttnArgs::Cut& t, int total) {
+  if (total <= t.whole) return t.whole;
+  const int c = (total + t.max_splits - 1) / t.max_splits;
+  return max(t.min_chunk, (c + 127) / 128 * 128);
 }
 
 struct Seq {
@@ -126,14 +132,14 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
   const int hkv = a.pg.hkv;
   // workgroups go to the XCDs round-robin by id: the query tiles of one (chunk, sequence, head) share an XCD's L2
   const int low = blockIdx.x % kXcds, rest = blockIdx.x / kXcds;
-  const int group = a.by_qtiles.div(rest), qt = rest - group * a.qtiles, item = group * kXcds + low;
-  if (item >= a.splits * a.B * hkv) return;
+  const int group = a.few.by_qtiles.div(rest), qt = rest - group * a.few.qtiles, item = group * kXcds + low;
+  if (item >= a.few.splits * a.B * hkv) return;
   const int bc = a.by_hkv.div(item), kvh = item - bc * hkv, c = a.by_b.div(bc), b = bc - c * a.B;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const Seq sq = attn_seq(a, b, threadIdx.x == 0 && c == 0 && kvh == 0 && qt == 0);
   if (sq.pos < 0) return;
-  const int total = sq.pos + a.R, chunk = chunk_of(a, total), n_chunks = (total + chunk - 1) / chunk;
-  if (c >= n_chunks) return;
+  const int total = sq.pos + a.R, chunk = chunk_of(a.few, total), n_chunks = (total + chunk - 1) / chunk;
+  if (c >= n_chunks || total >= a.many_from) return;
   const int QV = a.R * a.grp, qv = qt * 16 + lane % 16;
   const bool qok = qv < QV;
   const int r = qok ? a.by_grp.div(qv) : 0, hh = qok ? qv - r * a.grp : 0;
@@ -525,14 +531,14 @@ __global__ void __launch_bounds__(kWideWaves * kWave, 3) paged_attn_wide_kernel(
   touch_kernargs<PagedAttnArgs>();
   const int hkv = a.pg.hkv;
   const int low = blockIdx.x % kXcds, rest = blockIdx.x / kXcds;
-  const int group = a.by_qtiles.div(rest), qb = a.qtiles - 1 - (rest - group * a.qtiles), item = group * kXcds + low;
-  if (item >= a.splits * a.B * hkv) return;
+  const int group = a.many.by_qtiles.div(rest), qb = a.many.qtiles - 1 - (rest - group * a.many.qtiles), item = group * kXcds + low;
+  if (item >= a.many.splits * a.B * hkv) return;
   const int bc = a.by_hkv.div(item), kvh = item - bc * hkv, c = a.by_b.div(bc), b = bc - c * a.B;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave, half = lane / 32;
   const Seq sq = attn_seq(a, b, threadIdx.x == 0 && c == 0 && kvh == 0 && qb == 0);
   if (sq.pos < 0) return;
-  const int total = sq.pos + a.R, chunk = chunk_of(a, total), n_chunks = (total + chunk - 1) / chunk;
-  if (c >= n_chunks) return;
+  const int total = sq.pos + a.R, chunk = chunk_of(a.many, total), n_chunks = (total + chunk - 1) / chunk;
+  if (c >= n_chunks || total < a.many_from) return;
   const int QV = a.R * a.grp, q_block = qb * NW * 32, q0 = q_block + wave * 32, qv = q0 + lane % 32;
   const int block_end = __builtin_amdgcn_readfirstlane(sq.pos + min(a.R - 1, a.by_grp.div(q_block + NW * 32 - 1)) + 1);
   const int p_begin = c * chunk, p_end = min(block_end, p_begin + chunk);
@@ -797,7 +803,8 @@ __global__ void __launch_bounds__(kThreads) paged_combine_kernel(PagedAttnArgs a
     int p = a.rows ? a.rows[(int64_t)b * a.R].pos : a.len[b];
     const bool ok = (!a.rows || a.rows[(int64_t)b * a.R].valid) && p >= 0 && (int64_t)p + a.R <= a.max_len;
     const int total = p + a.R;
-    if (ok) n = (total + chunk_of(a, total) - 1) / chunk_of(a, total);
+    const int chunk = chunk_of(total < a.many_from ? a.few : a.many, total);
+    if (ok) n = (total + chunk - 1) / chunk;
   }
   const int64_t at = part_row(a, bh, 0, qv), stride = a.qpad;  // (of a chunk)
   const float* o = a.part + at * HD + d;
@@ -880,14 +887,13 @@ __global__ void __launch_bounds__(kThreads) paged_combine_kernel(PagedAttnArgs a
 
 template <bool E4, int HD>
 void launch_t(const PagedAttnArgs& a, hipStream_t st) {
-  const int64_t items = (int64_t)a.splits * a.B * a.pg.hkv;
-  const dim3 grid((unsigned)(ceil_div(items, kXcds) * kXcds * a.qtiles));
-  if (a.wide)
-    hipLaunchKernelGGL((paged_attn_wide_kernel<E4, HD>), grid, dim3(kWideWaves * kWave), 0, st, a);
-  else if (a.qtiles == 1)
-    hipLaunchKernelGGL((paged_attn_kernel<E4, HD, true>), grid, dim3(kThreads), 0, st, a);
-  else
-    hipLaunchKernelGGL((paged_attn_kernel<E4, HD, false>), grid, dim3(kThreads), 0, st, a);
+  auto grid = [&](const PagedAttnArgs::Cut& t) { return dim3((unsigned)(ceil_div((int64_t)t.splits * a.B * a.pg.hkv, kXcds) * kXcds * t.qtiles)); };
+  if (a.many_from <= a.max_len)
+    hipLaunchKernelGGL((paged_attn_wide_kernel<E4, HD>), grid(a.many), dim3(kWideWaves * kWave), 0, st, a);
+  if (a.many_from > 0 && a.few.qtiles == 1)
+    hipLaunchKernelGGL((paged_attn_kernel<E4, HD, true>), grid(a.few), dim3(kThreads), 0, st, a);
+  else if (a.many_from > 0)
+    hipLaunchKernelGGL((paged_attn_kernel<E4, HD, false>), grid(a.few), dim3(kThreads), 0, st, a);
   if (a.splits > 1) {
     const int64_t vecs = (int64_t)a.B * a.pg.hkv * a.R * a.grp;
     if (a.splits <= kSmallJoin)
@@ -899,37 +905,51 @@ void launch_t(const PagedAttnArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// The cut of a call: chunks per sequence at most, and those that a sequence of max_len positions has.
-static void attn_splits(PagedAttnArgs* a) {
+static void cut_call(PagedAttnArgs* a) {
   const int QV = a->R * a->grp;
-  const int64_t blocks = (int64_t)a->B * a->pg.hkv * ceil_div(QV, 32 * kWideWaves);
-  a->wide = QV > 16 && blocks >= kWideBlocks;
-  a->qtiles = (int)(a->wide ? ceil_div(QV, 32 * kWideWaves) : ceil_div(QV, 16));
+  const int64_t blocks = ceil_div(QV, 32 * kWideWaves);
+  const bool all = QV > 16 && a->B * a->pg.hkv * blocks >= kWideBlocks;
+  a->many_from = all ? 0 : QV >= kManyVectors ? kManyFrom : QV >= kSomeVectors ? kSomeFrom : INT32_MAX;
+  auto cut = [&](int64_t qtiles, int64_t items, int min_chunk, int whole, int longest) {
+    PagedAttnArgs::Cut t{};
+    t.qtiles = (int)qtiles;
+    t.max_splits = (int)std::max<int64_t>(1, items / (a->pg.hkv * qtiles));
+    t.min_chunk = min_chunk;
+    t.whole = whole;
+    t.splits = longest <= whole ? 1 : std::min(t.max_splits, (int)ceil_div(longest, min_chunk));
+    return t;
+  };
+  const int64_t tiles = ceil_div(QV, 16);
+  a->few = cut(tiles, kTargetItems, kMinChunk, a->pg.hkv * tiles >= kManyItems ? kWholeMany : kWhole, std::min(a->max_len, a->many_from));
+  a->many = cut(blocks, kWideItems / (all ? std::max(a->B, kWideFew) : kWideFew), kWideChunk, kWideChunk, a->max_len);
+  a->splits = std::max(a->many_from > 0 ? a->few.splits : 1, a->many_from <= a->max_len ? a->many.splits : 1);
   a->qpad = (int)align_up(QV, 16);
-  const int64_t items = a->wide ? kWideItems / std::max(a->B, kWideFew) : kTargetItems;
-  a->max_splits = (int)std::max<int64_t>(1, items / ((int64_t)a->pg.hkv * a->qtiles));
-  a->whole = a->wide ? kWideChunk : (int64_t)a->pg.hkv * a->qtiles >= kManyItems ? kWholeMany : kWhole;
-  a->splits = a->max_len <= a->whole ? 1 : std::min(a->max_splits, (int)ceil_div(a->max_len, a->wide ? kWideChunk : kMinChunk));
 }
 
 // Enough for a call of a->B sequences, a->R rows and a->max_len positions and for each with fewer of any of them, whichever
-// kernel takes it and however it is cut: where there is more than one chunk, kTargetItems workgroups of 16 vectors a sequence,
-// or kWideItems of 128 a call, are not passed, and no more chunks than kSizeStep positions each.
+// kernel takes it and however it is cut.  A sequence has no more chunks than kSizeStep positions each, and where it has more
+// than one kTargetItems workgroups of 16 vectors at most; or kWideItems / kWideFew of 128, of which a call has kWideItems where
+// the many-vector kernel takes all, and elsewhere less than kWideBlocks times a sequence's chunks.
 size_t paged_attn_workspace(PagedAttnArgs a, int hd) {
-  constexpr int kSizeStep = 128;
+  constexpr int kSizeStep = 128, kBlock = 32 * kWideWaves;
   static_assert(kSizeStep <= kMinChunk && kSizeStep <= kWideChunk, "");
   if (a.max_len <= kSizeStep) return 0;
-  attn_splits(&a);
-  const int64_t most = a.pg.hkv * ceil_div(a.max_len, kSizeStep) * a.qpad, call = kWideItems * 32 * kWideWaves;  // (below 2^61)
+  cut_call(&a);
+  const int64_t most = a.pg.hkv * ceil_div(a.max_len, kSizeStep) * a.qpad;  // of a sequence (below 2^61)
   int64_t rows = a.B * std::min<int64_t>(most, kTargetItems * 16);
-  if (a.wide) rows = std::max(rows, std::min(a.B * std::min(most, call), call));
+  if (a.many_from == 0) rows = std::max(rows, std::min<int64_t>(a.B * std::min<int64_t>(most, kWideItems * kBlock), kWideItems * kBlock));
+  if (a.R * a.grp >= kSomeVectors) {
+    const int64_t one = kWideItems / kWideFew * kBlock, call = kWideBlocks * kBlock * ceil_div(kWideItems / kWideFew, a.pg.hkv * (kSomeVectors / kBlock));
+    rows = std::max(rows, std::min(a.B * std::min(most, one), call));
+  }
   return (size_t)rows * (hd + 2) * 4;
 }
 
 int launch_paged_attn(PagedAttnArgs a, int hd, bool e4, hipStream_t st) {
-  attn_splits(&a);
-  a.by_grp = FastDiv(a.grp), a.by_hkv = FastDiv(a.pg.hkv), a.by_b = FastDiv(a.B), a.by_qtiles = FastDiv(a.qtiles), a.by_qv = FastDiv(a.R * a.grp);
-  const int64_t blocks = (ceil_div((int64_t)a.splits * a.B * a.pg.hkv, kXcds) * kXcds) * a.qtiles;
+  cut_call(&a);
+  a.by_grp = FastDiv(a.grp), a.by_hkv = FastDiv(a.pg.hkv), a.by_b = FastDiv(a.B), a.by_qv = FastDiv(a.R * a.grp);
+  a.few.by_qtiles = FastDiv(a.few.qtiles), a.many.by_qtiles = FastDiv(a.many.qtiles);
+  const int64_t blocks = align_up((int64_t)a.splits * a.B * a.pg.hkv, kXcds) * a.few.qtiles;  // (of either kernel at most)
   if (blocks >= (int64_t(1) << 31) || (int64_t)a.B * a.R * a.hq >= (int64_t(1) << 31))  // (the join's index is of 32 bits)
     return fail(SDD_EUNSUPPORTED, "%d x %d rows in one call", a.B, a.R);
   prof_begin(PROF_ATTN, st);

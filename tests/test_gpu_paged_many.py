@@ -292,3 +292,29 @@ def test_tensors_off_the_device_are_refused(S):  # noqa: F811
         c.pool.append(torch.zeros(1, 1, 8 * 64, dtype=torch.bfloat16), 4, c.table, lens)
     with pytest.raises(ValueError, match="device"):
         S.token_logprobs(torch.zeros(1, 2, 8).cuda(), torch.zeros(1, 2, dtype=torch.int32))
+
+
+# ---- long sequences of calls that both kernels take -------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("hq, hkv, hd, R, at", [(16, 2, 64, 200, [2359, 2360, 0, 2700]), (16, 2, 128, 65, [6078, 6079, 40]),
+                                               (8, 1, 64, 64, [6080, 9000])])
+def test_the_length_decides(S, dtype, hq, hkv, hd, R, at):  # noqa: F811
+    """Sequences on both sides of the length from which the other kernel takes them, in one call: the values, and the bits of
+    each alone and under another max_len."""
+    assert vectors(hq, hkv, R, len(at)) < 160 and R * hq // hkv >= 512
+    c, k, v = fill(S, dtype, hkv, hd, 64, R, at)
+    q = randn(9, len(at), R, hq, hd).to(torch.bfloat16)
+    got = check_attention(S, c, k, v, q, at)
+    qd = q.cuda()
+    for b, a in enumerate(at):
+        for max_len in (a + R, 20000):
+            table = torch.cat([c.table[b:b + 1], torch.full((1, 300), -1, dtype=torch.int32, device="cuda")], 1)
+            one = c.pool.attention(qd[b:b + 1], table, i32([a]), max_len=max_len)
+            assert torch.equal(one[0], got[b]), (b, max_len)
+    # a padded one, and one without its first page, among them
+    err, out = i32([0]), torch.full_like(qd, 7.0)
+    c.table[-1, 0] = -1
+    c.pool.attention(qd, c.table, i32([-1] + at[1:]), out=out, err=err)
+    assert err.item() == 4 and (out[0] == 7).all() and torch.equal(out[1:-1], got[1:-1]) and not torch.equal(out[-1], got[-1])
