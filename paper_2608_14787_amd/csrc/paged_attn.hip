@@ -38,8 +38,8 @@ constexpr int kWhole = 768, kWholeMany = 1536, kManyItems = 64;
 
 // The many-vector kernel: a workgroup's waves, a tile of 32 query vectors each; the number of such workgroups (before the cut
 // into chunks) from which a call takes it; its chunks and items.  Measured, 64/8 heads of 128, bf16, this kernel against the
-// other, both with the join: eight sequences of 284-3761 positions, 33 rows (192 workgroups) 57 / 76 us; one sequence, 1024
-// rows behind 1024 positions (512) 73 / 127; 256 rows (128) 39 / 28, and behind 8000 positions 114 / 153; 33 rows (24) 18 / 14.
+// other, both with the join: eight sequences of 284-3761 positions, 33 rows (192 workgroups) 57 / 76 us; six of 2000 (144) 45 /
+// 50; four of 1000 (96) 30 / 19; one sequence, 1024 rows behind 1024 positions (512) 73 / 127; 256 rows (128) 38 / 27.
 // Chunks of 256, 512, 768, 1024 with the first of these: 63, 57.5, 57, 61 us (longer ones leave compute units idle, shorter
 // ones write more partial results).  A call has kWideItems workgroups at most: with many sequences partial results would cost
 // more than they give (64 sequences, 33 rows: 279 us, and 366 where a sequence's chunks did not depend on the batch), with one
