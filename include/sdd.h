@@ -415,7 +415,8 @@ int sdd_confidence_prefix(const void* logits, int dtype, size_t seq_stride, int 
 
 /* Workspace bytes for sdd_token_logprobs over up to n_rows rows and n_top
  * alternatives (zeroed once by sdd_workspace_init; calls leave it reusable by
- * calls of other shapes up to these). */
+ * calls of other shapes up to these; calls that may run at the same time need
+ * one each). */
 int sdd_logprobs_workspace_bytes(int n_rows, int V, int n_top, size_t* bytes);
 
 /* What a served answer reports beside its tokens.  Row r of sequence b at logits +
