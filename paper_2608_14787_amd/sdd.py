@@ -133,10 +133,10 @@ def _stream(stream=None):
 
 
 def _here(*tensors):
-    """Raw handle of the current stream; the tensors (None: absent) must be on the current device, whose kernels read them."""
+    """Raw handle of the current stream; the tensors must be on the current device, whose kernels read them."""
     dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else 0
     for t in tensors:
-        if t is not None and t.get_device() != dev:
+        if t.get_device() != dev:
             raise ValueError(f"tensors must be on the current device cuda:{dev}, got one on {t.device}")
     # (the handle alone: torch.cuda.current_stream makes a Stream object, 2.7 us of a call's 14)
     return torch._C._cuda_getCurrentRawStream(dev)
@@ -152,8 +152,10 @@ def _i32(t, name: str, allow_none: bool = False):
     if t is None:
         _need(allow_none, f"{name} is required")
         return
-    _need(t.dtype == torch.int32, f"{name} must be int32, got {t.dtype}")
-    _need(t.is_contiguous(), f"{name} must be contiguous")
+    if t.dtype != torch.int32:  # (the message is made only where it is raised)
+        raise ValueError(f"{name} must be int32, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
 
 
 def _rows(t, name: str):
@@ -268,11 +270,13 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, n_t
     if ws is None:
         ws = logprobs_workspace(n, V, n_top, logits.device)
     if out is None:
-        dev, f32 = logits.device, torch.float32
-        out = (None if tokens is None else torch.empty((B, R), dtype=f32, device=dev), torch.empty((B, R), dtype=f32, device=dev))
+        ent = logits.new_empty((B, R), dtype=torch.float32)
+        lp, top, top_lp = None if tokens is None else torch.empty_like(ent), None, None
+        out = (lp, ent)
         if n_top:
-            out += (torch.empty((B, R, n_top), dtype=torch.int32, device=dev), torch.empty((B, R, n_top), dtype=f32, device=dev))
-        lp, ent, top, top_lp = out if n_top else out + (None, None)
+            top_lp = ent.new_empty((B, R, n_top))
+            top = ent.new_empty((B, R, n_top), dtype=torch.int32)
+            out = (lp, ent, top, top_lp)
     else:
         lp, ent, top, top_lp = tuple(out) + (None,) * (4 - len(out))
         for t, nm, k in ((lp, "logprob", n), (ent, "entropy", n), (top_lp, "top_logprob", n * n_top)):
@@ -280,9 +284,9 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor | None = None, n_t
         _i32(top, "top", allow_none=n_top == 0)
         _need(top is None or top.numel() == n * n_top, "top must be [B, R, n_top]")
     _need(ws.is_contiguous(), "ws must be contiguous")
-    st = _here(logits, tokens, lp, ent, top, top_lp, ws)
-    _check(lib().sdd_token_logprobs(_addr(logits), _dtype_code(logits), logits.stride(0), B, R, V, _addr(tokens), n_top,
-                                    _addr(lp), _addr(ent), _addr(top), _addr(top_lp), _addr(ws), ws.nbytes, st))
+    st = _here(*[t for t in (logits, tokens, lp, ent, top, top_lp, ws) if t is not None])
+    _check(lib().sdd_token_logprobs(logits.data_ptr(), _dtype_code(logits), logits.stride(0), B, R, V, _addr(tokens), n_top,
+                                    _addr(lp), _addr(ent), _addr(top), _addr(top_lp), ws.data_ptr(), ws.nbytes, st))
     return out
 
 
@@ -424,14 +428,14 @@ class PagePool:
                   "rope must be contiguous fp32 [max_pos, head_dim / 2, 2]")
         _i32(err, "err", allow_none=True)
         if q_out is None:
-            q_out = torch.empty((B, R, n_q_heads, hd), dtype=torch.bfloat16, device=qkv.device)
+            q_out = qkv.new_empty((B, R, n_q_heads, hd), dtype=torch.bfloat16)
         else:
             _need(q_out.dtype == torch.bfloat16 and q_out.is_contiguous() and q_out.numel() == B * R * n_q_heads * hd,
                   "q_out must be contiguous bf16 [B, R, n_q_heads, head_dim]")
-        st = _here(self.buf, table, lens, qkv, q_norm, k_norm, rope, q_out, err)
-        _check(lib().sdd_paged_append(self._desc, _addr(table), table.shape[1], _addr(lens), B, R, n_q_heads, _addr(qkv),
+        st = _here(self.buf, table, lens, qkv, q_out, *[t for t in (q_norm, k_norm, rope, err) if t is not None])
+        _check(lib().sdd_paged_append(self._desc, table.data_ptr(), table.shape[1], lens.data_ptr(), B, R, n_q_heads, qkv.data_ptr(),
                                       _dtype_code(qkv), s1 if R > 1 else s0 if B > 1 else n, _addr(q_norm), _addr(k_norm), eps,
-                                      _addr(rope), 0 if rope is None else rope.shape[0], _addr(q_out), _addr(err), st))
+                                      _addr(rope), 0 if rope is None else rope.shape[0], q_out.data_ptr(), _addr(err), st))
         return q_out
 
     def attention_workspace(self, B: int, R: int, n_q_heads: int, max_len: int) -> torch.Tensor:
@@ -457,10 +461,11 @@ class PagePool:
         else:
             _need(out.dtype == torch.bfloat16 and out.is_contiguous() and out.numel() == q.numel(), "out must be contiguous bf16 like q")
         _need(ws.is_contiguous(), "ws must be contiguous")
-        _i32(err, "err", allow_none=True)
-        st = _here(self.buf, table, lens, q, out, err, ws)
-        _check(lib().sdd_paged_attention(self._desc, _addr(table), table.shape[1], _addr(lens), B, R, H, _addr(q),
-                                         hd ** -0.5 if scale is None else scale, max_len, _addr(out), _addr(err), _addr(ws),
+        if err is not None:
+            _i32(err, "err")
+        st = _here(self.buf, table, lens, q, out, ws) if err is None else _here(self.buf, table, lens, q, out, ws, err)
+        _check(lib().sdd_paged_attention(self._desc, table.data_ptr(), table.shape[1], lens.data_ptr(), B, R, H, q.data_ptr(),
+                                         hd ** -0.5 if scale is None else scale, max_len, out.data_ptr(), _addr(err), ws.data_ptr(),
                                          ws.nbytes, st))
         return out
 
@@ -473,7 +478,7 @@ class PagePool:
         self._seqs(table, start, B)
         shape = (B, n, self.n_kv_heads, self.head_dim)
         if out is None:
-            k = torch.empty(shape, dtype=torch.bfloat16, device=self.buf.device)
+            k = self.buf.new_empty(shape, dtype=torch.bfloat16)
             v = torch.empty_like(k)
         else:
             k, v = out
@@ -481,8 +486,8 @@ class PagePool:
                 _need(t.dtype == torch.bfloat16 and t.is_contiguous() and t.numel() == math.prod(shape),
                       "k and v must be contiguous bf16 [B, n, n_kv_heads, head_dim]")
         _i32(err, "err", allow_none=True)
-        st = _here(self.buf, table, start, k, v, err)
-        _check(lib().sdd_paged_read(self._desc, _addr(table), table.shape[1], _addr(start), B, n, _addr(k), _addr(v), _addr(err), st))
+        st = _here(self.buf, table, start, k, v) if err is None else _here(self.buf, table, start, k, v, err)
+        _check(lib().sdd_paged_read(self._desc, table.data_ptr(), table.shape[1], start.data_ptr(), B, n, k.data_ptr(), v.data_ptr(), _addr(err), st))
         return k, v
 
 
