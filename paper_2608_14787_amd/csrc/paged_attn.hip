@@ -13,7 +13,7 @@
 //
 // Bound, for 64/8 heads of 128: with few rows the stream of K and V (32 ragged sequences in bf16 52 us, 5.5 TB/s; 229000
 // positions in e4m3 80 us, 5.9 TB/s) or, short, the chain of page id, loads, products and joins (one row, 513 positions 6.7 us);
-// with many the softmax's instructions beside the products (1024 rows behind 1055 positions 64 us, 0.82 PFLOP/s; 4096 rows
+// with many the softmax's instructions beside the products (1024 rows behind 1055 positions 65 us, 0.81 PFLOP/s; 4096 rows
 // from 0 on 277, 1.0 PFLOP/s).
 #include <algorithm>
 #include <cmath>

@@ -138,7 +138,7 @@ def _here(*tensors):
     for t in tensors:
         if t.get_device() != dev:
             raise ValueError(f"tensors must be on the current device cuda:{dev}, got one on {t.device}")
-    # (the handle alone: torch.cuda.current_stream makes a Stream object, 2.7 us of a call's 14)
+    # (the handle alone: torch.cuda.current_stream makes a Stream object, 2.7 us of what was a call's 14)
     return torch._C._cuda_getCurrentRawStream(dev)
 
 
