@@ -96,9 +96,6 @@ __device__ inline int64_t out_index(const PagedAttnArgs& a, int b, int r, int h,
   const int row = b * a.R + r;
   return a.frag ? xfrag_index<uint16_t>(row, h * HD + dim, a.hq * HD / 32) : ((int64_t)row * a.hq + h) * HD + dim;
 }
-__device__ inline void store_out1(const PagedAttnArgs& a, int b, int r, int h, int HD, int dim, float y) {
-  a.out[out_index(a, b, r, h, HD, dim)] = f32_to_bf16(y);
-}
 __device__ inline void store_out4(const PagedAttnArgs& a, int b, int r, int h, int HD, int dim, const float* y) {
   *reinterpret_cast<uint2*>(a.out + out_index(a, b, r, h, HD, dim)) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
 }
@@ -423,8 +420,12 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
 // chunk.  The steps of K and V pass through a ring in LDS, loaded there directly (no registers, several steps in flight) and
 // read by every wave; e4m3 operands are converted on their way from LDS to the products.  S^T = K Q^T and O^T = V^T P^T by
 // 32x32x16 products: a lane holds 16 scores of one query vector, which are its operand of the second product as they stand
-// (the stored order of K's rows sees to that).  At 168 registers three workgroups share a compute unit (e4m3 keeps four values of
-// its end in scratch for that: eight sequences of 33 rows 71 us, 75 with two workgroups), and 36 or 48 KiB of LDS each.
+// (the stored order of K's rows sees to that).  At 168 registers three workgroups share a compute unit (bf16 with 128 dimensions
+// keeps two values of its end in scratch for that), and 36 or 48 KiB of LDS each.
+//
+// A tile's own rows see different parts of its last steps, and a hidden position's weight of 0 does not keep out a V value that is
+// not finite.  Such values are zeroed in those steps and added behind the loop, one position after the other, to the vectors that
+// see them: 1024 rows of 64/8 heads behind 3000 positions 143 us, with a NaN in the last position 166, with one in every row 189.
 
 // Four reads of 16 (8) bytes a lane from addr + off(i), and their wait, in one block: the compiler would hold every LDS read back
 // until all direct loads into LDS, those of later steps too, have landed.
@@ -462,62 +463,6 @@ __device__ inline void lds_read_e4(u32x4* k, u32x2* sb, uint32_t ak, uint32_t ak
   sb[0][0] = ks;
 }
 
-// The 32 query vectors from q0 over positions [p_begin, p_end), one after the other and position by position: what a wave whose
-// products met a non-finite V on the diagonal computes instead.  A lane holds HD / 64 dimensions.
-template <bool E4, int HD>
-__device__ inline void wide_one_by_one(const PagedAttnArgs& a, const Seq& sq, int b, int kvh, int q0, int c, int p_begin, int p_end,
-                                       bool whole) {
-  constexpr int N = HD / 64;
-  const int lane = threadIdx.x % kWave, d0 = N * lane, lg = a.pg.log_page;
-  auto value = [&](const char* side, int off) {
-    if constexpr (E4)
-      return (float)e4m3_frag(*reinterpret_cast<const uint8_t*>(side + off), 0, 1.f)[0];
-    else
-      return bf16_to_f32(*reinterpret_cast<const uint16_t*>(side + off));
-  };
-#pragma unroll 1
-  for (int qv = q0; qv < min(q0 + 32, a.R * a.grp); ++qv) {
-    const int r = a.by_grp.div(qv), hh = qv - r * a.grp;
-    const uint16_t* Q = a.q + ((int64_t)(b * a.R + r) * a.hq + kvh * a.grp + hh) * HD + d0;
-    float q[N], y[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) q[i] = bf16_to_f32((uint16_t)((Q[i] & a.q_and) ^ (a.q_xor & 0x8000u)));
-#pragma unroll 1
-    for (int p = p_begin; p < min(p_end, sq.pos + r + 1); ++p) {
-      const int id = a.pg.table[(int64_t)sq.row * a.pg.width + (p >> lg)], in = p & ((1 << lg) - 1);
-      if ((unsigned)id >= (unsigned)a.pg.n_pages) continue;
-      const char* k = page_head(a.pg, id, kvh);
-      float s = 0.f;
-#pragma unroll
-      for (int i = 0; i < N; ++i) s += q[i] * value(k, page_k_offset<E4, HD>(in, d0 + i));
-      s = wave_sum(s) * a.scale;
-      float vs = 1.f;
-      if constexpr (E4) {
-        s *= scale_value((uint8_t)k[2 * a.pg.side + in]);
-        vs = scale_value((uint8_t)k[2 * a.pg.side + (1 << lg) + in]);
-      }
-      const float mn = fmaxf(m, s), f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
-      const float w = __builtin_amdgcn_exp2f(s - (mn == -INFINITY ? 0.f : mn));
-      l = l * f + w;
-#pragma unroll
-      for (int i = 0; i < N; ++i) y[i] = y[i] * f + w * (vs * value(k + a.pg.side, page_v_offset<E4, HD>(in, d0 + i)));
-      m = mn;
-    }
-    if (whole) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) store_out1(a, b, r, kvh * a.grp + hh, HD, d0 + i, l == 0.f ? 0.f : y[i] / l);
-    } else {
-      const int64_t row = part_row(a, b * a.pg.hkv + kvh, c, qv);
-#pragma unroll
-      for (int i = 0; i < N; ++i) a.part[row * HD + d0 + i] = y[i];
-      if (lane == 0) {
-        a.part[part_rows(a) * HD + row * 2] = m;
-        a.part[part_rows(a) * HD + row * 2 + 1] = l;
-      }
-    }
-  }
-}
-
 template <bool E4, int HD>
 __global__ void __launch_bounds__(kWideWaves * kWave, 3) paged_attn_wide_kernel(PagedAttnArgs a) {
   constexpr int NW = kWideWaves;
@@ -542,11 +487,12 @@ __global__ void __launch_bounds__(kWideWaves * kWave, 3) paged_attn_wide_kernel(
   const int QV = a.R * a.grp, q_block = qb * NW * 32, q0 = q_block + wave * 32, qv = q0 + lane % 32;
   const int block_end = __builtin_amdgcn_readfirstlane(sq.pos + min(a.R - 1, a.by_grp.div(q_block + NW * 32 - 1)) + 1);
   const int p_begin = c * chunk, p_end = min(block_end, p_begin + chunk);
-  // the lane's query's position (-1: none), the tile's first position, the one past its last (0: no queries)
+  // the lane's query's position (-1: none; its column of the products is computed as any other and not stored); the tile's first
+  // position, which all its vectors see, and the one past its last (0: no queries)
   const bool qok = qv < QV;
   const int r = qok ? a.by_grp.div(qv) : 0, hh = qok ? qv - r * a.grp : 0;
   const int qpos = qok ? sq.pos + r : -1;
-  const int lo = __builtin_amdgcn_readfirstlane(q0 + 31 < QV ? sq.pos + a.by_grp.div(q0) : -1);
+  const int first = __builtin_amdgcn_readfirstlane(sq.pos + a.by_grp.div(q0));
   const int tile_end = __builtin_amdgcn_readfirstlane(q0 < QV ? sq.pos + min(a.R - 1, a.by_grp.div(q0 + 31)) + 1 : 0);
   const int lg = a.pg.log_page;
   int page0 = p_begin >> lg, ids = 0;  // the chunk's page ids, 64 at a time across the lanes
@@ -621,6 +567,8 @@ __global__ void __launch_bounds__(kWideWaves * kWave, 3) paged_attn_wide_kernel(
     phase_barrier();  // the step is whole, and the slot of the step before it has been read by every wave
     issue();
   };
+  const int own_rows = max(p_begin, (first + 1) & ~31);  // the step from which some of the tile's vectors see less than others
+  bool wild = false;                                     // the lane has zeroed a value there
   // Step p, at so in the ring.  INNER: every query vector sees the whole of it.
   auto step = [&](auto inner_c, int p, bool ok) {
     constexpr bool inner = decltype(inner_c)::value;
@@ -699,25 +647,41 @@ __global__ void __launch_bounds__(kWideWaves * kWave, 3) paged_attn_wide_kernel(
 #pragma unroll
     for (int g = 0; g < DB; g += 2) {
       bf16x8 v[4];
+      // Positions from p_end on are zeroed: their weights are 0, and 0 times a stale non-finite value would not be.  The tile's own
+      // rows see different parts of a step: what is not finite there is zeroed too, and added behind the loop to those that see it.
+      auto seen = [&](int i) { return (ok ? p_end : 0) - (p + 16 * (i % 2) + 8 * half); };  // positions of operand i
       if constexpr (E4) {
         u32x2 vr[4];
         lds_read8<512>(vr, rd_v + at_step + g * 1024);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = e4m3_frag(vr[i][0], vr[i][1], 1.f);
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (!inner)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const int n = max(0, min(4, seen(i) - 4 * k));
+              uint32_t w = vr[i][k] & (uint32_t)((uint64_t(1) << (8 * n)) - 1);
+              const uint32_t bad = ((w & 0x7f7f7f7fu) + 0x01010101u) & (p >= own_rows ? 0x80808080u : 0u);  // bit 7 of the NaN codes' bytes
+              w &= ~((bad << 1) - (bad >> 7));
+              wild |= bad != 0;
+              vr[i][k] = w;
+            }
+          v[i] = e4m3_frag(vr[i][0], vr[i][1], 1.f);
+        }
       } else {
         u32x4 vr[4];
         lds_read16<2, 2048, 512>(vr, rd_v + at_step + g * 2048);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(bf16x8, vr[i]);
-      }
-      if constexpr (!inner) {  // positions from p_end on zeroed: their weights are 0, and 0 times a stale non-finite value would not be
-#pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int n = (ok ? p_end : 0) - (p + 16 * (i % 2) + 8 * half);
-          u32x4 w = __builtin_bit_cast(u32x4, v[i]);
+          if constexpr (!inner)
 #pragma unroll
-          for (int k = 0; k < 4; ++k) w[k] &= (2 * k < n ? 0xffffu : 0u) | (2 * k + 1 < n ? 0xffff0000u : 0u);
-          v[i] = __builtin_bit_cast(bf16x8, w);
+            for (int k = 0; k < 4; ++k) {
+              uint32_t w = vr[i][k] & ((2 * k < seen(i) ? 0xffffu : 0u) | (2 * k + 1 < seen(i) ? 0xffff0000u : 0u));
+              const uint32_t bad = ((w & 0x7f807f80u) + 0x00800080u) & (p >= own_rows ? 0x80008000u : 0u);  // exponents of all ones
+              w &= ~((bad << 1) - (bad >> 15));
+              wild |= bad != 0;
+              vr[i][k] = w;
+            }
+          v[i] = __builtin_bit_cast(bf16x8, vr[i]);
         }
       }
 #pragma unroll
@@ -729,7 +693,7 @@ __global__ void __launch_bounds__(kWideWaves * kWave, 3) paged_attn_wide_kernel(
   int p = p_begin;
   // the steps that every query vector sees whole, up to a missing page; then the others (one loop after the other: as the two
   // sides of a branch in one loop they would each copy the accumulators)
-  const int p_inner = min(min(lo - 31, p_end - 32), tile_end - 1);
+  const int p_inner = min(min(first - 31, p_end - 32), tile_end - 1);
 #pragma unroll 1
   for (; p <= p_inner && (ok_bits >> (RS - 2) & 1); p += 32) {
     next_step();
@@ -746,20 +710,28 @@ __global__ void __launch_bounds__(kWideWaves * kWave, 3) paged_attn_wide_kernel(
   for (; p < p_end; p += 32) next_step();  // (steps behind the tile's last position: the other waves')
   __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));  // (the loads past the end: they clear LDS)
   if (a.err && bad_page && threadIdx.x == 0) atomicOr(a.err, kErrId);
-  const float lsum = xor32_op(l, [](float x, float y) { return x + y; });
-  // On the diagonal a position may be hidden from some of the query vectors only.  Where a V value there is not finite, the zero
-  // weight of those vectors has not kept it out, and their sums are not finite: then the wave's vectors one by one.
-  if (p_end > (lo < 0 ? sq.pos : lo) + 1) {
-    bool wild = false;
+  // The values that were zeroed: an infinity or NaN, times a positive weight, is itself.  At most 63 positions.
+  if (__any(wild)) {
+#pragma unroll 1
+    for (int p = own_rows; p < min(p_end, tile_end); ++p) {
+      const int id = a.pg.table[(int64_t)sq.row * a.pg.width + (p >> lg)], in = p & in_mask;
+      if ((unsigned)id >= (unsigned)a.pg.n_pages) continue;
+      const char* side = page_head(a.pg, id, kvh) + a.pg.side;
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+      for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) wild |= !__builtin_isfinite(o[db][i]);
-    if (__any(wild)) {
-      wide_one_by_one<E4, HD>(a, sq, b, kvh, q0, c, p_begin, p_end, n_chunks == 1);
-      return;
+        for (int i = 0; i < 16; ++i) {  // dimension 32 db + 8 (i / 4) + 4 half + i % 4
+          const char* at = side + page_v_offset<E4, HD>(in, 32 * db + 8 * (i / 4) + 4 * half + i % 4);
+          float v;
+          if constexpr (E4)
+            v = (*reinterpret_cast<const uint8_t*>(at) & 0x7f) == 0x7f ? NAN : 0.f;
+          else
+            v = bf16_to_f32(*reinterpret_cast<const uint16_t*>(at));
+          if (p <= qpos && !__builtin_isfinite(v)) o[db][i] += v;
+        }
     }
   }
+  const float lsum = xor32_op(l, [](float x, float y) { return x + y; });
   if (!qok) return;
   const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
   const int64_t row = part_row(a, b * hkv + kvh, c, qv);

@@ -1,0 +1,93 @@
+"""Paged attention over values that are not finite, in sequences long enough that the cost shows: what one bad value may cost,
+and that it reaches the rows that see it and no other."""
+import math
+
+import pytest
+import torch
+
+import paged_ref as ref
+from test_gpu_paged import Cache, S, i32, randn  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+def filled(S, dtype, hkv, hd, page, n, seed=1):  # noqa: F811
+    """A cache of one sequence of n positions, its values made on the device; and what it stands for, on the CPU."""
+    c = Cache(S, dtype, hkv, hd, page, [n])
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    kv = torch.randn(1, n, 2 * hkv * hd, generator=g, device="cuda").to(torch.bfloat16)
+    return c, kv
+
+
+def put(c, kv):
+    n = kv.shape[1]
+    c.pool.append(torch.cat([torch.zeros_like(kv[:, :, :c.hkv * c.hd]), kv], 2), c.hkv, c.table, i32([0]))
+    k, v = c.pool.read(c.table, i32([0]), n)
+    return k[0].cpu().double(), v[0].cpu().double()
+
+
+def microseconds(f, n=3):
+    f()
+    best = 1e30
+    for _ in range(n):
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        f()
+        b.record()
+        torch.cuda.synchronize()
+        best = min(best, a.elapsed_time(b) * 1e3)
+    return best
+
+
+LONG = [  # query heads, KV heads, head_dim, rows, positions before them: many query vectors, the sequence in one part
+    (64, 8, 128, 1024, 3000), (16, 16, 64, 2048, 2500)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("hq, hkv, hd, R, at", LONG)
+@pytest.mark.parametrize("side, where", [("v", "last"), ("v", "first"), ("k", "last"), ("v", "middle")])
+def test_one_bad_value_costs_little(S, dtype, hq, hkv, hd, R, at, side, where):  # noqa: F811
+    """The call with a NaN in one row of every KV head's K or V, seen by all rows or hidden from most, takes at most four times
+    the call without (the rows that share products with it are at most those of one 32-vector tile)."""
+    c, kv = filled(S, dtype, hkv, hd, 64, at + R)
+    put(c, kv)
+    q = randn(3, 1, R, hq, hd).to(torch.bfloat16).cuda()
+    lens, out = i32([at]), torch.empty_like(q)
+    ws = c.pool.attention_workspace(1, R, hq, at + R)
+    call = lambda: c.pool.attention(q, c.table, lens, max_len=at + R, out=out, ws=ws)  # noqa: E731
+    clean = microseconds(call)
+    pos = {"last": at + R - 1, "first": 0, "middle": at + R // 2 + 1}[where]
+    rows = kv[0, pos].view(2, hkv, hd)
+    rows[0 if side == "k" else 1, :, 3] = math.nan
+    put(c, kv)
+    spoilt = microseconds(call)
+    assert spoilt <= 4 * clean, (clean, spoilt)
+    sees = torch.arange(at, at + R) >= pos
+    o = out[0].cpu()
+    assert torch.isfinite(o[~sees].float()).all()
+    if sees.any():
+        dims = slice(3, 4) if side == "v" and dtype == "bf16" else slice(None)
+        assert torch.isnan(o[sees][..., dims]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("hq, hkv, hd, R, at", LONG)
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_a_bad_value_on_the_diagonal_of_a_long_part(S, dtype, hq, hkv, hd, R, at, bad):  # noqa: F811
+    c, kv = filled(S, dtype, hkv, hd, 64, at + R, seed=2)
+    r0 = R // 2 + 5
+    kv[0, at + r0].view(2, hkv, hd)[1, 2, 7] = bad
+    k, v = put(c, kv)
+    q = randn(4, 1, R, hq, hd).to(torch.bfloat16)
+    got = c.pool.attention(q.cuda(), c.table, i32([at]))[0].cpu().double()
+    grp = hq // hkv
+    for r in (0, 1, r0 - 33, r0 - 2, r0 - 1, r0, r0 + 1, r0 + 40, R - 1):
+        want, tol = ref.attention(q[0, r:r + 1].double(), k, v, at + r, hd ** -0.5)
+        off, w, t = (got[r:r + 1] - want).abs()[0], want[0], tol[0]
+        ok = torch.ones(hq, hd, dtype=torch.bool)
+        if r >= r0:
+            heads = slice(2 * grp, 3 * grp)
+            dims = slice(None) if dtype == "e4m3" else slice(7, 8)
+            ok[heads, dims] = False
+            assert not torch.isfinite(got[r, heads, dims]).any(), r
+        assert torch.isfinite(w[ok]).all() and (off <= t)[ok].all(), r
