@@ -600,10 +600,11 @@ class KVCache:
         _check(lib().sdd_kv_commit(self.handle, _ptr(seq_ids), seq_ids.numel(), _ptr(accepted_len),
                                    _ptr(next_token), _stream(stream)))
 
-    def workspace(self, max_rows: int) -> torch.Tensor:
+    def workspace(self, max_rows: int, stream=None) -> torch.Tensor:
         """Workspace for calls of up to max_rows rows on this cache (Model.workspace serves contiguous caches as well)."""
-        ws = torch.empty(_size_out(lib().sdd_kv_workspace_bytes, self.handle, max_rows), dtype=torch.uint8, device=self.buf.device)
-        workspace_init(ws)
+        with torch.cuda.stream(stream):  # (None: the current one)
+            ws = torch.empty(_size_out(lib().sdd_kv_workspace_bytes, self.handle, max_rows), dtype=torch.uint8, device=self.buf.device)
+            workspace_init(ws)
         return ws
 
 
@@ -611,7 +612,8 @@ class PagedKVCache(KVCache):
     """A KV cache in pages (sdd_paged_kv_create): memory for n_pages pages a layer, shared out to sequences as they grow.
 
     `table` (int32 [max_batch, width], device) may be written by the caller; assign() and release() keep it from a free
-    list on the host."""
+    list on the host.  With `stream`, the constructor, assign() and release() write it on that stream, as the calls that read it
+    run on theirs; a cache used on several streams is ordered between them by the caller."""
 
     def __init__(self, model: Model, max_batch: int, max_len: int, n_pages: int, page_size: int = 64, dtype: str = "bf16",
                  stream=None):
@@ -621,16 +623,17 @@ class PagedKVCache(KVCache):
         code = BF16 if dtype == "bf16" else E4M3
         n = _size_out(lib().sdd_paged_kv_bytes, C.byref(model.cfg), max_batch, max_len, page_size, code, n_pages)
         dev = model.buf.device
-        self.buf = torch.empty(n, dtype=torch.uint8, device=dev)
-        self.table = torch.full((max_batch, -(-max_len // page_size)), -1, dtype=torch.int32, device=dev)
         h = C.c_void_p()
-        _check(lib().sdd_paged_kv_create(model.handle, max_batch, max_len, page_size, code, n_pages, _ptr(self.table),
-                                         _ptr(self.buf), n, _stream(stream), C.byref(h)))
+        with torch.cuda.stream(stream):  # (None: the current one)
+            self.buf = torch.empty(n, dtype=torch.uint8, device=dev)
+            self.table = torch.full((max_batch, -(-max_len // page_size)), -1, dtype=torch.int32, device=dev)
+            _check(lib().sdd_paged_kv_create(model.handle, max_batch, max_len, page_size, code, n_pages, _ptr(self.table),
+                                             _ptr(self.buf), n, _stream(), C.byref(h)))
         self.handle = h
         self.free = list(range(n_pages - 1, -1, -1))
         self.held = [[] for _ in range(max_batch)]
 
-    def assign(self, seq: int, positions: int):
+    def assign(self, seq: int, positions: int, stream=None):
         """Gives sequence seq the pages that `positions` positions need (those it holds stay); raises when none are free."""
         _need(0 <= seq < self.max_batch, f"bad seq {seq}")
         have, want = len(self.held[seq]), -(-positions // self.page_size)
@@ -641,14 +644,16 @@ class PagedKVCache(KVCache):
             raise SDDError(ECAPACITY, f"{want - have} pages needed, {len(self.free)} free")
         new = [self.free.pop() for _ in range(want - have)]
         self.held[seq] += new
-        self.table[seq, have:want] = torch.tensor(new, dtype=torch.int32, device=self.table.device)
+        with torch.cuda.stream(stream):
+            self.table[seq, have:want] = torch.tensor(new, dtype=torch.int32, device=self.table.device)
 
-    def release(self, seq: int):
+    def release(self, seq: int, stream=None):
         """Takes all pages back from sequence seq."""
         _need(0 <= seq < self.max_batch, f"bad seq {seq}")
         self.free += reversed(self.held[seq])
         self.held[seq] = []
-        self.table[seq] = -1
+        with torch.cuda.stream(stream):
+            self.table[seq] = -1
 
     def pool(self, layer: int) -> PagePool:
         """One layer's pages (for PagePool.read)."""
