@@ -1865,6 +1865,7 @@ extern "C" int sdd_kv_workspace_bytes(const sdd_kv* kv, int max_rows, size_t* by
   SDD_REQUIRE(max_rows > 0 && max_rows <= 65536, "bad max_rows %d", max_rows);
   size_t paged = 0;
   if (kv->page_size) {
+    max_rows = std::max(max_rows, 16);  // (a prefill takes 16 rows at least)
     size_t part = 0;  // the largest partial results of any nb blocks of R rows, nb R <= max_rows
     for (int nb = 1; nb <= std::min(kv->max_batch, max_rows); ++nb) part = std::max(part, paged_part(kv, nb, max_rows / nb));
     paged = paged_ws(kv, 1, max_rows, part).total + 256;

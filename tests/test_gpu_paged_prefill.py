@@ -1,0 +1,34 @@
+"""Prefill into a paged cache: what its workspace decides, and what it does not."""
+import pytest
+
+import workloads as W
+from gpu_helpers import to_dev_i32
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = {"hd64": W.ModelShape(2, 512, 8, 2, 64, 1024, 2048, 1e-6, 1e6, True, "bf16"),
+          "hd128": W.ModelShape(2, 384, 7, 1, 128, 1088, 2176, 1e-6, 1e6, False, "bf16"),
+          "many": W.ModelShape(2, 512, 16, 8, 64, 1024, 2048, 1e-6, 1e6, True, "bf16")}
+
+
+@pytest.fixture(scope="module")
+def S():
+    from paper_2608_14787_amd import sdd
+    assert sdd.device_ok(), "needs a gfx950 device"
+    return sdd
+
+
+@pytest.mark.parametrize("rows", [1, 2, 9, 15, 16])
+@pytest.mark.parametrize("max_len", [600, 40000])
+def test_a_workspace_for_few_rows_serves_prefill(S, rows, max_len):
+    """As the contiguous cache's does: a decode step's workspace is enough to prefill with."""
+    shape = SHAPES["many"]
+    m = S.Model(shape)
+    m.init_random(22, W.WEIGHT_SIGMA)
+    toks = to_dev_i32(W.prompt(3, 100, shape.vocab))
+    kv = S.PagedKVCache(m, 1, max_len, 8, 32)
+    kv.assign(0, 128)
+    kv.prefill(0, toks, kv.workspace(rows))
+    cv = S.KVCache(m, 1, max_len)
+    cv.prefill(0, toks, cv.workspace(rows))
+    assert kv.state()[2] == 0 and kv.state()[0][0] == 99 == cv.state()[0][0]
