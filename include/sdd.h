@@ -169,11 +169,12 @@ int sdd_workspace_init(void* ws, size_t bytes, sdd_stream_t stream);
  * 0..n-2, sets len = n-1 and pending = tokens[n-1].  The prompt is processed
  * in row chunks, as few as the workspace's bytes hold (bf16: at most 4096 rows;
  * a larger workspace makes them fewer and faster).  Bits: rows go in passes of
- * the largest of 256, 128, 64, 32, 16 rows whose sdd_workspace_bytes the
- * workspace holds; the rows of a pass of more than 64 rows and those of a
+ * the largest of 256, 128, 64, 32, 16 rows whose sdd_workspace_bytes (and,
+ * over a paged cache, whose projections in fp32) the workspace holds; the rows of a pass of more than 64 rows and those of a
  * smaller one (a small workspace's, or the last pass) are summed in two
  * orders (sdd_verify_block, below), and nothing else of the chunks or the
- * workspace shows in the cache: workspaces for 256 rows or more give the same.
+ * workspace shows in the cache, paged or not: workspaces for 256 rows or more
+ * give the same.
  * The verifier KV cache is this library's reading of the verify call: the
  * paper's own verifier keeps no cache and recomputes the whole sequence every
  * call (Appendix "Evaluation and Throughput"; sdd_verify_full is that mode).
@@ -286,9 +287,10 @@ int sdd_rope_table(float* table, int max_pos, int head_dim, float theta, sdd_str
  * missing ones (ids outside [0, n_pages)) set sticky bit2 and are not seen.
  * Results equal the contiguous cache's up to rounding: q, k and v pass through
  * fp32 rows, norms and rotation being a launch of their own (sdd_paged_append),
- * and the attention (sdd_paged_attention) adds in its own order, which with
- * many query vectors counts the call's sequences too; SDD_E4M3 pages round K
- * and V to 8 bits besides.  Errors: SDD_EINVAL, SDD_ENOMEM,
+ * and the attention (sdd_paged_attention) adds in its own order, which in
+ * verify calls follows the call's row count and with many query vectors its
+ * sequences too, in prefills neither; SDD_E4M3 pages round K and V to 8 bits
+ * besides.  Errors: SDD_EINVAL, SDD_ENOMEM,
  * SDD_EUNSUPPORTED (fp32 model). */
 int sdd_paged_kv_bytes(const sdd_model_config* cfg, int max_batch, int max_len, int page_size, int dtype, int n_pages,
                        size_t* bytes);

@@ -1327,11 +1327,13 @@ static PagedWs paged_ws(const sdd_kv* kv, int nb, int R, size_t part_bytes) {
 static size_t paged_part(const sdd_kv* kv, int nb, int R) {
   return paged_attn_workspace(paged_attn_shape(kv, nb, R), kv->m->cfg.head_dim);
 }
-// What a call of nb blocks of up to R rows needs; 0 for a contiguous cache.
-static size_t paged_bytes(const sdd_kv* kv, int nb, int R) { return kv->page_size ? paged_ws(kv, nb, R, paged_part(kv, nb, R)).total : 0; }
+// What a call of nb blocks of up to R rows needs; 0 for a contiguous cache.  A prefill's chunks have no partial results.
+static size_t paged_bytes(const sdd_kv* kv, int nb, int R, bool prefill) {
+  return kv->page_size ? paged_ws(kv, nb, R, prefill ? 0 : paged_part(kv, nb, R)).total : 0;
+}
 // What a prefill's chunks of at most R rows leave of a workspace for their layout: a paged cache's part sits at its end.
 static size_t prefill_room(const sdd_kv* kv, int R, size_t bytes) {
-  const size_t p = paged_bytes(kv, 1, R);
+  const size_t p = paged_bytes(kv, 1, R, true);
   return p == 0 ? bytes : p < bytes ? (bytes - p) / 256 * 256 : 0;
 }
 static sdd_pages kv_pages(const sdd_kv* kv, int layer) {
@@ -1340,7 +1342,7 @@ static sdd_pages kv_pages(const sdd_kv* kv, int layer) {
 }
 
 // Head norms, rotation and cache rows of a layer's projection, then its attention, over a paged cache.
-static int paged_layer(CallCtx& cx, int layer, int nb, int R) {
+static int paged_layer(CallCtx& cx, int layer, int nb, int R, bool prefill) {
   sdd_kv* kv = cx.kv;
   const sdd_model* m = cx.m;
   const sdd_model_config& c = m->cfg;
@@ -1373,6 +1375,7 @@ static int paged_layer(CallCtx& cx, int layer, int nb, int R) {
   PagedAttnArgs t = paged_attn_shape(kv, nb, R);
   t.pg = d;
   t.rows = a.rows;
+  t.uncut = prefill;
   t.q = a.q_out;
   t.out = reinterpret_cast<uint16_t*>(cx.ws + cx.L.ao);
   t.frag = 1;
@@ -1581,7 +1584,7 @@ static int forward_rows(CallCtx& cx, int nb, int R, float* logits, int32_t* argm
         a.amax_v = reinterpret_cast<float*>(ws + cx.paged + p.amax_v);
         a.amax_i = reinterpret_cast<int*>(ws + cx.paged + p.amax_i);
         if ((rc = run_gemm(cx, EPI_ROWS, PROF_GEMM_QKV, Ly.qkv, hq + 2 * hk, (int)d, xa, a, M, m->ng_qkv, tp.qkv, &nx))) return rc;
-        if ((rc = paged_layer(cx, l, nb, R))) return rc;
+        if ((rc = paged_layer(cx, l, nb, R, prefill))) return rc;
       } else if ((rc = run_gemm(cx, EPI_QKV, PROF_GEMM_QKV, Ly.qkv, hq + 2 * hk, (int)d, xa, a, M, m->ng_qkv, tp.qkv, &nx))) return rc;
     }
     // attention
@@ -1903,7 +1906,8 @@ extern "C" int sdd_workspace_bytes(const sdd_model* m, int max_rows, size_t* byt
   return SDD_OK;
 }
 
-static int make_ctx(CallCtx& cx, sdd_model* m, sdd_kv* kv, void* ws, size_t ws_bytes, int nb, int R, hipStream_t st) {
+static int make_ctx(CallCtx& cx, sdd_model* m, sdd_kv* kv, void* ws, size_t ws_bytes, int nb, int R, hipStream_t st,
+                    bool prefill = false) {
   const int rows = nb * R;
   SDD_REQUIRE(m && kv && ws, "NULL pointer");
   SDD_REQUIRE(kv->m == m, "KV cache belongs to another model");
@@ -1914,7 +1918,7 @@ static int make_ctx(CallCtx& cx, sdd_model* m, sdd_kv* kv, void* ws, size_t ws_b
   cx.L = ws_layout(m, rows);
   cx.st = st;
   cx.paged = cx.L.total;
-  const size_t need = cx.L.total + paged_bytes(kv, nb, R);
+  const size_t need = cx.L.total + paged_bytes(kv, nb, R, prefill);
   if (need > ws_bytes)
     return fail(SDD_ECAPACITY, "workspace of %zu bytes is too small for %d rows (%zu needed)", ws_bytes, rows, need);
   return SDD_OK;
@@ -1990,7 +1994,7 @@ extern "C" int sdd_kv_prefill(sdd_model* m, sdd_kv* kv, int seq, const int32_t* 
   for (int i = 0, c0 = 0; c0 < n - 1; ++i) {
     const int rows = c0 < plan.main ? plan.begin(i + 1) - c0 : std::min(plan.rest, n - 1 - c0);
     CallCtx cx;
-    int rc = make_ctx(cx, m, kv, ws, ws_bytes, 1, 16, st);
+    int rc = make_ctx(cx, m, kv, ws, ws_bytes, 1, 16, st, true);
     if (rc) return rc;
     cx.paged = prefill_room(kv, plan.layout, ws_bytes);
     cx.L = prefill_layout(m, plan.layout, cx.paged);

@@ -100,6 +100,9 @@ struct PagedAttnArgs {
   uint16_t* out;        // the same, or fragment-major rows (frag)
   int frag;
   int B, R, hq, grp, max_len;
+  // A chunk of a prompt, whose cut is the workspace's affair and may not show in the results: the many-vector kernel with every
+  // sequence in one part, where a vector's sums depend on its own position and the cache alone.  No partial results.
+  bool uncut;
   // |scale| of the scores, times log2(e) (1 for a scale of 0); the queries' bits are masked and flipped for its sign
   float scale;
   uint32_t q_and, q_xor;
@@ -120,7 +123,7 @@ struct PagedAttnArgs {
   FastDiv by_grp, by_hkv, by_b, by_qv;
   float* part;  // partial results
 };
-// Bytes of partial results that a call needs (B, R, hq, grp, max_len and pg.hkv are read).
+// Bytes of partial results that a call needs that is not `uncut` (B, R, hq, grp, max_len and pg.hkv are read).
 size_t paged_attn_workspace(PagedAttnArgs a, int head_dim);
 int launch_paged_attn(PagedAttnArgs a, int head_dim, bool e4, hipStream_t st);
 

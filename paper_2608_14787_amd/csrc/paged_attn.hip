@@ -609,8 +609,10 @@ __global__ void __launch_bounds__(kWideWaves * kWave, 3) paged_attn_wide_kernel(
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, sv[i]);
     top = xor32_op(top, [](float x, float y) { return fmaxf(x, y); });
-    if (__any(top * a.scale > m_far)) {
-      const float mn = fmaxf(m, top);
+    // (each vector's reference moves by its own scores: what it gives does not depend on the others of its tile)
+    const bool far = top * a.scale > m_far;
+    if (__any(far)) {
+      const float mn = far ? fmaxf(m, top) : m;
       const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * a.scale);
       l *= f;
 #pragma unroll
@@ -880,7 +882,7 @@ void launch_t(const PagedAttnArgs& a, hipStream_t st) {
 static void cut_call(PagedAttnArgs* a) {
   const int QV = a->R * a->grp;
   const int64_t blocks = ceil_div(QV, 32 * kWideWaves);
-  const bool all = QV > 16 && a->B * a->pg.hkv * blocks >= kWideBlocks;
+  const bool all = a->uncut || (QV > 16 && a->B * a->pg.hkv * blocks >= kWideBlocks);
   a->many_from = all ? 0 : QV >= kManyVectors ? kManyFrom : QV >= kSomeVectors ? kSomeFrom : INT32_MAX;
   auto cut = [&](int64_t qtiles, int64_t items, int min_chunk, int whole, int longest) {
     PagedAttnArgs::Cut t{};
@@ -893,7 +895,7 @@ static void cut_call(PagedAttnArgs* a) {
   };
   const int64_t tiles = ceil_div(QV, 16);
   a->few = cut(tiles, kTargetItems, kMinChunk, a->pg.hkv * tiles >= kManyItems ? kWholeMany : kWhole, std::min(a->max_len, a->many_from));
-  a->many = cut(blocks, kWideItems / (all ? std::max(a->B, kWideFew) : kWideFew), kWideChunk, kWideChunk, a->max_len);
+  a->many = cut(blocks, a->uncut ? 1 : kWideItems / (all ? std::max(a->B, kWideFew) : kWideFew), kWideChunk, kWideChunk, a->max_len);
   a->splits = std::max(a->many_from > 0 ? a->few.splits : 1, a->many_from <= a->max_len ? a->many.splits : 1);
   a->qpad = (int)align_up(QV, 16);
 }

@@ -1,5 +1,6 @@
 """Prefill into a paged cache: what its workspace decides, and what it does not."""
 import pytest
+import torch
 
 import workloads as W
 from gpu_helpers import to_dev_i32
@@ -32,3 +33,27 @@ def test_a_workspace_for_few_rows_serves_prefill(S, rows, max_len):
     cv = S.KVCache(m, 1, max_len)
     cv.prefill(0, toks, cv.workspace(rows))
     assert kv.state()[2] == 0 and kv.state()[0][0] == 99 == cv.state()[0][0]
+def cached(S, m, dtype, toks, ws_rows):
+    """K/V of the prompt's positions in every layer, after a prefill with a workspace for ws_rows rows."""
+    n = len(toks)
+    kv = S.PagedKVCache(m, 1, n + 8, n // 32 + 2, 32, dtype)
+    kv.assign(0, n)
+    kv.prefill(0, to_dev_i32(toks), kv.workspace(ws_rows))
+    assert kv.state()[2] == 0
+    return [kv.pool(layer).read(kv.table, to_dev_i32([0]), n - 1) for layer in range(2)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("name", list(SHAPES))
+@pytest.mark.parametrize("n", [130, 402, 1000, 2861])
+def test_bits_do_not_depend_on_the_workspace(S, name, dtype, n):
+    """Workspaces for 256 rows or more leave the same bits in the pages, however many chunks they make of the prompt."""
+    m = S.Model(SHAPES[name])
+    m.init_random(21, W.WEIGHT_SIGMA)
+    toks = W.prompt(n, n, SHAPES[name].vocab)
+    want = cached(S, m, dtype, toks, 256)
+    for rows in (300, 512, 1024, 4096):
+        for (k, v), (wk, wv) in zip(cached(S, m, dtype, toks, rows), want):
+            assert torch.equal(k, wk) and torch.equal(v, wv), rows
+
+
