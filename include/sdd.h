@@ -331,7 +331,8 @@ int sdd_paged_attention_workspace_bytes(const sdd_pages* pg, int B, int R, int n
  * step, R = gamma + 1 a block's verification, a larger R a chunk of a prompt.
  * max_len: no sequence's len + R is larger (a longer one is refused); the
  * host's bound sizes the launch, so that a captured call serves all lengths up
- * to it.  A row that sees nothing (its pages are invalid) gives zeros.  Sums and
+ * to it.  A row that sees nothing (its pages are invalid) gives zeros, one whose
+ * scores pass fp32's range NaN.  Sums and
  * softmax statistics are fp32 and in a fixed order: results are
  * bit-reproducible and do not depend on what the call's other sequences hold;
  * below a B * n_kv_heads * ceil(R * n_q_heads / n_kv_heads / 128) of 160 not on B

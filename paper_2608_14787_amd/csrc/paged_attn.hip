@@ -621,6 +621,7 @@ __global__ void __launch_bounds__(kWideWaves * kWave, 3) paged_attn_wide_kernel(
         for (int i = 0; i < 16; ++i) o[db][i] *= f;
       m = mn;
       ref = m == -INFINITY ? 0.f : -m * a.scale;
+      ref = __builtin_isfinite(ref) ? ref : NAN;  // (scores past the range have no weights; minus infinity would make all of them 0)
       m_far = m == -INFINITY ? -INFINITY : kFar - ref;
     }
     float e[16], sum = 0.f;

@@ -91,3 +91,18 @@ def test_a_bad_value_on_the_diagonal_of_a_long_part(S, dtype, hq, hkv, hd, R, at
             ok[heads, dims] = False
             assert not torch.isfinite(got[r, heads, dims]).any(), r
         assert torch.isfinite(w[ok]).all() and (off <= t)[ok].all(), r
+
+
+@pytest.mark.parametrize("hq, hkv, B, R", [(16, 8, 1, 1), (16, 8, 1, 33), (16, 8, 1, 1400), (80, 40, 4, 20)])
+def test_scores_past_the_range(S, hq, hkv, B, R):  # noqa: F811
+    """A score that passes fp32's range is no weight of 0: the row's result is the softmax's (that position alone) or NaN."""
+    hd, at = 64, 40
+    c = Cache(S, "bf16", hkv, hd, 32, [at + R] * B)
+    k, v = torch.zeros(B, at + R, hkv, hd, dtype=torch.float64), randn(2, 1, at + R, hkv, hd).repeat(B, 1, 1, 1)
+    k[:, 7, :, 0] = 2e19
+    k, v = c.put(k, v, [0] * B)
+    q = torch.zeros(B, R, hq, hd, dtype=torch.bfloat16)
+    q[..., 0] = 1.6e19  # 3.2e38, and more than fp32 holds once log2 e is in it
+    got = c.pool.attention(q.cuda(), c.table, i32([at] * B), scale=1.0).cpu().double()
+    want = v[0, 7].repeat_interleave(hq // hkv, 0).expand(B, R, hq, hd)
+    assert (torch.isnan(got) | ((got - want).abs() <= 2.0 ** -8 * want.abs())).all()

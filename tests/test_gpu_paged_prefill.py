@@ -33,6 +33,8 @@ def test_a_workspace_for_few_rows_serves_prefill(S, rows, max_len):
     cv = S.KVCache(m, 1, max_len)
     cv.prefill(0, toks, cv.workspace(rows))
     assert kv.state()[2] == 0 and kv.state()[0][0] == 99 == cv.state()[0][0]
+
+
 def cached(S, m, dtype, toks, ws_rows):
     """K/V of the prompt's positions in every layer, after a prefill with a workspace for ws_rows rows."""
     n = len(toks)
@@ -55,5 +57,3 @@ def test_bits_do_not_depend_on_the_workspace(S, name, dtype, n):
     for rows in (300, 512, 1024, 4096):
         for (k, v), (wk, wv) in zip(cached(S, m, dtype, toks, rows), want):
             assert torch.equal(k, wk) and torch.equal(v, wv), rows
-
-
