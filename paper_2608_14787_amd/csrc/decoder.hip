@@ -1749,11 +1749,14 @@ static int launch_embed(CallCtx& cx, EmbedArgs e, int M) {
 
 using namespace sdd;
 
+// Lengths, pending tokens and the error word.
+static size_t kv_header_bytes(int max_batch) { return align_up((2 * (size_t)max_batch + 1) * 4, 256); }
+
 extern "C" int sdd_kv_bytes(const sdd_model_config* cfg, int max_batch, int max_len, size_t* bytes) {
   SDD_REQUIRE(cfg && bytes, "NULL pointer");
   SDD_REQUIRE(max_batch > 0 && max_len > 0, "bad max_batch/max_len");
   const int es = cfg->dtype == SDD_BF16 ? 2 : 4;
-  size_t hdr = align_up((size_t)(2 * max_batch + 1) * 4, 256);
+  size_t hdr = kv_header_bytes(max_batch);
   size_t rope = align_up((size_t)max_len * cfg->head_dim * 4, 256);
   size_t per_layer = align_up((size_t)max_batch * cfg->n_kv_heads * kv_ld(max_len) * cfg->head_dim * es, 256);
   *bytes = hdr + rope + 2 * per_layer * (size_t)std::max(1, cfg->n_layers);
@@ -1779,7 +1782,7 @@ extern "C" int sdd_kv_create(sdd_model* m, int max_batch, int max_len, void* buf
   kv->len = reinterpret_cast<int32_t*>(kv->base);
   kv->pending = kv->len + max_batch;
   kv->err = kv->pending + max_batch;
-  size_t hdr = align_up((size_t)(2 * max_batch + 1) * 4, 256);
+  size_t hdr = kv_header_bytes(max_batch);
   kv->rope = reinterpret_cast<float*>(kv->base + hdr);
   size_t rope = align_up((size_t)max_len * c.head_dim * 4, 256);
   kv->ld = kv_ld(max_len);
@@ -1808,8 +1811,9 @@ extern "C" int sdd_paged_kv_bytes(const sdd_model_config* cfg, int max_batch, in
   size_t layer = 0;
   int rc = sdd_pages_bytes(&pg, &layer);
   if (rc) return rc;
-  *bytes = align_up((size_t)(2 * max_batch + 1) * 4, 256) + align_up((size_t)max_len * cfg->head_dim * 4, 256) +
-           align_up(layer, 256) * (size_t)std::max(1, cfg->n_layers);
+  const size_t layers = (size_t)std::max(1, cfg->n_layers), small = kv_header_bytes(max_batch) + align_up((size_t)max_len * cfg->head_dim * 4, 256);
+  SDD_REQUIRE(layer <= ((size_t)INT64_MAX - small) / layers - 256, "%d pages in each of %d layers are past the address range", n_pages, cfg->n_layers);
+  *bytes = small + align_up(layer, 256) * layers;
   return SDD_OK;
 }
 
@@ -1832,7 +1836,7 @@ extern "C" int sdd_paged_kv_create(sdd_model* m, int max_batch, int max_len, int
   kv->len = reinterpret_cast<int32_t*>(kv->base);
   kv->pending = kv->len + max_batch;
   kv->err = kv->pending + max_batch;
-  const size_t hdr = align_up((size_t)(2 * max_batch + 1) * 4, 256);
+  const size_t hdr = kv_header_bytes(max_batch);
   kv->rope = reinterpret_cast<float*>(kv->base + hdr);
   kv->k = kv->base + hdr + align_up((size_t)max_len * c.head_dim * 4, 256);
   kv->page_size = page_size;
