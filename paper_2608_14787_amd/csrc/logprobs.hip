@@ -462,12 +462,17 @@ int launch(Job j, int64_t rows, hipStream_t st) {
   j.C = (int)ceil_div(vectors, j.chunk);
   const dim3 grid((unsigned)(rows * j.C));
   prof_begin(PROF_LOGP, st);
-  if (j.V < VEC)
-    hipLaunchKernelGGL((logprobs_kernel<T, true, 1>), grid, dim3(kThreads), 0, st, j);
-  else if (j.n_top > 0)
-    hipLaunchKernelGGL((logprobs_kernel<T, true, VEC>), grid, dim3(kThreads), 0, st, j);
+  auto with = [&](auto top) {
+    constexpr bool TOP = decltype(top)::value;
+    if (j.V < VEC)
+      hipLaunchKernelGGL((logprobs_kernel<T, TOP, 1>), grid, dim3(kThreads), 0, st, j);
+    else
+      hipLaunchKernelGGL((logprobs_kernel<T, TOP, VEC>), grid, dim3(kThreads), 0, st, j);
+  };
+  if (j.n_top > 0)
+    with(std::true_type());
   else
-    hipLaunchKernelGGL((logprobs_kernel<T, false, VEC>), grid, dim3(kThreads), 0, st, j);
+    with(std::false_type());
   prof_end(PROF_LOGP, st);
   return check_launch("logprobs_kernel");
 }
