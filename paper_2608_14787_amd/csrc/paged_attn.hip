@@ -11,6 +11,10 @@
 // of them a workgroup, sharing each step through a ring in LDS.  A third joins the chunks' results in chunk order.  The cut of
 // a sequence into chunks depends on its own length and the call's shape, not on what the others hold.
 //
+// The rows of a tile see different parts of its last steps, where a hidden position's weight of 0 does not keep out a V value that
+// is not finite.  Both kernels zero such values there and add them behind the loop to the vectors that see them: 1024 rows of 64/8
+// heads behind 3000 positions 143 us, with a NaN in the last position 151, in every row 175; 33 rows behind 1000 17 and 28.
+//
 // Bound, for 64/8 heads of 128: with few rows the stream of K and V (32 ragged sequences in bf16 52 us, 5.5 TB/s; 229000
 // positions in e4m3 80 us, 5.9 TB/s) or, short, the chain of page id, loads, products and joins (one row, 513 positions 6.7 us);
 // with many the softmax's instructions beside the products (1024 rows behind 1055 positions 65 us, 0.81 PFLOP/s; 4096 rows
@@ -118,6 +122,27 @@ __device__ inline uint4 load_q(const PagedAttnArgs& a, const uint16_t* q) {
 }
 __device__ inline uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
+// Adds what is not finite among the V values of positions p .. p + 7 (a group of a step) and of dimension dim to y, as far as a
+// vector at position qpos sees them: an infinity or NaN, times a positive weight, is itself.
+template <bool E4, int HD>
+__device__ inline float add_wild(const PagedAttnArgs& a, int page, int kvh, int p, int dim, int qpos, float y) {
+  const char* v = page_head(a.pg, page, kvh) + a.pg.side + page_v_offset<E4, HD>(p & ((1 << a.pg.log_page) - 1), dim);
+  if constexpr (E4) {
+    const uint2 w = *reinterpret_cast<const uint2*>(v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (p + i <= qpos && ((i < 4 ? w.x : w.y) >> (8 * (i % 4)) & 0x7f) == 0x7f) y = NAN;
+  } else {
+    const uint4 w = load16(v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float x = bf16_to_f32((uint16_t)((i / 2 == 0 ? w.x : i / 2 == 1 ? w.y : i / 2 == 2 ? w.z : w.w) >> (16 * (i % 2))));
+      if (p + i <= qpos && !__builtin_isfinite(x)) y += x;
+    }
+  }
+  return y;
+}
+
 template <bool E4, int HD, bool ONCE>
 __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a) {
   constexpr int KK = HD / 32, DB = HD / 16;
@@ -210,39 +235,47 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
   };
 
   f32x4 o[DB];
-  float m, l;        // (m: of the scores before the scale)
-  float ref, m_far;  // -m scale (0 for no m), and the score from which m moves
-  auto reset = [&]() {
 #pragma unroll
-    for (int db = 0; db < DB; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
-    m = -INFINITY, l = 0.f, ref = 0.f, m_far = -INFINITY;
-  };
-  reset();
-  // V operand of 16 dimensions, positions outside `mask` (a bit for each of the lane's 8) zeroed: their weights are 0, and 0
-  // times a stale or foreign non-finite value would not be
-  auto v_frag = [&](int db, uint32_t mask) {
+  for (int db = 0; db < DB; ++db) o[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;        // (m: of the scores before the scale)
+  float ref = 0.f, m_far = -INFINITY;  // -m scale (0 for no m), and the score from which m moves
+  // the step from which some of the tile's vectors see less than others (a single row's: none)
+  const int own_rows = tile_end == lo + 1 ? INT32_MAX : max(p_begin, (lo + 1) & ~31);
+  bool wild = false;                                  // the lane has zeroed a value there
+  // V operand of 16 dimensions.  Of a step that not every vector sees whole, positions outside `mask` (a bit for each of the
+  // lane's 8) are zeroed: their weights are 0, and 0 times a stale or foreign non-finite value would not be.  So is what is not
+  // finite among the tile's own rows, to be added behind the loop.
+  auto v_frag = [&](auto part, auto own, int db, uint32_t mask) {
+    constexpr bool PART = decltype(part)::value, OWN = decltype(own)::value;
     if constexpr (E4) {
-      uint32_t x = word(vr[db / 2], db % 2 * 2), y = word(vr[db / 2], db % 2 * 2 + 1);
-      if (mask != 255) {  // (lane by lane: no product in here)
-        uint32_t mx = 0, my = 0;
+      uint32_t w[2] = {word(vr[db / 2], db % 2 * 2), word(vr[db / 2], db % 2 * 2 + 1)};
+      if constexpr (PART) {
+        uint32_t keep[2] = {0, 0};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          mx |= (mask >> i & 1) ? 0xffu << (8 * i) : 0u;
-          my |= (mask >> (4 + i) & 1) ? 0xffu << (8 * i) : 0u;
+        for (int i = 0; i < 8; ++i) keep[i / 4] |= (mask >> i & 1) ? 0xffu << (8 * (i % 4)) : 0u;
+        w[0] &= keep[0], w[1] &= keep[1];
+      }
+      if constexpr (OWN)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const uint32_t bad = ((w[k] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;  // (the NaN codes)
+          w[k] &= ~((bad << 1) - (bad >> 7));
+          wild |= bad != 0;
         }
-        x &= mx, y &= my;
-      }
-      return e4m3_frag(x, y, 1.f);
+      return e4m3_frag(w[0], w[1], 1.f);
     } else {
-      uint4 w = vr[db];
-      if (mask != 255) {
-        uint32_t k[4];
+      uint32_t w[4] = {vr[db].x, vr[db].y, vr[db].z, vr[db].w};
+      if constexpr (PART)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          k[i] = ((mask >> (2 * i) & 1) ? 0xffffu : 0u) | ((mask >> (2 * i + 1) & 1) ? 0xffff0000u : 0u);
-        w.x &= k[0], w.y &= k[1], w.z &= k[2], w.w &= k[3];
-      }
-      return __builtin_bit_cast(bf16x8, w);
+        for (int k = 0; k < 4; ++k) w[k] &= ((mask >> (2 * k) & 1) ? 0xffffu : 0u) | ((mask >> (2 * k + 1) & 1) ? 0xffff0000u : 0u);
+      if constexpr (OWN)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t bad = ((w[k] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;  // (exponents of all ones)
+          w[k] &= ~((bad << 1) - (bad >> 15));
+          wild |= bad != 0;
+        }
+      return __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
     }
   };
   auto below = [&](int p, int end) {  // mask of the lane's positions of step p that lie before end
@@ -252,9 +285,8 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
   constexpr int kStride = 32 * kWaves;
   const int p0 = p_begin + 32 * wave;
   Place pl;
-  // Step p, whose place is pl; issues the next one's loads.  ONE: every query vector's product by itself, V zeroed where it is
-  // hidden from it.
-  auto step = [&](auto one, int p) {
+  // Step p, whose place is pl; issues the next one's loads.
+  auto step = [&](int p) {
     const bool ok = pl.ok;
     f32x4 s[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
@@ -315,57 +347,38 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
     }
     const bf16x8 pf = __builtin_bit_cast(bf16x8, make_uint4(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]),
                                                             pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7])));
-    if constexpr (decltype(one)::value) {
-#pragma unroll 1
-      for (int q = 0; q < 16; ++q) {
-        const uint32_t seen = below(p, ok ? min(p_end, __builtin_amdgcn_readlane(qpos, q) + 1) : 0);
+    auto values = [&](auto part, auto own, uint32_t mask) {
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const f32x4 y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(db, seen), pf, o[db], 0, 0, 0);
-          if (lane % 16 == q) o[db] = y;  // (a product's columns are independent: the others are not taken)
-        }
-      }
-    } else if (inner) {
-#pragma unroll
-      for (int db = 0; db < DB; ++db) o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(db, 255), pf, o[db], 0, 0, 0);
-    } else {
-      const uint32_t mask = below(p, ok ? p_end : 0);
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(db, mask), pf, o[db], 0, 0, 0);
-      }
-    }
+      for (int db = 0; db < DB; ++db) o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v_frag(part, own, db, mask), pf, o[db], 0, 0, 0);
+    };
+    if (inner)
+      values(std::false_type(), std::false_type(), 0);
+    else if (p < own_rows)
+      values(std::true_type(), std::false_type(), below(p, ok ? p_end : 0));
+    else
+      values(std::true_type(), std::true_type(), below(p, ok ? p_end : 0));
   };
-  auto steps = [&](auto one) {
-    pl = place(p0);
-    load_k(pl);
+  pl = place(p0);
+  load_k(pl);
+  load_v(pl);
+  if (wave < KK) *reinterpret_cast<uint4*>(s_q + wave * 1024 + lane * 16) = q_frag;
+  __syncthreads();  // the queries are in LDS
+#pragma unroll 1
+  for (int p = p0; p < p_end; p += kStride) {
+    step(p);
+    __builtin_amdgcn_sched_barrier(0);
     load_v(pl);
-    if constexpr (!decltype(one)::value) {
-      if (wave < KK) *reinterpret_cast<uint4*>(s_q + wave * 1024 + lane * 16) = q_frag;
-      __syncthreads();  // the queries are in LDS
-    }
+  }
+  // what the wave zeroed of its steps (48 positions at most, in two of them)
+  if (__any(wild)) {
 #pragma unroll 1
-    for (int p = p0; p < p_end; p += kStride) {
-      step(one, p);
-      __builtin_amdgcn_sched_barrier(0);
-      load_v(pl);
-    }
-  };
-  steps(std::false_type{});
-  // On the tile's diagonal a position may be hidden from some of the query vectors only.  Where a V value there is not finite,
-  // the zero weight of those vectors has not kept it out, and their sums are not finite: then the wave's steps again, each
-  // vector's product by itself.
-  if (lo + 1 < tile_end && p_end > lo + 1) {
-    bool wild = false;
+    for (int p = own_rows; p < min(p_end, tile_end); p += 8) {
+      const int id = a.pg.table[(int64_t)sq.row * a.pg.width + (p >> lg)];
+      if ((p - p_begin) / 32 % kWaves != wave || (unsigned)id >= (unsigned)a.pg.n_pages) continue;
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+      for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) wild |= !__builtin_isfinite(o[db][i]);
-    if (__any(wild)) {
-      reset();
-      page0 = p_begin >> lg;
-      load_ids();
-      steps(std::true_type{});
+        for (int i = 0; i < 4; ++i) o[db][i] = add_wild<E4, HD>(a, id, kvh, p, 16 * db + 4 * (lane / 16) + i, qpos, o[db][i]);
     }
   }
   m *= a.scale;  // (-inf stays: the scale is positive)
@@ -422,10 +435,6 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
 // 32x32x16 products: a lane holds 16 scores of one query vector, which are its operand of the second product as they stand
 // (the stored order of K's rows sees to that).  At 168 registers three workgroups share a compute unit (bf16 with 128 dimensions
 // keeps two values of its end in scratch for that), and 36 or 48 KiB of LDS each.
-//
-// A tile's own rows see different parts of its last steps, and a hidden position's weight of 0 does not keep out a V value that is
-// not finite.  Such values are zeroed in those steps and added behind the loop, one position after the other, to the vectors that
-// see them: 1024 rows of 64/8 heads behind 3000 positions 143 us, with a NaN in the last position 166, with one in every row 189.
 
 // Four reads of 16 (8) bytes a lane from addr + off(i), and their wait, in one block: the compiler would hold every LDS read back
 // until all direct loads into LDS, those of later steps too, have landed.
@@ -713,25 +722,17 @@ __global__ void __launch_bounds__(kWideWaves * kWave, 3) paged_attn_wide_kernel(
   for (; p < p_end; p += 32) next_step();  // (steps behind the tile's last position: the other waves')
   __builtin_amdgcn_s_waitcnt(wait_vmcnt(0));  // (the loads past the end: they clear LDS)
   if (a.err && bad_page && threadIdx.x == 0) atomicOr(a.err, kErrId);
-  // The values that were zeroed: an infinity or NaN, times a positive weight, is itself.  At most 63 positions.
+  // what the wave zeroed (64 positions at most)
   if (__any(wild)) {
 #pragma unroll 1
-    for (int p = own_rows; p < min(p_end, tile_end); ++p) {
-      const int id = a.pg.table[(int64_t)sq.row * a.pg.width + (p >> lg)], in = p & in_mask;
+    for (int p = own_rows; p < min(p_end, tile_end); p += 8) {
+      const int id = a.pg.table[(int64_t)sq.row * a.pg.width + (p >> lg)];
       if ((unsigned)id >= (unsigned)a.pg.n_pages) continue;
-      const char* side = page_head(a.pg, id, kvh) + a.pg.side;
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {  // dimension 32 db + 8 (i / 4) + 4 half + i % 4
-          const char* at = side + page_v_offset<E4, HD>(in, 32 * db + 8 * (i / 4) + 4 * half + i % 4);
-          float v;
-          if constexpr (E4)
-            v = (*reinterpret_cast<const uint8_t*>(at) & 0x7f) == 0x7f ? NAN : 0.f;
-          else
-            v = bf16_to_f32(*reinterpret_cast<const uint16_t*>(at));
-          if (p <= qpos && !__builtin_isfinite(v)) o[db][i] += v;
-        }
+        for (int i = 0; i < 16; ++i)  // dimension 32 db + 8 (i / 4) + 4 half + i % 4
+          o[db][i] = add_wild<E4, HD>(a, id, kvh, p, 32 * db + 8 * (i / 4) + 4 * half + i % 4, qpos, o[db][i]);
     }
   }
   const float lsum = xor32_op(l, [](float x, float y) { return x + y; });

@@ -93,6 +93,55 @@ def test_a_bad_value_on_the_diagonal_of_a_long_part(S, dtype, hq, hkv, hd, R, at
         assert torch.isfinite(w[ok]).all() and (off <= t)[ok].all(), r
 
 
+FEW = [(64, 8, 128, 33, 1000), (64, 8, 128, 60, 6000), (28, 4, 128, 200, 2200), (8, 8, 64, 17, 500), (28, 4, 128, 1, 700)]  # (as above)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("hq, hkv, hd, R, at", FEW)
+@pytest.mark.parametrize("side, where", [("v", "last"), ("v", "first"), ("k", "last")])
+def test_one_bad_value_costs_little_among_few_rows(S, dtype, hq, hkv, hd, R, at, side, where):  # noqa: F811
+    """The same where the sequence's steps are shared out over waves and workgroups: two and a half times at most."""
+    c, kv = filled(S, dtype, hkv, hd, 64, at + R)
+    put(c, kv)
+    q = randn(3, 1, R, hq, hd).to(torch.bfloat16).cuda()
+    lens, out = i32([at]), torch.empty_like(q)
+    ws = c.pool.attention_workspace(1, R, hq, at + R)
+    call = lambda: c.pool.attention(q, c.table, lens, max_len=at + R, out=out, ws=ws)  # noqa: E731
+    clean = microseconds(call, 10)
+    kv[0, at + R - 1 if where == "last" else 0].view(2, hkv, hd)[0 if side == "k" else 1, :, 3] = math.nan
+    put(c, kv)
+    spoilt = microseconds(call, 10)
+    assert spoilt <= 2.5 * clean, (clean, spoilt)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "e4m3"])
+@pytest.mark.parametrize("hq, hkv, hd, R, at", FEW)
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("where", [0, 0.5, 1])
+def test_a_bad_value_among_few_rows(S, dtype, hq, hkv, hd, R, at, bad, where):  # noqa: F811
+    c, kv = filled(S, dtype, hkv, hd, 32, at + R, seed=3)
+    r0 = round(where * (R - 1))
+    h0, d0 = hkv - 1, hd - 5
+    kv[0, at + r0].view(2, hkv, hd)[1, h0, d0] = bad
+    k, v = put(c, kv)
+    q = randn(4, 1, R, hq, hd).to(torch.bfloat16)
+    got = c.pool.attention(q.cuda(), c.table, i32([at]))[0].cpu().double()
+    grp = hq // hkv
+    for r in sorted({0, 1, r0 - 1, r0, r0 + 1, R - 1} & set(range(R))):
+        want, tol = ref.attention(q[0, r:r + 1].double(), k, v, at + r, hd ** -0.5)
+        off = (got[r:r + 1] - want).abs()[0]
+        ok = torch.ones(hq, hd, dtype=torch.bool)
+        if r >= r0:
+            heads = slice(h0 * grp, (h0 + 1) * grp)
+            dims = slice(None) if dtype == "e4m3" else slice(d0, d0 + 1)
+            ok[heads, dims] = False
+            if dtype == "e4m3" or math.isnan(bad):
+                assert torch.isnan(got[r, heads, dims]).all(), r
+            else:  # (its weight is positive)
+                assert (got[r, heads, dims] == bad).all(), r
+        assert (off <= tol[0])[ok].all(), r
+
+
 @pytest.mark.parametrize("hq, hkv, B, R", [(16, 8, 1, 1), (16, 8, 1, 33), (16, 8, 1, 1400), (80, 40, 4, 20)])
 def test_scores_past_the_range(S, hq, hkv, B, R):  # noqa: F811
     """A score that passes fp32's range is no weight of 0: the row's result is the softmax's (that position alone) or NaN."""
