@@ -145,7 +145,8 @@ int sdd_kv_destroy(sdd_kv* kv);
  * (host pointers, either may be NULL) and the sticky error word (bit0: a
  * capacity overflow was refused on the device, bit1: a token outside
  * [0, vocab) was replaced by 0, bit2: a sequence id outside [0, max_batch)
- * was refused, bit3: a GEMM workgroup's internal hand-off between its waves
+ * was refused, or a paged cache's block table holds no page for a position of
+ * a call, bit3: a GEMM workgroup's internal hand-off between its waves
  * gave up after its bounded wait, so that call's outputs are invalid). */
 int sdd_kv_state(sdd_kv* kv, int32_t* len, int32_t* pending, int32_t* error_bits,
                  sdd_stream_t stream);
@@ -200,7 +201,10 @@ int sdd_kv_prefill(sdd_model* m, sdd_kv* kv, int seq, const int32_t* tokens, int
  * Bits: a row's outputs depend on its sequence alone, not on the other
  * sequences or rows of the call, except (bf16) for one line: calls of up to 64
  * rows in all and calls of more add a row's products in different orders, and
- * their results differ by rounding. */
+ * their results differ by rounding.  Over a paged cache the rows a sequence has
+ * in the call (gamma) count too, and from some size on its sequences
+ * (sdd_paged_attention): a block's verification and the decode steps of its
+ * tokens differ by rounding. */
 int sdd_verify_block(sdd_model* m, sdd_kv* kv, const int32_t* seq_ids, int n_seq,
                      const int32_t* drafts, int gamma, float* logits, int32_t* argmax,
                      void* ws, size_t ws_bytes, sdd_stream_t stream);
@@ -239,7 +243,8 @@ int sdd_kv_commit(sdd_kv* kv, const int32_t* seq_ids, int n_seq, const int32_t* 
  * of every KV head; the pages of a sequence, in any order and anywhere in the
  * pool, are the entries of its row of a block table (device int32
  * [B][table_width]): position p lies in page table[b][p / page_size].  Several
- * sequences may hold the same page (a common prefix, to be read): a position
+ * sequences may hold the same page (a common prefix, to be read; which page is
+ * whose is the caller's to know): a position
  * that more than one of them appends to in one call, or a page named twice in
  * a row of the table, ends up as any mix of what they wrote there.
  * Stored order, for callers that move pages themselves: head h of page p starts
@@ -337,7 +342,7 @@ int sdd_paged_attention_workspace_bytes(const sdd_pages* pg, int B, int R, int n
  * bit-reproducible and do not depend on what the call's other sequences hold;
  * below a B * n_kv_heads * ceil(R * n_q_heads / n_kv_heads / 128) of 160 not on B
  * either (from there B decides into how many parts a sequence's sums are cut;
- * R, whose rows share work, always counts).  Errors: SDD_EINVAL, SDD_ENOMEM (small workspace),
+ * R decides that always).  Errors: SDD_EINVAL, SDD_ENOMEM (small workspace),
  * SDD_EUNSUPPORTED. */
 int sdd_paged_attention(const sdd_pages* pg, const int32_t* table, int table_width, const int32_t* len, int B, int R,
                         int n_q_heads, const uint16_t* q, float scale, int max_len, uint16_t* out, int32_t* err,

@@ -4,8 +4,9 @@
 // Both are streams: a row's (n_q + 2 n_kv) heads are read once, q is written once and K/V once in the cache's type; the
 // rotation's cosines and sines are read from a table (angles in 64 bits when it is made: in 32 bits, position 10^5 would be
 // off by 4e-3 rad at the first frequency).  Bound: the memory.  64/8 heads of 128: 4095 rows appended (168 MB, norms and
-// rotation) 42 us, 4.0 TB/s where a copy of torch's runs at 4.9; eight prefixes of 4001 positions read from e4m3 pages (197 MB)
-// 34 us, 5.8 TB/s, from bf16 (262 MB) 45 (in- and outputs changing from call to call); one row appended 4.4 us, read 3.2.
+// rotation) 38 us, 4.4 TB/s where a copy of torch's runs at 4.9, and rows in fp32 (252 MB) 53 us; eight prefixes of 4001
+// positions read from e4m3 pages (197 MB) 34 us, 5.8 TB/s, from bf16 (262 MB) 45 (in- and outputs changing from call to call); one
+// row appended 4.4 us, read 3.2.
 #include <algorithm>
 #include <cmath>
 

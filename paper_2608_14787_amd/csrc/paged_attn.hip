@@ -18,10 +18,10 @@
 // is not finite.  Both kernels zero such values there and add them behind the loop to the vectors that see them: 1024 rows of 64/8
 // heads behind 3000 positions 143 us, with a NaN in the last position 151, in every row 175; 33 rows behind 1000 17 and 28.
 //
-// Bound, for 64/8 heads of 128: with few rows the stream of K and V (32 ragged sequences in bf16 52 us, 5.5 TB/s; 229000
-// positions in e4m3 80 us, 5.9 TB/s) or, short, the chain of page id, loads, products and joins (one row, 513 positions 6.7 us);
+// Bound, for 64/8 heads of 128: with few rows the stream of K and V (32 ragged sequences in bf16 53 us, 5.4 TB/s; 229000
+// positions in e4m3 80 us, 5.9 TB/s) or, short, the chain of page id, loads, products and joins (one row, 513 positions 6.9 us);
 // with many the softmax's instructions beside the products (1024 rows behind 1055 positions 65 us, 0.81 PFLOP/s; 4096 rows
-// from 0 on 277, 1.0 PFLOP/s).
+// from 0 on 268, 1.0 PFLOP/s).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>

@@ -612,7 +612,8 @@ class PagedKVCache(KVCache):
     """A KV cache in pages (sdd_paged_kv_create): memory for n_pages pages a layer, shared out to sequences as they grow.
 
     `table` (int32 [max_batch, width], device) may be written by the caller; assign() and release() keep it from a free
-    list on the host.  With `stream`, the constructor, assign() and release() write it on that stream, as the calls that read it
+    list on the host, without counts: what assign() hands out is one sequence's until its release(), so a page that the caller
+    writes into the rows of several must not be released before all are done with it.  With `stream`, the constructor, assign() and release() write it on that stream, as the calls that read it
     run on theirs; a cache used on several streams is ordered between them by the caller."""
 
     def __init__(self, model: Model, max_batch: int, max_len: int, n_pages: int, page_size: int = 64, dtype: str = "bf16",
