@@ -239,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, 3) paged_attn_kernel(PagedAttnArgs a
   float ref = 0.f;               // -m scale (0 for no m)
   // the step from which some of the tile's vectors see less than others (a single row's: none)
   const int own_rows = tile_end == lo + 1 ? INT32_MAX : max(p_begin, (lo + 1) & ~31);
-  bool wild = false;                                  // the lane has zeroed a value there
+  bool wild = false;  // the lane has zeroed a value there
   // V operand of 16 dimensions.  Of a step that not every vector sees whole, positions outside `mask` (a bit for each of the
   // lane's 8) are zeroed: their weights are 0, and 0 times a stale or foreign non-finite value would not be.  So is what is not
   // finite among the tile's own rows, to be added behind the loop.
@@ -677,7 +677,7 @@ __global__ void __launch_bounds__(kWideWaves * kWave, 3) paged_attn_wide_kernel(
             for (int k = 0; k < 2; ++k) {
               const int n = max(0, min(4, seen(i) - 4 * k));
               uint32_t w = vr[i][k] & (uint32_t)((uint64_t(1) << (8 * n)) - 1);
-              const uint32_t bad = ((w & 0x7f7f7f7fu) + 0x01010101u) & (p >= own_rows ? 0x80808080u : 0u);  // bit 7 of the NaN codes' bytes
+              const uint32_t bad = ((w & 0x7f7f7f7fu) + 0x01010101u) & (p >= own_rows ? 0x80808080u : 0u);  // (the NaN codes)
               w &= ~((bad << 1) - (bad >> 7));
               wild |= bad != 0;
               vr[i][k] = w;
@@ -693,7 +693,7 @@ __global__ void __launch_bounds__(kWideWaves * kWave, 3) paged_attn_wide_kernel(
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               uint32_t w = vr[i][k] & ((2 * k < seen(i) ? 0xffffu : 0u) | (2 * k + 1 < seen(i) ? 0xffff0000u : 0u));
-              const uint32_t bad = ((w & 0x7f807f80u) + 0x00800080u) & (p >= own_rows ? 0x80008000u : 0u);  // exponents of all ones
+              const uint32_t bad = ((w & 0x7f807f80u) + 0x00800080u) & (p >= own_rows ? 0x80008000u : 0u);  // (exponents of all ones)
               w &= ~((bad << 1) - (bad >> 15));
               wild |= bad != 0;
               vr[i][k] = w;
