@@ -45,6 +45,7 @@ typedef struct ihipStream_t* sdd_stream_t; /* a hipStream_t; NULL = default stre
 #define SDD_F32 0
 #define SDD_BF16 1
 #define SDD_E4M3 2 /* paged caches only */
+#define SDD_E8M0 3 /* scales of 8-bit products only: a byte b stands for 2^(b - 127), 255 for NaN */
 
 /* acceptance modes (Sec. 3.1; Appendix "Baselines and Sweep Settings") */
 #define SDD_GREEDY 0  /* accept x^_j iff it is the target argmax (lowest index on ties) */
@@ -354,6 +355,79 @@ int sdd_paged_attention(const sdd_pages* pg, const int32_t* table, int table_wid
 int sdd_paged_read(const sdd_pages* pg, const int32_t* table, int table_width, const int32_t* start, int B, int n,
                    uint16_t* k, uint16_t* v, int32_t* err, sdd_stream_t stream);
 
+/* ---- products in 8 bits --------------------------------------------------- */
+
+/* Rows and matrices as e4m3 codes (OCP: no infinities) with a scale for each
+ * block of 128 columns: the projections around the paged cache's append and
+ * attention, for weights held in 8 bits.  A row [K] has ceil(K / 128) blocks (the
+ * last may be shorter), a matrix [N][K] blocks of 128 x 128; K is a multiple of 16.
+ * Scales are fp32 (SDD_F32) or bytes (SDD_E8M0), for rows block-major
+ * [ceil(K / 128)][M] (so that a step of the product reads those of its rows side by side),
+ * for matrices [ceil(N / 128)][ceil(K / 128)].
+ * Conversion of a block y: with a = max |y|, the scale s is max(a / 448, 2^-126)
+ * (SDD_F32), or 2^e with e the smallest exponent in [-126, 127] that has a <=
+ * 448 2^e (SDD_E8M0); 1 where a = 0.  Codes are y / s in fp32, rounded once to
+ * the nearest code.  A block with an infinity or NaN has NaN codes and s = 1.
+ * A row's result does not depend on the other rows of its call.
+ * Outputs overlap no input, but for residual_out, which may be the residual. */
+
+/* Rows x [M][K] (SDD_BF16 or SDD_F32; row_stride elements apart, base and stride
+ * 16-byte aligned) to codes [M][K] and scales.  Errors: SDD_EINVAL (NULL pointer,
+ * bad shape, dtype or alignment). */
+int sdd_e4m3_quantize(const void* x, int dtype, size_t row_stride, int M, int K, uint8_t* codes, void* scales,
+                      int scale_dtype, sdd_stream_t stream);
+
+/* The same of a matrix [N][K], in blocks of 128 x 128. */
+int sdd_e4m3_quantize_matrix(const void* x, int dtype, size_t row_stride, int N, int K, uint8_t* codes, void* scales,
+                             int scale_dtype, sdd_stream_t stream);
+
+/* Residual and RMS norm before a product: r = residual + x in fp32 (residual
+ * [M][K], SDD_BF16 or SDD_F32, NULL: r = x), written to residual_out in the
+ * residual's type; y = r / sqrt(mean r^2 + eps) * gain (gain fp32 [K]) in fp32
+ * from r before it is rounded, converted to codes and scales; y_out (may be
+ * NULL) also receives y as bf16 [M][K].  K at most 65536.  Errors: as above, and
+ * SDD_EUNSUPPORTED for a larger K. */
+int sdd_e4m3_rmsnorm(const void* x, int dtype, size_t row_stride, const void* residual, void* residual_out,
+                     int residual_dtype, const float* gain, float eps, int M, int K, uint8_t* codes, void* scales,
+                     int scale_dtype, uint16_t* y_out, sdd_stream_t stream);
+
+/* SwiGLU before the down projection: row m of x holds K gate values and then K
+ * of the up projection; y = g / (1 + e^-g) * u in fp32, converted. */
+int sdd_e4m3_swiglu(const void* x, int dtype, size_t row_stride, int M, int K, uint8_t* codes, void* scales,
+                    int scale_dtype, sdd_stream_t stream);
+
+/* A matrix [N][K] in the order the product reads it, in a caller-owned device
+ * buffer of sdd_e4m3_matrix_bytes() bytes (256-byte aligned): tiles of 16 rows x
+ * 128 columns, [row tile][block][half][lane][16 bytes], lane 16 g + r holding
+ * columns 64 half + 16 g .. + 15 of row r, zeros behind the matrix's ends; then the
+ * scales as fp32. */
+typedef struct {
+  int N, K; /* K a multiple of 16, at most 2^20; N at most 2^24 */
+  void* data; /* device */
+} sdd_e4m3_matrix;
+
+/* Errors: SDD_EINVAL.  (m->data is not read.) */
+int sdd_e4m3_matrix_bytes(const sdd_e4m3_matrix* m, size_t* bytes);
+/* Lays row-major codes [N][K] (16-byte aligned) and scales out into m->data; they
+ * may be freed when the stream is through. */
+int sdd_e4m3_matrix_load(const sdd_e4m3_matrix* m, const uint8_t* codes, const void* scales, int scale_dtype,
+                         sdd_stream_t stream);
+
+/* Workspace of sdd_e4m3_matmul for calls of at most M rows on matrices of this
+ * shape (0: none is needed).  It needs no initialization and carries nothing from one call to the next; calls that
+ * may run at the same time need one each. */
+int sdd_e4m3_matmul_workspace_bytes(const sdd_e4m3_matrix* m, int M, size_t* bytes);
+
+/* out[r][n] = sum_j xs[j][r] ws[n / 128][j] sum_k x[r][k] w[n][k] (k over block j),
+ * r < M: codes x [M][K] (16-byte aligned) and scales xs [ceil(K / 128)][M] as the
+ * operators above leave them; out SDD_BF16 or SDD_F32, rows out_stride elements
+ * apart (elements between them are left alone).
+ * Products of a block are summed by the matrix cores, blocks in fp32, the result
+ * is rounded once, in an order fixed by the shapes: results are bit-reproducible.
+ * Errors: SDD_EINVAL, SDD_ENOMEM (small workspace). */
+int sdd_e4m3_matmul(const sdd_e4m3_matrix* m, const uint8_t* x, const void* x_scales, int scale_dtype, int M, void* out,
+                    int out_dtype, size_t out_stride, void* ws, size_t ws_bytes, sdd_stream_t stream);
+
 /* ---- acceptance and confidence ---------------------------------------- */
 
 /* Workspace bytes for sdd_accept / sdd_confidence_prefix at these shapes
@@ -547,6 +621,8 @@ int sdd_survival_mlp(const sdd_mlp* m, const uint16_t* hidden, const float* scal
 #define SDD_PROF_MLP 1024u
 #define SDD_PROF_LOGPROBS 2048u
 #define SDD_PROF_PAGES 4096u /* paged cache: append and read (its attention: SDD_PROF_ATTN) */
+#define SDD_PROF_GEMM8 8192u /* product in 8 bits */
+#define SDD_PROF_ROWS8 16384u /* rows and matrices into 8 bits */
 
 /* Starts timing: until sdd_profile_stop, every every-th launch (1: each) of
  * the classes in class_mask is bracketed by two HIP events on its own stream

@@ -1,0 +1,413 @@
+// Rows and matrices into 8 bits (gfx950): e4m3 codes with a scale for each block of 128 columns, of rows as they are, after
+// a residual's addition and an RMS norm, or after SwiGLU, and of matrices in blocks of 128 x 128.
+//
+// A block y with a = max |y|: s = max(a / 448, 2^-126), or the least power of two with a <= 448 s; codes = e4m3(y / s).  The
+// quotient is a product with 1 / s (exact for powers of two; otherwise off by an fp32 rounding before the one to 3 bits).
+// Bound: the memory, and for few rows the chain load, sum, maximum, store.  A lane holds 16 consecutive columns (16 bytes of
+// codes; 32 or 64 of input), eight lanes a block: its maximum is three steps inside a row of lanes, and no value changes lanes.
+#include <algorithm>
+
+#include "e4m3.h"
+
+namespace sdd {
+namespace {
+
+constexpr int kPer = 16;                    // columns of a lane
+constexpr int kLanes = kBlock8 / kPer;      // lanes of a block
+constexpr int kWaveCols = kWave * kPer;     // columns of a wave
+constexpr int kMaxNormThreads = 1024, kMaxNormK = 65536;
+
+template <typename T>
+struct Raw {  // 16 elements as they lie in memory
+  uint4 v[sizeof(T)];
+  __device__ inline void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T); ++i) v[i] = load16(reinterpret_cast<const char*>(p) + 16 * i);
+  }
+  __device__ inline void zero() {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T); ++i) v[i] = make_uint4(0, 0, 0, 0);
+  }
+  __device__ inline void values(float* y) const {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T); ++i) unpack16(v[i], y + i * (16 / sizeof(T)), T());
+  }
+};
+
+// max |y|, or infinity where a value is not finite
+__device__ inline float amax16(const float* y) {
+  float m = 0.f, z = 0.f;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    m = fmaxf(m, fabsf(y[i]));
+    z = __builtin_fmaf(y[i], 0.f, z);  // 0 for finite values, NaN otherwise
+  }
+  return z == 0.f ? m : INFINITY;
+}
+__device__ inline float amax_block(float m) {  // over the eight lanes of a block
+  m = fmaxf(m, dpp_f<kDppXor1>(m));
+  m = fmaxf(m, dpp_f<kDppXor2>(m));
+  return fmaxf(m, dpp_f<kDppHalfMirror>(m));
+}
+
+struct Scale {
+  float inv;    // 1 / s; NaN: the block is not finite
+  float s;
+  int byte;     // of a power of two
+};
+__device__ inline Scale scale_of(float a, bool e8) {
+  if (a == INFINITY) return Scale{__builtin_nanf(""), 1.f, 127};
+  if (a == 0.f) return Scale{1.f, 1.f, 127};
+  if (e8) {
+    // a = f 2^x, f in [1, 2); 448 = 1.75 2^8
+    const uint32_t u = __builtin_bit_cast(uint32_t, a);
+    const int x = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u);
+    const int byte = max(1, min(254, x + 127));
+    return Scale{__builtin_bit_cast(float, byte == 254 ? 0x00400000u : (uint32_t)(254 - byte) << 23), 0.f, byte};
+  }
+  const float s = fmaxf(a / 448.f, 0x1p-126f);
+  return Scale{1.f / s, s, 0};
+}
+__device__ inline uint4 encode16(const float* y, float inv) {
+  if (inv != inv) return make_uint4(0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu);
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = codes4(y[4 * i] * inv, y[4 * i + 1] * inv, y[4 * i + 2] * inv, y[4 * i + 3] * inv);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ inline void store_scale(void* scales, bool e8, int64_t i, const Scale& sc) {
+  if (e8)
+    reinterpret_cast<uint8_t*>(scales)[i] = (uint8_t)sc.byte;
+  else
+    reinterpret_cast<float*>(scales)[i] = sc.s;
+}
+
+struct RowsArgs {
+  const char* x;
+  int64_t stride;  // elements
+  int M, K;
+  uint8_t* codes;
+  void* scales;
+  int e8;
+  // rmsnorm
+  const char* res;
+  char* res_out;
+  const float* gain;
+  uint16_t* y;
+  float eps;
+};
+
+// The lane's 16 columns from `col` of row m, y, to codes; the first lane of a block stores its scale.
+__device__ inline void store_rows(const RowsArgs& a, int64_t m, int col, const float* y) {
+  const Scale sc = scale_of(amax_block(amax16(y)), a.e8);
+  if (col >= a.K) return;
+  *reinterpret_cast<uint4*>(a.codes + m * a.K + col) = encode16(y, sc.inv);
+  if (col % kBlock8 == 0) store_scale(a.scales, a.e8, (int64_t)(col / kBlock8) * a.M + m, sc);
+}
+
+// Rows as they are, or after SwiGLU: a wave takes 1024 columns of a row.
+template <typename T, bool SWIGLU>
+__global__ void __launch_bounds__(256) rows_kernel(RowsArgs a, int segs) {
+  const int lane = threadIdx.x % kWave;
+  const int64_t item = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+  const int64_t m = item / segs;
+  if (m >= a.M) return;
+  const int col = (int)(item - m * segs) * kWaveCols + lane * kPer;
+  const T* x = reinterpret_cast<const T*>(a.x) + m * a.stride + col;
+  Raw<T> r, u;
+  r.zero(), u.zero();
+  if (col < a.K) {
+    r.load(x);
+    if constexpr (SWIGLU) u.load(x + a.K);
+  }
+  float y[kPer];
+  r.values(y);
+  if constexpr (SWIGLU) {
+    float up[kPer];
+    u.values(up);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) y[i] = y[i] * __builtin_amdgcn_rcpf(1.f + __expf(-y[i])) * up[i];
+  }
+  store_rows(a, m, col, y);
+}
+
+// A workgroup takes a row, C vectors of 16 columns a thread, kept in registers between the sum and the conversion.
+template <typename T, typename RT, bool RES, int C>
+__global__ void __launch_bounds__(kMaxNormThreads) norm_kernel(RowsArgs a) {
+  __shared__ float s_sum[kMaxNormThreads / kWave];
+  const int64_t m = blockIdx.x;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
+  const T* x = reinterpret_cast<const T*>(a.x) + m * a.stride;
+  float y[C][kPer];
+  float sum = 0.f;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int col = (c * (int)blockDim.x + (int)threadIdx.x) * kPer;
+    Raw<T> r;
+    r.zero();
+    if (col < a.K) r.load(x + col);
+    r.values(y[c]);
+    if constexpr (RES) {
+      Raw<RT> q;
+      q.zero();
+      if (col < a.K) q.load(reinterpret_cast<const RT*>(a.res) + m * a.K + col);
+      float z[kPer];
+      q.values(z);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) y[c][i] += z[i];
+      if (col < a.K) {
+        RT* o = reinterpret_cast<RT*>(a.res_out) + m * a.K + col;
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(RT); ++i) {
+          const float* v = y[c] + i * (16 / sizeof(RT));
+          uint4 w;
+          if constexpr (sizeof(RT) == 2)
+            w = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+          else
+            w = make_uint4(__builtin_bit_cast(uint32_t, v[0]), __builtin_bit_cast(uint32_t, v[1]), __builtin_bit_cast(uint32_t, v[2]),
+                           __builtin_bit_cast(uint32_t, v[3]));
+          reinterpret_cast<uint4*>(o)[i] = w;
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) sum = __builtin_fmaf(y[c][i], y[c][i], sum);
+  }
+  sum = wave_sum(sum);
+  if (lane == 0) s_sum[wave] = sum;
+  __syncthreads();
+  sum = 0.f;
+  for (int w = 0; w < waves; ++w) sum += s_sum[w];
+  const float rs = 1.f / sqrtf(sum / (float)a.K + a.eps);
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int col = (c * (int)blockDim.x + (int)threadIdx.x) * kPer;
+    if (col < a.K) {
+      Raw<float> g;
+      g.load(a.gain + col);
+      float gv[kPer];
+      g.values(gv);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) y[c][i] = y[c][i] * rs * gv[i];
+      if (a.y) {
+        uint4* o = reinterpret_cast<uint4*>(a.y + m * a.K + col);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float* v = y[c] + 8 * i;
+          o[i] = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+        }
+      }
+    } else {  // (zeros times a norm that is not finite)
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) y[c][i] = 0.f;
+    }
+    store_rows(a, m, col, y[c]);
+  }
+}
+
+// A workgroup takes a block of 128 x 128, four vectors of 16 columns a thread.
+template <typename T>
+__global__ void __launch_bounds__(256) matrix_kernel(RowsArgs a, int KB) {
+  __shared__ float s_max[4];
+  const int nb = blockIdx.x / KB, kb = blockIdx.x - nb * KB;
+  const int col = kb * kBlock8 + threadIdx.x % kLanes * kPer;
+  Raw<T> r[4];
+  float mx = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t row = (int64_t)nb * kBlock8 + i * 32 + threadIdx.x / kLanes;
+    r[i].zero();
+    if (row < a.M && col < a.K) r[i].load(reinterpret_cast<const T*>(a.x) + row * a.stride + col);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float y[kPer];
+    r[i].values(y);
+    mx = fmaxf(mx, amax16(y));
+  }
+  mx = wave_max(mx);
+  if (threadIdx.x % kWave == 0) s_max[threadIdx.x / kWave] = mx;
+  __syncthreads();
+  const Scale sc = scale_of(fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3])), a.e8);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t row = (int64_t)nb * kBlock8 + i * 32 + threadIdx.x / kLanes;
+    if (row >= a.M || col >= a.K) continue;
+    float y[kPer];
+    r[i].values(y);
+    *reinterpret_cast<uint4*>(a.codes + row * a.K + col) = encode16(y, sc.inv);
+  }
+  if (threadIdx.x == 0) store_scale(a.scales, a.e8, (int64_t)nb * KB + kb, sc);
+}
+
+// Row-major codes and scales to the stored order: a thread moves 16 bytes.
+__global__ void __launch_bounds__(256) load_codes_kernel(const uint8_t* codes, uint4* to, int N, int K, int KB, int64_t n) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  const int lane = (int)(i % kWave), half = (int)(i / kWave % 2);
+  const int64_t tile = i / (2 * kWave);
+  const int64_t nt = tile / KB, row = nt * 16 + lane % 16;
+  const int col = (int)(tile - nt * KB) * kBlock8 + half * 64 + lane / 16 * 16;
+  to[i] = row < N && col < K ? load16(codes + row * K + col) : make_uint4(0, 0, 0, 0);
+}
+__global__ void __launch_bounds__(256) load_scales_kernel(const void* scales, int e8, float* to, int64_t n) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  to[i] = e8 ? e8m0_value(reinterpret_cast<const uint8_t*>(scales)[i]) : reinterpret_cast<const float*>(scales)[i];
+}
+
+bool aligned16(const void* p) { return (uintptr_t)p % 16 == 0; }
+
+// The arguments that every conversion has.
+int check_rows(const void* x, int dtype, size_t stride, int M, int K, int width, const void* codes, const void* scales, int scale_dtype) {
+  SDD_REQUIRE(x && codes && scales, "NULL pointer");
+  SDD_REQUIRE(dtype == SDD_BF16 || dtype == SDD_F32, "rows must be bf16 or fp32 (dtype %d)", dtype);
+  SDD_REQUIRE(scale_dtype == SDD_F32 || scale_dtype == SDD_E8M0, "scales must be fp32 or E8M0 (dtype %d)", scale_dtype);
+  SDD_REQUIRE(M > 0 && M <= kMaxM8 && K > 0 && K <= kMaxK8 && K % 16 == 0, "bad shape [%d][%d] (K a multiple of 16, at most 2^20)", M, K);
+  const size_t es = dtype == SDD_F32 ? 4 : 2;
+  SDD_REQUIRE(stride >= (size_t)width && stride <= ((size_t)1 << 32), "row stride %zu for rows of %d", stride, width);
+  SDD_REQUIRE(aligned16(x) && stride * es % 16 == 0 && aligned16(codes), "rows and codes must be 16-byte aligned");
+  SDD_REQUIRE(scale_dtype == SDD_E8M0 || (uintptr_t)scales % 4 == 0, "scales must be 4-byte aligned");
+  return SDD_OK;
+}
+
+RowsArgs rows_args(const void* x, size_t stride, int M, int K, uint8_t* codes, void* scales, int scale_dtype) {
+  RowsArgs a = {};
+  a.x = reinterpret_cast<const char*>(x);
+  a.stride = (int64_t)stride;
+  a.M = M;
+  a.K = K;
+  a.codes = codes;
+  a.scales = scales;
+  a.e8 = scale_dtype == SDD_E8M0;
+  return a;
+}
+
+template <bool SWIGLU>
+int launch_rows(const RowsArgs& a, int dtype, hipStream_t st) {
+  const int segs = (int)ceil_div(a.K, kWaveCols);
+  const int64_t blocks = ceil_div((int64_t)a.M * segs, 4);
+  SDD_REQUIRE(blocks < ((int64_t)1 << 31), "too many rows (%d of %d)", a.M, a.K);
+  prof_begin(PROF_ROWS8, st);
+  if (dtype == SDD_F32)
+    hipLaunchKernelGGL((rows_kernel<float, SWIGLU>), dim3((unsigned)blocks), dim3(256), 0, st, a, segs);
+  else
+    hipLaunchKernelGGL((rows_kernel<uint16_t, SWIGLU>), dim3((unsigned)blocks), dim3(256), 0, st, a, segs);
+  prof_end(PROF_ROWS8, st);
+  return check_launch("rows_kernel");
+}
+
+template <typename T, typename RT, bool RES>
+void launch_norm(const RowsArgs& a, hipStream_t st) {
+  const int vecs = a.K / kPer;
+  const int threads = (int)std::min<int64_t>(kMaxNormThreads, ceil_div(vecs, kWave) * kWave);
+  const int c = (int)ceil_div(vecs, threads);
+  if (c == 1)
+    hipLaunchKernelGGL((norm_kernel<T, RT, RES, 1>), dim3(a.M), dim3(threads), 0, st, a);
+  else if (c == 2)
+    hipLaunchKernelGGL((norm_kernel<T, RT, RES, 2>), dim3(a.M), dim3(threads), 0, st, a);
+  else
+    hipLaunchKernelGGL((norm_kernel<T, RT, RES, 4>), dim3(a.M), dim3(threads), 0, st, a);
+}
+template <typename T>
+void launch_norm(const RowsArgs& a, int residual_dtype, hipStream_t st) {
+  if (!a.res) return launch_norm<T, float, false>(a, st);
+  if (residual_dtype == SDD_F32) return launch_norm<T, float, true>(a, st);
+  launch_norm<T, uint16_t, true>(a, st);
+}
+
+}  // namespace
+
+int check_matrix(const sdd_e4m3_matrix* m) {
+  SDD_REQUIRE(m != nullptr, "matrix description is NULL");
+  SDD_REQUIRE(m->N > 0 && m->N <= kMaxN8 && m->K > 0 && m->K <= kMaxK8 && m->K % 16 == 0,
+              "bad matrix [%d][%d] (K a multiple of 16, at most 2^20; N at most 2^24)", m->N, m->K);
+  return SDD_OK;
+}
+
+}  // namespace sdd
+
+using namespace sdd;
+
+extern "C" int sdd_e4m3_quantize(const void* x, int dtype, size_t row_stride, int M, int K, uint8_t* codes, void* scales,
+                                 int scale_dtype, sdd_stream_t stream) {
+  if (int rc = check_rows(x, dtype, row_stride, M, K, K, codes, scales, scale_dtype)) return rc;
+  return launch_rows<false>(rows_args(x, row_stride, M, K, codes, scales, scale_dtype), dtype, reinterpret_cast<hipStream_t>(stream));
+}
+
+extern "C" int sdd_e4m3_swiglu(const void* x, int dtype, size_t row_stride, int M, int K, uint8_t* codes, void* scales,
+                               int scale_dtype, sdd_stream_t stream) {
+  SDD_REQUIRE(K <= kMaxK8, "K %d", K);
+  if (int rc = check_rows(x, dtype, row_stride, M, K, 2 * K, codes, scales, scale_dtype)) return rc;
+  return launch_rows<true>(rows_args(x, row_stride, M, K, codes, scales, scale_dtype), dtype, reinterpret_cast<hipStream_t>(stream));
+}
+
+extern "C" int sdd_e4m3_quantize_matrix(const void* x, int dtype, size_t row_stride, int N, int K, uint8_t* codes, void* scales,
+                                        int scale_dtype, sdd_stream_t stream) {
+  if (int rc = check_rows(x, dtype, row_stride, N, K, K, codes, scales, scale_dtype)) return rc;
+  const int KB = (int)ceil_div(K, kBlock8);
+  const int64_t blocks = ceil_div(N, kBlock8) * KB;
+  SDD_REQUIRE(blocks < ((int64_t)1 << 31), "matrix [%d][%d] is too large", N, K);
+  const RowsArgs a = rows_args(x, row_stride, N, K, codes, scales, scale_dtype);
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  prof_begin(PROF_ROWS8, st);
+  if (dtype == SDD_F32)
+    hipLaunchKernelGGL((matrix_kernel<float>), dim3((unsigned)blocks), dim3(256), 0, st, a, KB);
+  else
+    hipLaunchKernelGGL((matrix_kernel<uint16_t>), dim3((unsigned)blocks), dim3(256), 0, st, a, KB);
+  prof_end(PROF_ROWS8, st);
+  return check_launch("matrix_kernel");
+}
+
+extern "C" int sdd_e4m3_rmsnorm(const void* x, int dtype, size_t row_stride, const void* residual, void* residual_out,
+                                int residual_dtype, const float* gain, float eps, int M, int K, uint8_t* codes, void* scales,
+                                int scale_dtype, uint16_t* y_out, sdd_stream_t stream) {
+  if (int rc = check_rows(x, dtype, row_stride, M, K, K, codes, scales, scale_dtype)) return rc;
+  SDD_REQUIRE(gain && aligned16(gain), "gain is NULL or not 16-byte aligned");
+  SDD_REQUIRE(!residual == !residual_out, "residual and residual_out come together");
+  SDD_REQUIRE(!residual || residual_dtype == SDD_BF16 || residual_dtype == SDD_F32, "residual must be bf16 or fp32 (dtype %d)", residual_dtype);
+  SDD_REQUIRE(aligned16(residual) && aligned16(residual_out) && aligned16(y_out), "residual and y must be 16-byte aligned");
+  SDD_REQUIRE(eps >= 0.f && eps < INFINITY, "eps %g", (double)eps);
+  if (K > kMaxNormK) return fail(SDD_EUNSUPPORTED, "rows of %d (at most %d are built)", K, kMaxNormK);
+  RowsArgs a = rows_args(x, row_stride, M, K, codes, scales, scale_dtype);
+  a.res = reinterpret_cast<const char*>(residual);
+  a.res_out = reinterpret_cast<char*>(residual_out);
+  a.gain = gain;
+  a.eps = eps;
+  a.y = y_out;
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  prof_begin(PROF_ROWS8, st);
+  if (dtype == SDD_F32)
+    launch_norm<float>(a, residual_dtype, st);
+  else
+    launch_norm<uint16_t>(a, residual_dtype, st);
+  prof_end(PROF_ROWS8, st);
+  return check_launch("norm_kernel");
+}
+
+extern "C" int sdd_e4m3_matrix_bytes(const sdd_e4m3_matrix* m, size_t* bytes) {
+  SDD_REQUIRE(bytes != nullptr, "bytes is NULL");
+  if (int rc = check_matrix(m)) return rc;
+  *bytes = (size_t)(matrix_code_bytes(m) + ceil_div(ceil_div(m->N, kBlock8) * ceil_div(m->K, kBlock8) * 4, 256) * 256);
+  return SDD_OK;
+}
+
+extern "C" int sdd_e4m3_matrix_load(const sdd_e4m3_matrix* m, const uint8_t* codes, const void* scales, int scale_dtype,
+                                    sdd_stream_t stream) {
+  if (int rc = check_matrix(m)) return rc;
+  SDD_REQUIRE(m->data && codes && scales, "NULL pointer");
+  SDD_REQUIRE(scale_dtype == SDD_F32 || scale_dtype == SDD_E8M0, "scales must be fp32 or E8M0 (dtype %d)", scale_dtype);
+  SDD_REQUIRE((uintptr_t)m->data % 256 == 0 && aligned16(codes), "the matrix must be 256-byte aligned, its codes 16-byte");
+  SDD_REQUIRE(scale_dtype == SDD_E8M0 || (uintptr_t)scales % 4 == 0, "scales must be 4-byte aligned");
+  const int KB = (int)ceil_div(m->K, kBlock8);
+  const int64_t n = matrix_code_bytes(m) / 16, ns = ceil_div(m->N, kBlock8) * KB;
+  SDD_REQUIRE(n / 256 < ((int64_t)1 << 31) - 1, "matrix [%d][%d] is too large", m->N, m->K);
+  hipStream_t st = reinterpret_cast<hipStream_t>(stream);
+  prof_begin(PROF_ROWS8, st);
+  hipLaunchKernelGGL(load_codes_kernel, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, codes, reinterpret_cast<uint4*>(m->data),
+                     m->N, m->K, KB, n);
+  hipLaunchKernelGGL(load_scales_kernel, dim3((unsigned)ceil_div(ns, 256)), dim3(256), 0, st, scales, scale_dtype == SDD_E8M0,
+                     reinterpret_cast<float*>(reinterpret_cast<char*>(m->data) + matrix_code_bytes(m)), ns);
+  prof_end(PROF_ROWS8, st);
+  return check_launch("load_codes_kernel");
+}

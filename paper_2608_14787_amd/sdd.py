@@ -16,7 +16,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libsdd.so")
 
 OK, EINVAL, ENOMEM, EHIP, ECAPACITY, EUNSUPPORTED = 0, -1, -2, -3, -4, -5
-F32, BF16, E4M3 = 0, 1, 2
+F32, BF16, E4M3, E8M0 = 0, 1, 2, 3
 GREEDY, RATIO, TOPK, LENIENT, RATIO_SAMPLE = 0, 1, 2, 3, 4
 (T_EMBED, T_LM_HEAD, T_FINAL_NORM, T_WQ, T_WK, T_WV, T_WO, T_WGATE, T_WUP, T_WDOWN,
  T_ATTN_NORM, T_FFN_NORM, T_Q_NORM, T_K_NORM) = range(14)
@@ -84,6 +84,14 @@ _SIGS = {
     "sdd_paged_read": (I, [P, P, I, P, I, I, P, P, P, P]),
     "sdd_logprobs_workspace_bytes": (I, [I, I, I, P]),
     "sdd_token_logprobs": (I, [P, I, SZ, I, I, I, P, I, P, P, P, P, P, SZ, P]),
+    "sdd_e4m3_quantize": (I, [P, I, SZ, I, I, P, P, I, P]),
+    "sdd_e4m3_quantize_matrix": (I, [P, I, SZ, I, I, P, P, I, P]),
+    "sdd_e4m3_rmsnorm": (I, [P, I, SZ, P, P, I, P, F, I, I, P, P, I, P, P]),
+    "sdd_e4m3_swiglu": (I, [P, I, SZ, I, I, P, P, I, P]),
+    "sdd_e4m3_matrix_bytes": (I, [P, P]),
+    "sdd_e4m3_matrix_load": (I, [P, P, P, I, P]),
+    "sdd_e4m3_matmul_workspace_bytes": (I, [P, I, P]),
+    "sdd_e4m3_matmul": (I, [P, P, P, I, I, P, I, SZ, P, SZ, P]),
     "sdd_profile_start": (I, [C.c_uint, I, I]),
     "sdd_profile_read": (I, [C.c_uint, P, P, P, P]),
     "sdd_profile_stop": (I, []),
@@ -92,6 +100,7 @@ _SIGS = {
 PROF_EMBED, PROF_GEMM_QKV, PROF_ATTN, PROF_GEMM_O = 1, 2, 4, 8
 PROF_GEMM_GATEUP, PROF_GEMM_DOWN, PROF_GEMM_LM, PROF_ACCEPT, PROF_CONF = 16, 32, 64, 128, 256
 PROF_SCHED, PROF_MLP, PROF_LOGPROBS, PROF_PAGES = 512, 1024, 2048, 4096
+PROF_GEMM8, PROF_ROWS8 = 8192, 16384
 SIG_RAW, SIG_MARGINAL, SIG_CONDITIONAL = 0, 1, 2
 (SKIP_OK, SKIP_STALE, SKIP_NO_CANDIDATE, SKIP_SHORT, SKIP_SHORT_BLOCK, SKIP_SPECIAL,
  SKIP_REPEAT) = range(7)
@@ -489,6 +498,186 @@ class PagePool:
         st = _here(self.buf, table, start, k, v) if err is None else _here(self.buf, table, start, k, v, err)
         _check(lib().sdd_paged_read(self._desc, table.data_ptr(), table.shape[1], start.data_ptr(), B, n, k.data_ptr(), v.data_ptr(), _addr(err), st))
         return k, v
+
+
+# ---- products in 8 bits -----------------------------------------------------------------------
+
+_SCALES = {"f32": (F32, torch.float32), "e8m0": (E8M0, torch.float8_e8m0fnu)}
+
+
+def _scale_code(t: torch.Tensor) -> int:
+    if t.dtype == torch.float32:
+        return F32
+    if t.dtype == torch.float8_e8m0fnu:
+        return E8M0
+    raise TypeError(f"scales must be float32 or float8_e8m0fnu, got {t.dtype}")
+
+
+def _codes_out(x, M, K, scale, out, matrix=False):
+    """(codes, scales) to write into, checked where they are given, and the scales' code."""
+    if scale not in _SCALES:
+        raise ValueError(f"scale must be f32 or e8m0, got {scale}")
+    code, dtype = _SCALES[scale]
+    blocks = -(-K // 128)
+    shape = (-(-M // 128), blocks) if matrix else (blocks, M)
+    if out is None:
+        return x.new_empty((M, K), dtype=torch.float8_e4m3fn), x.new_empty(shape, dtype=dtype), code
+    codes, scales = out
+    _codes(codes, "codes")
+    _need(tuple(codes.shape) == (M, K), f"codes must be [{M}, {K}]")
+    _need(scales.dtype == dtype and scales.is_contiguous() and tuple(scales.shape) == shape, f"scales must be contiguous {dtype} {list(shape)}")
+    return codes, scales, code
+
+
+def _codes(t, name):
+    if t.dtype != torch.float8_e4m3fn or t.dim() != 2 or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous float8_e4m3fn [rows, K]")
+
+
+def _rows2(x, name):
+    if x.dim() != 2 or x.shape[0] == 0 or x.stride(1) != 1:
+        raise ValueError(f"{name} must be [rows, columns] with unit column stride")
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+def e4m3_quantize(x: torch.Tensor, *, scale: str = "f32", out=None, stream=None):
+    """sdd_e4m3_quantize of rows x [M, K] (bf16 or fp32): (codes float8_e4m3fn [M, K], scales [ceil(K / 128), M]).
+
+    scale: "f32", or "e8m0" for powers of two (float8_e8m0fnu).  `out` gives the tensors to write into."""
+    if stream is not None:  # (what the call makes is that stream's)
+        with torch.cuda.stream(stream):
+            return e4m3_quantize(x, scale=scale, out=out)
+    s0, dt = _rows2(x, "x"), _dtype_code(x)
+    M, K = x.shape
+    codes, scales, code = _codes_out(x, M, K, scale, out)
+    st = _here(x, codes, scales)
+    _check(lib().sdd_e4m3_quantize(x.data_ptr(), dt, s0, M, K, codes.data_ptr(), scales.data_ptr(), code, st))
+    return codes, scales
+
+
+def e4m3_quantize_matrix(x: torch.Tensor, *, scale: str = "f32", out=None, stream=None):
+    """sdd_e4m3_quantize_matrix of x [N, K]: (codes float8_e4m3fn [N, K], scales [ceil(N / 128), ceil(K / 128)])."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return e4m3_quantize_matrix(x, scale=scale, out=out)
+    s0, dt = _rows2(x, "x"), _dtype_code(x)
+    N, K = x.shape
+    codes, scales, code = _codes_out(x, N, K, scale, out, matrix=True)
+    st = _here(x, codes, scales)
+    _check(lib().sdd_e4m3_quantize_matrix(x.data_ptr(), dt, s0, N, K, codes.data_ptr(), scales.data_ptr(), code, st))
+    return codes, scales
+
+
+def e4m3_swiglu(x: torch.Tensor, *, scale: str = "f32", out=None, stream=None):
+    """sdd_e4m3_swiglu of rows x [M, 2 K], the gate's columns first: (codes [M, K], scales [ceil(K / 128), M])."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return e4m3_swiglu(x, scale=scale, out=out)
+    s0, dt = _rows2(x, "x"), _dtype_code(x)
+    M, K = x.shape
+    _need(K % 2 == 0, "x must be [M, 2 K]")
+    K //= 2
+    codes, scales, code = _codes_out(x, M, K, scale, out)
+    st = _here(x, codes, scales)
+    _check(lib().sdd_e4m3_swiglu(x.data_ptr(), dt, s0, M, K, codes.data_ptr(), scales.data_ptr(), code, st))
+    return codes, scales
+
+
+def e4m3_rmsnorm(x: torch.Tensor, gain: torch.Tensor, *, eps: float = 1e-6, residual: torch.Tensor | None = None,
+                 residual_out: torch.Tensor | None = None, y=False, scale: str = "f32", out=None, stream=None):
+    """sdd_e4m3_rmsnorm of rows x [M, K] + residual [M, K]: (codes, scales, residual_out, y).
+
+    The sum is written to residual_out (default: in place of residual; None without one).  y: True, or a bf16 [M, K]
+    tensor, for the normed rows besides (else None)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return e4m3_rmsnorm(x, gain, eps=eps, residual=residual, residual_out=residual_out, y=y, scale=scale, out=out)
+    s0, dt = _rows2(x, "x"), _dtype_code(x)
+    M, K = x.shape
+    if gain.dtype != torch.float32 or not gain.is_contiguous() or gain.numel() != K:
+        raise ValueError("gain must be contiguous fp32 [K]")
+    codes, scales, code = _codes_out(x, M, K, scale, out)
+    used = [x, gain, codes, scales]
+    rd = F32
+    if residual is not None:
+        if residual_out is None:
+            residual_out = residual
+        rd = _dtype_code(residual)
+        for t, nm in ((residual, "residual"), (residual_out, "residual_out")):
+            if t.dtype != residual.dtype or not t.is_contiguous() or tuple(t.shape) != (M, K):
+                raise ValueError(f"{nm} must be contiguous {residual.dtype} [{M}, {K}]")
+        used += [residual, residual_out]
+    else:
+        _need(residual_out is None, "residual_out needs a residual")
+    if y is True:
+        y = x.new_empty((M, K), dtype=torch.bfloat16)
+    elif y is False:
+        y = None
+    if y is not None:
+        if y.dtype != torch.bfloat16 or not y.is_contiguous() or tuple(y.shape) != (M, K):
+            raise ValueError(f"y must be contiguous bf16 [{M}, {K}]")
+        used.append(y)
+    st = _here(*used)
+    _check(lib().sdd_e4m3_rmsnorm(x.data_ptr(), dt, s0, _addr(residual), _addr(residual_out), rd, gain.data_ptr(), eps, M, K,
+                                  codes.data_ptr(), scales.data_ptr(), code, _addr(y), st))
+    return codes, scales, residual_out, y
+
+
+class MatrixDesc(C.Structure):
+    _fields_ = [("N", C.c_int), ("K", C.c_int), ("data", P)]
+
+
+class E4M3Matrix:
+    """A matrix [N, K] (PyTorch Linear [out][in]) of e4m3 codes with a scale for each 128 x 128 block, laid out once for the
+    product in a torch-owned device buffer (codes and scales are not referenced afterwards)."""
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, stream=None):
+        _codes(codes, "codes")
+        N, K = codes.shape
+        sd = _scale_code(scales)
+        _need(scales.is_contiguous() and tuple(scales.shape) == (-(-N // 128), -(-K // 128)),
+              "scales must be contiguous [ceil(N / 128), ceil(K / 128)]")
+        self.shape = (N, K)
+        self.desc = MatrixDesc(N, K, None)
+        n = _size_out(lib().sdd_e4m3_matrix_bytes, C.byref(self.desc))
+        with torch.cuda.stream(stream):  # (None: the current one)
+            self.buf = codes.new_empty(n, dtype=torch.uint8)
+            self.desc.data = self.buf.data_ptr()
+            st = _here(codes, scales, self.buf)
+            _check(lib().sdd_e4m3_matrix_load(C.byref(self.desc), codes.data_ptr(), scales.data_ptr(), sd, st))
+        self._desc = C.byref(self.desc)
+
+    def workspace(self, max_rows: int) -> torch.Tensor:
+        """Workspace for products of up to max_rows rows on this matrix, one call at a time."""
+        n = _size_out(lib().sdd_e4m3_matmul_workspace_bytes, self._desc, max_rows)
+        return self.buf.new_empty(n)
+
+    def matmul(self, codes: torch.Tensor, scales: torch.Tensor, *, dtype: torch.dtype = torch.bfloat16, out=None, ws=None,
+               stream=None) -> torch.Tensor:
+        """sdd_e4m3_matmul of rows in 8 bits (codes [M, K], scales [ceil(K / 128), M]) with this matrix: [M, N] in `dtype` (bf16
+        or fp32), or in `out` (rows may lie apart)."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self.matmul(codes, scales, dtype=dtype, out=out, ws=ws)
+        _codes(codes, "codes")
+        N, K = self.shape
+        M = codes.shape[0]
+        if codes.shape[1] != K:
+            raise ValueError(f"codes must be [M, {K}]")
+        if not scales.is_contiguous() or tuple(scales.shape) != (-(-K // 128), M):
+            raise ValueError(f"scales must be contiguous [{-(-K // 128)}, {M}]")
+        if out is None:
+            out = codes.new_empty((M, N), dtype=dtype)
+        elif tuple(out.shape) != (M, N) or out.stride(1) != 1:
+            raise ValueError(f"out must be [{M}, {N}] with unit column stride")
+        if ws is None:
+            ws = self.workspace(M)
+        _need(ws.is_contiguous(), "ws must be contiguous")
+        sd, od = _scale_code(scales), _dtype_code(out)
+        st = _here(self.buf, codes, scales, out, ws)
+        _check(lib().sdd_e4m3_matmul(self._desc, codes.data_ptr(), scales.data_ptr(), sd, M, out.data_ptr(), od,
+                                     out.stride(0) if M > 1 else N, ws.data_ptr(), ws.nbytes, st))
+        return out
 
 
 # ---- decoder ------------------------------------------------------------------------------

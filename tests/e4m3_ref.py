@@ -1,0 +1,114 @@
+"""Plain 64-bit forms of the 8-bit products' operators, with the tolerances that their fp32 arithmetic gives (CPU torch)."""
+import math
+
+import torch
+
+HALF = {torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}  # a rounding's largest relative error
+U = 2.0 ** -24
+
+
+def blocks(n):
+    return -(-n // 128)
+
+
+def spread(scales, M, K, high):
+    """Scales [M / high, K / 128] to [M, K]."""
+    return scales.repeat_interleave(high, 0)[:M].repeat_interleave(128, 1)[:, :K]
+
+
+def block_max(y, high):
+    M, K = y.shape
+    pad = torch.nn.functional.pad(y.abs(), (0, -K % 128, 0, -M % high))
+    return pad.view(-1, high, blocks(K), 128).amax((1, 3))
+
+
+def half_step(v):
+    """Half the distance of e4m3 codes at v (of the larger binade where v lies on a border)."""
+    _, e = torch.frexp(v.abs().clamp(min=2.0 ** -6))
+    return torch.pow(2.0, (e - 5).double())
+
+
+def check_codes(y, codes, scales, kind, high=1, rel=0.0, least=0.0):
+    """codes [M, K] and scales [M / high, K / 128] against y (float64), each value of which fp32 arithmetic knows up to a relative
+    `rel` and an absolute `least`."""
+    M, K = y.shape
+    amax = block_max(y, high)
+    bad = ~torch.isfinite(amax)
+    codes, scales = codes.double(), scales.double()
+    assert scales.shape == amax.shape
+    ok = ~bad & (amax > least)
+    assert (scales[bad] == 1).all() and (scales[amax == 0] == 1).all()
+    if kind == "f32":
+        want = (amax / 448).clamp(min=2.0 ** -126)
+        # the maximum's error and the division's (2^-149: a step of fp32's smallest numbers)
+        assert ((scales - want).abs()[ok] <= (want * (rel + U) + least + 2.0 ** -149)[ok]).all()
+    else:
+        assert (torch.frexp(scales)[0] == 0.5).all()
+        # the smallest power of two that holds the maximum, which is known up to its error
+        assert (amax * (1 - rel - U) - least <= 448 * scales)[ok].all()
+        small = ok & (scales > 2.0 ** -126)
+        assert (amax * (1 + rel + U) + least > 224 * scales)[small].all()
+    s, bads = spread(scales, M, K, high), spread(bad, M, K, high)
+    assert torch.isnan(codes[bads]).all()
+    v = y / s
+    # y's error, then 1 / s and the product with it; the code is the nearest of that
+    tol = half_step(v) + v.abs() * (rel + 2 * U) + least / s
+    # (a maximum that the scale's own rounding puts above 448 is 448)
+    err = (codes - v).abs()
+    assert (err <= tol)[~bads].all(), (err - tol)[~bads].max()
+
+
+def rmsnorm(x, residual, gain, eps):
+    """(r, y, relative error of r, of y) in float64."""
+    r = x.double() + (residual.double() if residual is not None else 0)
+    K = r.shape[1]
+    y = r / torch.sqrt((r * r).mean(1, keepdim=True) + eps) * gain.double()
+    C = -(-K // 16384)
+    # the sum of squares: a lane's 16 C products added one by one, 6 steps over the wave, up to 16 waves; mean and eps; half of it
+    # through the root; root, quotient and two products; r's own rounding, in the squares too
+    rel_r = U if residual is not None else 0.0
+    return r, y, rel_r, (0.5 * (16 * C + 6 + 16 + 2) + 4) * U + 2 * rel_r
+
+
+def swiglu(x):
+    g, u = x.double().chunk(2, dim=1)
+    y = g / (1 + torch.exp(-g)) * u
+    # the exponent's argument is off by |g| (2 roundings), the exponential by a step, then a sum, a reciprocal (a step), two products
+    rel = (2 * float(g[torch.isfinite(g)].abs().clamp(max=88).max()) + 2 + 1 + 2 + 2) * U
+    # below -88 e^-g passes fp32's range, and the quotient is zero
+    least = float(u[torch.isfinite(u)].abs().max()) * 88 * 2.0 ** -125
+    return y, rel, least
+
+
+def matmul(codes, scales, wc, ws):
+    """(out, sum of |products|) in float64 of codes [M, K], scales [K / 128, M], wc [N, K], ws [N / 128, K / 128]."""
+    M, K = codes.shape
+    N = wc.shape[0]
+    x = codes.double() * spread(scales.double().t(), M, K, 1)
+    w = wc.double() * spread(ws.double(), N, K, 128)
+    return x @ w.t(), x.abs() @ w.abs().t()
+
+
+def matmul_tol(out, mag, K, dtype):
+    """Products of codes are exact.  A block's 128 are summed in fp32 in an unknown order (each addition may truncate: a whole
+    step), a block's scales and its addition are three roundings, the parts of a sum at most 32 more."""
+    return mag * (128 * 2 + 3 + blocks(K) + 32) * U + HALF[dtype] * out.abs() * (1 + 2.0 ** -6) + 2.0 ** -133
+
+
+def random_rows(g, M, K, dtype=torch.float32):
+    loud = torch.where(torch.rand(K, generator=g) < 0.02, 20.0, 1.0)
+    return (torch.randn(M, K, generator=g) * loud * torch.exp(0.5 * torch.randn(M, 1, generator=g))).to(dtype)
+
+
+def random_codes(g, M, K, scale, matrix=False, spreadx=3.0):
+    """Codes of all finite values and scales of any size (matrix: of [128 x 128] blocks, else block-major)."""
+    c = torch.randint(0, 254, (M, K), generator=g)
+    c = torch.where(c >= 127, c + 1, c).to(torch.uint8).view(torch.float8_e4m3fn)
+    shape = (blocks(M), blocks(K)) if matrix else (blocks(K), M)
+    if scale == "f32":
+        return c, torch.exp(spreadx * torch.randn(shape, generator=g)) * 0.01
+    return c, torch.randint(115, 130, shape, generator=g).to(torch.uint8).view(torch.float8_e8m0fnu)
+
+
+def finite_pow2(byte):
+    return math.ldexp(1.0, byte - 127)

@@ -1,0 +1,191 @@
+"""Rows and matrices into 8 bits against their 64-bit forms."""
+import pytest
+import torch
+
+import e4m3_ref as R
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+SHAPES = [(1, 16), (1, 128), (3, 144), (2, 1040), (33, 688), (5, 3584), (2, 25600), (130, 272)]
+
+
+@pytest.fixture(scope="module")
+def S():
+    from paper_2608_14787_amd import sdd
+    return sdd
+
+
+def gen(*seed):
+    g = torch.Generator()
+    g.manual_seed(hash(seed) & 0x7fffffff if not all(isinstance(s, int) for s in seed) else sum(s * 7919 ** i for i, s in enumerate(seed)) & 0x7fffffff)
+    return g
+
+
+def strided(x, pad):
+    """x in rows that lie `pad` elements further apart."""
+    big = torch.full((x.shape[0], x.shape[1] + pad), 3e5, dtype=x.dtype, device="cuda")
+    big[:, :x.shape[1]] = x.cuda()
+    return big[:, :x.shape[1]]
+
+
+def cpu(*ts):
+    return [None if t is None else t.cpu() for t in ts]
+
+
+@pytest.mark.parametrize("scale", ["f32", "e8m0"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K", SHAPES)
+def test_quantize(S, M, K, dtype, scale):
+    x = R.random_rows(gen(M, K), M, K, DT[dtype])
+    codes, scales = cpu(*S.e4m3_quantize(strided(x, 16), scale=scale))
+    R.check_codes(x.double(), codes, scales.t(), scale)
+
+
+@pytest.mark.parametrize("scale", ["f32", "e8m0"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,K", [(1, 16), (128, 128), (129, 144), (300, 688), (127, 1040), (257, 256)])
+def test_quantize_matrix(S, N, K, dtype, scale):
+    x = R.random_rows(gen(N, K, 1), N, K, DT[dtype])
+    codes, scales = cpu(*S.e4m3_quantize_matrix(strided(x, 8), scale=scale))
+    R.check_codes(x.double(), codes, scales, scale, high=128)
+
+
+def odd_values():
+    """Rows of 256: zeros, the largest and smallest numbers, values on rounding borders, infinities and NaN in one block."""
+    x = torch.zeros(12, 256)
+    x[1] = torch.linspace(-1, 1, 256)
+    x[2, :] = torch.finfo(torch.float32).max
+    x[3, 5] = 2.0 ** -149
+    x[4] = torch.linspace(-2.0 ** -130, 2.0 ** -127, 256)
+    x[5, 3], x[5, 130] = float("inf"), 2.5
+    x[6, 200], x[6, 4] = float("nan"), -7.0
+    x[7, 127], x[7, 128] = -float("inf"), 448.0
+    x[8] = torch.arange(256.0) + 0.5          # halves between codes
+    x[9] = 448.0 * 2.0 ** 100
+    x[10, ::3] = -0.0
+    x[11] = torch.where(torch.arange(256) % 2 == 0, 449.0, 1e-9)
+    return x
+
+
+@pytest.mark.parametrize("scale", ["f32", "e8m0"])
+def test_quantize_odd_values(S, scale):
+    x = odd_values()
+    codes, scales = cpu(*S.e4m3_quantize(x.cuda(), scale=scale))
+    R.check_codes(x.double(), codes, scales.t(), scale)
+    for row, lo in ((5, 128), (6, 0), (7, 128)):  # the other block of a row with an infinity or NaN
+        alone, s = cpu(*S.e4m3_quantize(x[row:row + 1, lo:lo + 128].contiguous().cuda(), scale=scale))
+        assert torch.equal(alone.view(torch.uint8)[0], codes.view(torch.uint8)[row, lo:lo + 128])
+        assert torch.equal(s[0].float(), scales[lo // 128, row:row + 1].float())
+
+
+def test_ties_to_even(S):
+    """Powers of two as scales make quotients exact: every border between two codes goes to the even one, as in torch."""
+    c = torch.arange(0, 126, dtype=torch.uint8).view(torch.float8_e4m3fn).double()
+    mid = (c[1:] + c[:-1]) / 2
+    x = torch.zeros(1, 128)
+    x[0, :125] = mid.float()
+    x[0, 127] = 448
+    codes, scales = cpu(*S.e4m3_quantize(x.cuda(), scale="e8m0"))
+    assert scales.float().item() == 1
+    assert torch.equal(codes.view(torch.uint8), x.to(torch.float8_e4m3fn).view(torch.uint8))
+
+
+@pytest.mark.parametrize("scale,res,y", [("f32", "f32", True), ("e8m0", "bf16", False), ("f32", None, True), ("e8m0", None, False),
+                                         ("f32", "bf16", True)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K", SHAPES + [(2, 16400), (1, 65536), (3, 40000)])
+def test_rmsnorm(S, M, K, dtype, scale, res, y):
+    g = gen(M, K, 2)
+    x = R.random_rows(g, M, K, DT[dtype])
+    gain = 1 + 0.1 * torch.randn(K, generator=g)
+    r = None if res is None else (4 * R.random_rows(g, M, K)).to(DT[res])
+    held = None if r is None else r.cuda()
+    codes, scales, ro, yo = S.e4m3_rmsnorm(strided(x, 8), gain.cuda(), eps=1e-6, residual=held, y=y, scale=scale)
+    assert ro is held  # in place
+    codes, scales, ro, yo = cpu(codes, scales, ro, yo)
+    wr, wy, rel_r, rel_y = R.rmsnorm(x, r, gain, 1e-6)
+    # where a residual cancels x, r is still off by half a step of itself only: the sum is rounded once
+    R.check_codes(wy, codes, scales.t(), scale, rel=rel_y)
+    if r is not None:
+        assert ((ro.double() - wr).abs() <= wr.abs() * (rel_r + R.HALF[DT[res]] * 1.01)).all()
+    if y:
+        assert ((yo.double() - wy).abs() <= wy.abs() * (rel_y + R.HALF[torch.bfloat16] * 1.01)).all()
+    else:
+        assert yo is None
+
+
+def test_rmsnorm_residual_out(S):
+    """Another output leaves the residual as it was; both ways give the same."""
+    g = gen(3)
+    x, r, gain = R.random_rows(g, 5, 400, torch.bfloat16).cuda(), R.random_rows(g, 5, 400).cuda(), torch.ones(400).cuda()
+    keep, to = r.clone(), torch.empty_like(r)
+    a = S.e4m3_rmsnorm(x, gain, residual=r, residual_out=to, y=True)
+    assert torch.equal(r, keep) and a[2] is to
+    b = S.e4m3_rmsnorm(x, gain, residual=r, y=torch.empty(5, 400, dtype=torch.bfloat16, device="cuda"))
+    assert torch.equal(r, to)
+    for s, t in zip(a, b):
+        assert torch.equal(s.view(torch.uint8) if s.dtype == torch.float8_e4m3fn else s, t.view(torch.uint8) if t.dtype == torch.float8_e4m3fn else t)
+
+
+def test_rmsnorm_bad_row_is_alone(S):
+    g = gen(4)
+    x, gain = R.random_rows(g, 6, 640), torch.ones(640)
+    want = S.e4m3_rmsnorm(x.cuda(), gain.cuda(), y=True)
+    x[2, 77], x[4, 600] = float("nan"), float("inf")
+    got = S.e4m3_rmsnorm(x.cuda(), gain.cuda(), y=True)
+    keep = torch.tensor([0, 1, 3, 5])
+    assert torch.equal(want[0].view(torch.uint8).cpu()[keep], got[0].view(torch.uint8).cpu()[keep])
+    assert torch.equal(want[1].cpu()[:, keep], got[1].cpu()[:, keep]) and torch.equal(want[3].cpu()[keep], got[3].cpu()[keep])
+    codes, scales = cpu(*got[:2])
+    assert torch.isnan(codes[2].float()).all() and (scales[:, 2] == 1).all()
+    # an infinity makes the root infinite: its own block is no number, the others are zeros
+    assert torch.isnan(codes[4, 512:].float()).all() and (codes[4, :512].float() == 0).all() and (scales[:, 4] == 1).all()
+
+
+def test_rmsnorm_zero_rows(S):
+    codes, scales, _, y = cpu(*S.e4m3_rmsnorm(torch.zeros(3, 160).cuda(), torch.ones(160).cuda(), y=True))
+    assert (codes.float() == 0).all() and (scales == 1).all() and (y == 0).all()
+
+
+@pytest.mark.parametrize("scale", ["f32", "e8m0"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K", SHAPES)
+def test_swiglu(S, M, K, dtype, scale):
+    g = gen(M, K, 5)
+    x = torch.cat([4 * torch.randn(M, K, generator=g), R.random_rows(g, M, K)], 1).to(DT[dtype])
+    codes, scales = cpu(*S.e4m3_swiglu(strided(x, 24), scale=scale))
+    y, rel, least = R.swiglu(x)
+    R.check_codes(y, codes, scales.t(), scale, rel=rel, least=least)
+
+
+def test_swiglu_far_gates(S):
+    """Gates whose exponential passes fp32's range either way, and infinities: zero, the gate itself, no number."""
+    x = torch.ones(1, 512)
+    x[0, :6] = torch.tensor([-1000.0, 1000.0, -90.0, 90.0, -87.0, 0.0])
+    x[0, 128], x[0, 200] = float("inf"), 3.0
+    codes, scales = cpu(*S.e4m3_swiglu(x.cuda()))
+    v = codes[0].float() * scales[:, 0].repeat_interleave(128)
+    assert v[0] == 0 and v[1] == 1000 and v[2] == 0 and abs(v[3] - 90) <= 90 * 2.0 ** -4 and v[5] == 0
+    assert torch.isnan(v[128:]).all()
+
+
+@pytest.mark.parametrize("M", [1, 33])
+def test_rows_do_not_depend_on_others(S, M):
+    g = gen(6)
+    x, gain = R.random_rows(g, 40, 1376, torch.bfloat16).cuda(), torch.ones(1376, device="cuda")
+    for f in (lambda t: S.e4m3_quantize(t), lambda t: S.e4m3_swiglu(t), lambda t: S.e4m3_rmsnorm(t, gain)[:2]):
+        whole, part = f(x), f(x[3:3 + M])
+        assert torch.equal(whole[0].view(torch.uint8)[3:3 + M], part[0].view(torch.uint8))
+        assert torch.equal(whole[1][:, 3:3 + M], part[1])
+
+
+def test_rows_given_outputs_and_stream(S):
+    g = gen(7)
+    x = R.random_rows(g, 9, 272, torch.bfloat16).cuda()
+    want = S.e4m3_quantize(x)
+    side = torch.cuda.Stream()
+    out = (torch.empty(9, 272, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(3, 9, device="cuda"))
+    side.wait_stream(torch.cuda.current_stream())
+    got = S.e4m3_quantize(x, out=out, stream=side)
+    side.synchronize()
+    assert got[0] is out[0] and torch.equal(got[0].view(torch.uint8), want[0].view(torch.uint8)) and torch.equal(got[1], want[1])
