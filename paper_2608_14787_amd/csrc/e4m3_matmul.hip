@@ -4,6 +4,8 @@
 // four columns of one output row and need one activation scale.  A block's 128 products are summed by the matrix cores from
 // zero and added to the accumulators in fp32 with the block's two scales.
 #include <algorithm>
+#include <cmath>
+#include <type_traits>
 
 #include "e4m3.h"
 #include "gemm.h"
@@ -200,27 +202,44 @@ __global__ void __launch_bounds__(kFewWaves * kWave, 2) few_rows_kernel(MatArgs 
 
 // ---- rows shared through LDS ------------------------------------------------------------------------------
 //
-// A workgroup takes 8 NT row tiles of the matrix, NT a wave, up to 16 MT rows, and a part of K.  The rows' codes pass through
-// LDS, CB blocks at a time in two buffers, so that they are read from L2 once a workgroup; a wave's own tiles go from memory to
-// registers, R - 1 blocks ahead.
+// A workgroup of 8 / GK x GK waves takes NT row tiles of the matrix a wave, all of up to 16 MT rows, and a part of K.  The rows'
+// codes pass through LDS, CB blocks of columns at a time in two buffers, so that they are read from L2 once a workgroup; a
+// wave's own tiles go from memory to registers, R - 1 blocks ahead.  Of a chunk's blocks each of the GK waves of a tile takes
+// every GK-th; they join in LDS, in their order.
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-template <int MT, int NT, int R, bool FP8, bool E8, bool F32>
-__global__ void __launch_bounds__(512, MT * NT <= 4 ? 4 : 2) shared_rows_kernel(MatArgs a) {
-  constexpr int CB = R, kThreads = 512, kRows = 16 * MT;
-  constexpr int PIECES = kRows * CB * 8 / kThreads;  // 16-byte pieces of a chunk a thread moves
-  static_assert(kRows * CB * 8 % kThreads == 0, "pieces of a chunk over the threads");
-  __shared__ __align__(16) u32x4 s_x[2][MT][CB][2][kWave];
-  __shared__ float s_xs[2][CB][kRows];
+constexpr int kSharedThreads = 512;
+
+template <int MT, int NT, int GK, bool FP8, bool E8, bool F32>
+__global__ void __launch_bounds__(kSharedThreads, 2) shared_rows_kernel(MatArgs a) {
+  constexpr int R = MT >= 8 ? 2 : 4;           // blocks of a wave in registers
+  constexpr int CB = GK == 8 ? 8 : MT >= 8 ? 2 : 4;  // blocks of a chunk
+  constexpr int SPC = CB / GK;                 // of them a wave's
+  constexpr int U = R / SPC;                   // chunks until a wave's registers come round
+  constexpr int GN = 8 / GK, kRows = 16 * MT;
+  constexpr bool AHEAD = U % 2 == 0;           // codes are asked for two chunks ahead, not one
+  static_assert(SPC >= 1 && SPC * U == R && (AHEAD || U == 1), "a wave's registers turn with the chunks");
+  constexpr int PIECES = kRows * CB * 8 / kSharedThreads;  // 16-byte pieces of a chunk a thread moves
+  static_assert(kRows * CB * 8 % kSharedThreads == 0, "pieces of a chunk over the threads");
+  constexpr int XS = (CB * kRows + kSharedThreads - 1) / kSharedThreads;
+  union Shared {
+    struct {
+      u32x4 x[2][MT][CB][2][kWave];
+      float xs[2][CB][kRows];
+    } in;
+    f32x4 part[GK > 1 ? 8 : 1][MT * NT][kWave];
+  };
+  __shared__ __align__(16) Shared s;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  const int groups = (a.NT + 8 * NT - 1) / (8 * NT);
+  const int wn = wave % GN, wk = wave / GN;
+  const int groups = (a.NT + GN * NT - 1) / (GN * NT);
   const int group = blockIdx.x % groups, rest = blockIdx.x / groups, split = rest % a.splits, m0 = rest / a.splits * kRows;
   const int k0 = split * a.per, n = min(a.KB, k0 + a.per) - k0;  // blocks of this part
   __amdgpu_buffer_rsrc_t rw[NT], rws[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    const int tile = min((group * 8 + wave) * NT + t, a.NT - 1);
+    const int tile = min((group * GN + wn) * NT + t, a.NT - 1);
     rw[t] = __builtin_amdgcn_make_buffer_rsrc((void*)(a.w + ((int64_t)tile * a.KB + k0) * kTile8), 0, n * kTile8, kBufferRsrcWord3);
     rws[t] = __builtin_amdgcn_make_buffer_rsrc((void*)(a.ws + (int64_t)(tile / 8) * a.KB + k0), 0, n * 4, kBufferRsrcWord3);
   }
@@ -230,44 +249,51 @@ __global__ void __launch_bounds__(512, MT * NT <= 4 ? 4 : 2) shared_rows_kernel(
     u32x4 w[NT][2];
     float ws[NT];
   };
-  auto load_w = [&](W& s, int i) {  // (blocks from n on: past the descriptors' ends)
+  auto load_w = [&](W& r, int step) {  // (blocks from n on: past the descriptors' ends)
+    const int i = step * GK + wk;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) s.w[t][h] = __builtin_amdgcn_raw_buffer_load_b128(rw[t], i * kTile8 + h * 1024 + lane * 16, 0, kNtCpol);
-      s.ws[t] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rws[t], i * 4, 0, 0));
+      for (int h = 0; h < 2; ++h) r.w[t][h] = __builtin_amdgcn_raw_buffer_load_b128(rw[t], i * kTile8 + h * 1024 + lane * 16, 0, kNtCpol);
+      r.ws[t] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rws[t], i * 4, 0, 0));
     }
   };
   // A chunk's codes: CB * 8 neighbouring threads take a row's 16-byte pieces; piece c of row r lies in its half's column c % 4
   // of the fragment, at place r ^ c % 8, which spreads a row's pieces over the banks.
   const int pc = threadIdx.x % (CB * 8), pr = threadIdx.x / (CB * 8);
-  constexpr int STEP = kThreads / (CB * 8);
-  u32x4 piece[PIECES];
-  float xscale[(CB * kRows + kThreads - 1) / kThreads];
-  auto load_x = [&](int i) {
+  constexpr int STEP = kSharedThreads / (CB * 8);
+  struct X {
+    u32x4 piece[PIECES];
+    float scale[XS];
+  };
+  auto load_x = [&](X& v, int i) {
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
       const int r = pr + p * STEP, k = (k0 + i) * kBlock8 + pc * 16;
-      piece[p] = __builtin_amdgcn_raw_buffer_load_b128(rx, i * 8 + pc < n * 8 && k < a.K && r < rows ? r * a.K + k : kNowhere, 0, 0);
+      int at = r * a.K + k;
+      at = i * 8 + pc < n * 8 && k < a.K && r < rows ? at : kNowhere;
+      asm volatile("" : "+v"(at));  // (a select, not a branch around the load)
+      v.piece[p] = __builtin_amdgcn_raw_buffer_load_b128(rx, at, 0, 0);
     }
 #pragma unroll
-    for (int p = 0; p < (CB * kRows + kThreads - 1) / kThreads; ++p) {
-      const int at = threadIdx.x + p * kThreads, kb = at / kRows, r = at % kRows;
+    for (int p = 0; p < XS; ++p) {
+      const int at = threadIdx.x + p * kSharedThreads, kb = at / kRows, r = at % kRows;
       const bool ok = kb < CB && i + kb < n;
-      xscale[p] = x_scale<E8>(a, ok ? k0 + i + kb : k0, m0 + min(r, rows - 1));
+      const float xs = x_scale<E8>(a, ok ? k0 + i + kb : k0, m0 + min(r, rows - 1));
+      v.scale[p] = ok ? xs : 0.f;
     }
   };
-  auto store_x = [&](int buf) {
+  auto store_x = [&](const X& v, int buf) {
     const int kb = pc / 8, h = pc / 4 % 2, g = pc % 4;
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
       const int r = pr + p * STEP;
-      s_x[buf][r / 16][kb][h][16 * g + ((r % 16) ^ (pc % 8))] = piece[p];
+      s.in.x[buf][r / 16][kb][h][16 * g + ((r % 16) ^ (pc % 8))] = v.piece[p];
     }
 #pragma unroll
-    for (int p = 0; p < (CB * kRows + kThreads - 1) / kThreads; ++p) {
-      const int at = threadIdx.x + p * kThreads;
-      if (at < CB * kRows) s_xs[buf][at / kRows][at % kRows] = xscale[p];
+    for (int p = 0; p < XS; ++p) {
+      const int at = threadIdx.x + p * kSharedThreads;
+      if (at < CB * kRows) s.in.xs[buf][at / kRows][at % kRows] = v.scale[p];
     }
   };
   f32x4 acc[MT][NT];
@@ -276,213 +302,501 @@ __global__ void __launch_bounds__(512, MT * NT <= 4 ? 4 : 2) shared_rows_kernel(
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int g4 = lane / 16, r16 = lane % 16;
-  auto multiply = [&](const W& s, int buf, int kb) {
+  // Row tiles go in groups of G: a group's fragments are read while the one before it is multiplied.
+  constexpr int G = MT <= 4 ? MT : MT % 4 == 0 ? 4 : 3;
+  static_assert(MT % G == 0, "whole groups");
+  struct F {
+    u32x4 x[G][2];
+    float xs[G];
+  };
+  auto read_x = [&](F& f, int buf, int kb, int g) {
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      u32x4 x[2];
+    for (int i = 0; i < G; ++i) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) x[h] = s_x[buf][i][kb][h][16 * g4 + (r16 ^ (4 * h + g4))];
-      const float xs = s_xs[buf][kb][i * 16 + r16];
-#pragma unroll
-      for (int j = 0; j < NT; ++j) {
-        f32x4 p = f32x4{0.f, 0.f, 0.f, 0.f};
-        if constexpr (FP8) {
-          const i32x8 wf = {(int)s.w[j][0][0], (int)s.w[j][0][1], (int)s.w[j][0][2], (int)s.w[j][0][3],
-                            (int)s.w[j][1][0], (int)s.w[j][1][1], (int)s.w[j][1][2], (int)s.w[j][1][3]};
-          const i32x8 xf = {(int)x[0][0], (int)x[0][1], (int)x[0][2], (int)x[0][3], (int)x[1][0], (int)x[1][1], (int)x[1][2], (int)x[1][3]};
-          p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf, xf, p, 0, 0, 0, 127, 0, 127);
-        } else {
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-              p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(s.w[j][h][2 * c], s.w[j][h][2 * c + 1]),
-                                                          widen(x[h][2 * c], x[h][2 * c + 1]), p, 0, 0, 0);
-        }
-        const float sc = xs * s.ws[j];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_fmaf(p[e], sc, acc[i][j][e]);
-      }
+      for (int h = 0; h < 2; ++h) f.x[i][h] = s.in.x[buf][g * G + i][kb][h][16 * g4 + (r16 ^ (4 * h + g4))];
+      f.xs[i] = s.in.xs[buf][kb][(g * G + i) * 16 + r16];
     }
+  };
+  auto multiply = [&](const W& r, int buf, int kb) {
+    F f[2];
+    read_x(f[0], buf, kb, 0);
+#pragma unroll
+    for (int g = 0; g < MT / G; ++g) {
+      if (g + 1 < MT / G) read_x(f[(g + 1) % 2], buf, kb, g + 1);
+      const F& v = f[g % 2];
+      f32x4 p[G][NT];
+#pragma unroll
+      for (int i = 0; i < G; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          p[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+          if constexpr (FP8) {
+            const i32x8 wf = {(int)r.w[j][0][0], (int)r.w[j][0][1], (int)r.w[j][0][2], (int)r.w[j][0][3],
+                              (int)r.w[j][1][0], (int)r.w[j][1][1], (int)r.w[j][1][2], (int)r.w[j][1][3]};
+            const i32x8 xf = {(int)v.x[i][0][0], (int)v.x[i][0][1], (int)v.x[i][0][2], (int)v.x[i][0][3],
+                              (int)v.x[i][1][0], (int)v.x[i][1][1], (int)v.x[i][1][2], (int)v.x[i][1][3]};
+            p[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf, xf, p[i][j], 0, 0, 0, 127, 0, 127);
+          }
+        }
+      if constexpr (!FP8) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            bf16x8 wf[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) wf[j] = widen(r.w[j][h][2 * c], r.w[j][h][2 * c + 1]);
+#pragma unroll
+            for (int i = 0; i < G; ++i) {
+              const bf16x8 xf = widen(v.x[i][h][2 * c], v.x[i][h][2 * c + 1]);
+#pragma unroll
+              for (int j = 0; j < NT; ++j) p[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[j], xf, p[i][j], 0, 0, 0);
+            }
+          }
+      }
+#pragma unroll
+      for (int i = 0; i < G; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          const float sc = v.xs[i] * r.ws[j];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[g * G + i][j][e] = __builtin_fmaf(p[i][j][e], sc, acc[g * G + i][j][e]);
+        }
+    }
+    // (the products stay in their step: unpinned, they are moved behind the loads and barriers of later ones)
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) asm volatile("" : "+v"(acc[i][j]));
   };
   auto turn = [&]() {  // a buffer is written, the other has been read
     __builtin_amdgcn_s_waitcnt(kWaitLgkm0);
     phase_barrier();
   };
+  // Loads return in their order, so that waiting for a chunk's codes means waiting for every tile that was asked for before
+  // them: AHEAD has more than a chunk of tiles in flight.
   W w[R];
-  load_x(0);
+  X xr[AHEAD ? 2 : 1];
+  load_x(xr[0], 0);
+  if constexpr (AHEAD) load_x(xr[1], CB);
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int i = 0; i < R - 1; ++i) {
     load_w(w[i], i);
     __builtin_amdgcn_sched_barrier(0);
   }
-  store_x(0);
+  store_x(xr[0], 0);
   turn();
-  int buf = 0;
-  for (int i = 0; i < n; i += CB) {
-    load_x(i + CB);
-    __builtin_amdgcn_sched_barrier(0);
+  const int chunks = (n + CB - 1) / CB;
+  for (int c = 0;;) {
 #pragma unroll
-    for (int j = 0; j < CB; ++j) {
-      load_w(w[(j + R - 1) % R], i + j + R - 1);
+    for (int u = 0; u < U; ++u) {
+      const int buf = AHEAD ? u % 2 : c % 2;
+      load_x(xr[AHEAD ? u % 2 : 0], (c + (AHEAD ? 2 : 1)) * CB);
       __builtin_amdgcn_sched_barrier(0);
-      if (i + j < n) multiply(w[j], buf, j);
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    store_x(buf ^ 1);
-    turn();
-    buf ^= 1;
-  }
 #pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const int tile = (group * 8 + wave) * NT + j, m = m0 + i * 16 + r16;
-      asm volatile("" : "+v"(acc[i][j]));
-      if (tile >= a.NT) continue;
-      if (a.splits > 1) {
-        if (m < a.M) *reinterpret_cast<f32x4*>(a.part + ((int64_t)split * a.M + m) * (a.NT * 16) + tile * 16 + g4 * 4) = acc[i][j];
-      } else {
-        store4<F32>(a, m, tile * 16 + g4 * 4, acc[i][j]);
+      for (int j = 0; j < SPC; ++j) {
+        const int slot = u * SPC + j;
+        load_w(w[(slot + R - 1) % R], c * SPC + j + R - 1);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(w[slot], buf, j * GK + wk);  // (behind the part's end: zeros times scales of zero)
+        __builtin_amdgcn_sched_barrier(0);
       }
+      store_x(xr[AHEAD ? (u + 1) % 2 : 0], buf ^ 1);
+      turn();
+      if (++c >= chunks) goto done;
     }
+  }
+done:
+  if constexpr (GK > 1) {  // (the buffers have been read: a barrier lies behind the last chunk)
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) s.part[wave][i * NT + j][lane] = acc[i][j];
+    __syncthreads();
+  }
+  auto put = [&](int i, int tile, int l, f32x4 v) {
+    const int m = m0 + i * 16 + l % 16, col = tile * 16 + l / 16 * 4;
+    if (tile >= a.NT) return;
+    if (a.splits > 1) {
+      if (m < a.M) *reinterpret_cast<f32x4*>(a.part + ((int64_t)split * a.M + m) * (a.NT * 16) + col) = v;
+    } else {
+      store4<F32>(a, m, col, v);
+    }
+  };
+  if constexpr (GK > 1) {
+    for (int item = threadIdx.x; item < GN * MT * NT * kWave; item += kSharedThreads) {
+      const int l = item % kWave, t = item / kWave % (MT * NT), g = item / (kWave * MT * NT);
+      f32x4 v = s.part[g][t][l];
+#pragma unroll
+      for (int k = 1; k < GK; ++k) v += s.part[k * GN + g][t][l];
+      put(t / NT, (group * GN + g) * NT + t % NT, l, v);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        asm volatile("" : "+v"(acc[i][j]));
+        put(i, (group * GN + wn) * NT + j, lane, acc[i][j]);
+      }
+  }
 }
 
-// Parts of sums, added in their order: a thread takes four columns of a row.
+// Parts of sums, added in their order: a thread takes four columns of a row, eight parts in flight at a time (one after the
+// other, six parts of 33 x 5120 took 4.8 us).
 template <bool F32>
 __global__ void __launch_bounds__(256) join_kernel(MatArgs a) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t m = i / (a.NT * 4);
-  if (m >= a.M) return;
-  const int n = (int)(i - m * (a.NT * 4)) * 4;
-  const float* p = a.part + m * (a.NT * 16) + n;
-  const int64_t step = (int64_t)a.M * (a.NT * 16);
-  f32x4 v = *reinterpret_cast<const f32x4*>(p);
-  for (int s = 1; s < a.splits; ++s) v += *reinterpret_cast<const f32x4*>(p + s * step);
-  if (n < a.N) store4<F32>(a, (int)m, n, v);
+  const int n = ((int)blockIdx.x * 256 + (int)threadIdx.x) * 4, m = blockIdx.y;
+  if (n >= a.N) return;
+  const int width = a.NT * 16;
+  const float* p = a.part + (int64_t)m * width + n;
+  const int64_t step = (int64_t)a.M * width;
+  f32x4 v = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < a.splits; s += 8) {
+    f32x4 q[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) q[u] = *reinterpret_cast<const f32x4*>(p + min(s + u, a.splits - 1) * step);
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (s + u < a.splits) v += q[u];
+  }
+  store4<F32>(a, m, n, v);
 }
 
 // ---- many rows --------------------------------------------------------------------------------------------
 //
-// A workgroup takes 128 rows of the matrix and 128 of the activations, through LDS a block of columns at a time; four waves
-// of 64 x 64.
+// A workgroup of GN x GM waves takes 16 WN GN rows of the matrix and 16 WM GM of the activations; both pass through LDS a block
+// of columns at a time, loaded there directly into the buffer that the products do not read.  Scales come eight blocks at a
+// time.
 
-template <bool E8, bool F32>
-__global__ void __launch_bounds__(256) many_rows_kernel(MatArgs a) {
-  __shared__ __align__(16) uint4 s_w[8][2][kWave], s_x[8][2][kWave];
+// 16 bytes a lane from descriptor rs at voffset + soffset to LDS at `to` + 16 lane.  Not the builtin: behind that the compiler
+// holds every LDS read back until all such loads have landed, those of the other buffer too.
+__device__ inline void load_direct(u32x4 rs, uint32_t to, int voffset, int soffset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(voffset), "s"(rs), "s"(soffset)
+               : "memory");
+}
+template <bool BYTE>  // a word a lane to `to` + 4 lane: four bytes of memory, or one
+__device__ inline void load_direct_word(u32x4 rs, uint32_t to, int voffset, int soffset) {
+  if constexpr (BYTE)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_ubyte %1, %2, %3 offen lds" ::"s"(to), "v"(voffset), "s"(rs), "s"(soffset)
+                 : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(to), "v"(voffset), "s"(rs), "s"(soffset)
+                 : "memory");
+}
+__device__ inline u32x4 descriptor(const void* p, int bytes) {
+  const uint64_t at = (uint64_t)p;
+  return u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)bytes, (uint32_t)kBufferRsrcWord3};
+}
+template <typename T>
+__device__ inline T uniform(T v) {
+  static_assert(sizeof(T) % 4 == 0, "words");
+  union {
+    T t;
+    int w[sizeof(T) / 4];
+  } u = {v};
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 4; ++i) u.w[i] = __builtin_amdgcn_readfirstlane(u.w[i]);
+  return u.t;
+}
+__device__ inline uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p; }
+__device__ inline i32x8 fragment(const u32x4& a, const u32x4& b) {
+  return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
+}
+
+constexpr int kStripe = 4;
+constexpr int kScaleSteps = 8;  // blocks whose scales lie in LDS at a time (in two halves)
+
+template <int WN, int WM, int GN, int GM, int RS, bool FP8, bool E8, bool F32>
+__global__ void __launch_bounds__(kWave * GN * GM, 2) many_rows_kernel(MatArgs a) {
+  constexpr int kWaves = GN * GM, kThreads = kWave * kWaves, BN = 16 * WN * GN, BM = 16 * WM * GM;
+  constexpr int LW = BN / 16 / kWaves, LX = BM / 8 / kWaves;  // KiB of a step that a wave loads, of each half of the tiles and of the rows
+  constexpr int HALF = WN / 2;                                // a wave's tiles of a half
+  static_assert(BN / 16 % kWaves == 0 && BM / 8 % kWaves == 0 && BN % 128 == 0 && WN % 2 == 0 && LX % 2 == 0, "a step's loads over the waves");
+  constexpr int kStage = (BN + BM) * kBlock8;
+  constexpr int LS = BM * kScaleSteps / kThreads;  // scale loads of a wave, for kScaleSteps blocks
+  static_assert(BM * kScaleSteps % kThreads == 0 && BM % 64 == 0 && BN / 128 * kScaleSteps <= kWave, "scales over the waves");
+  __shared__ __align__(16) char s_ring[RS * kStage];
+  __shared__ uint32_t s_xs[2][kScaleSteps][BM];
+  __shared__ float s_ws[2][kWave];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  const int n_blocks = (a.NT + 7) / 8;
-  const int bn = blockIdx.x % n_blocks, bm = blockIdx.x / n_blocks;
-  const int wn = wave % 2 * 4, wm = wave / 2 * 4;
-  f32x4 acc[4][4];
+  const int n_blocks = (a.NT * 16 + BN - 1) / BN, m_blocks = (a.M + BM - 1) / BM;
+  // Workgroups go to the XCDs in turn.  One XCD's, in their order: kStripe blocks of the matrix's rows, all blocks of the
+  // activations in turn, so that the 32 at work together share both in its L2 (one block of the matrix's rows at a time: 3% more).
+  const int low = blockIdx.x % kXcds, at = blockIdx.x / kXcds;
+  const int stripe = at / (kStripe * m_blocks), in = at - stripe * kStripe * m_blocks;
+  const int wide = min(kStripe, (n_blocks * a.splits + kXcds - 1) / kXcds - stripe * kStripe);
+  const int bm = in / wide, item = (stripe * kStripe + in - bm * wide) * kXcds + low;
+  if (item >= n_blocks * a.splits) return;
+  const int bn = item % n_blocks, split = item / n_blocks;
+  const int k0 = split * a.per, n = min(a.KB, k0 + a.per) - k0;
+  const int t0 = bn * (BN / 16), m0 = bm * BM;
+  const int tiles = min(BN / 16, a.NT - t0), rows = min(BM, a.M - m0);
+  const int w_blocks = (a.NT + 7) / 8;
+  const u32x4 rw = uniform(descriptor(a.w + (int64_t)t0 * a.KB * kTile8, tiles * a.KB * kTile8));
+  const u32x4 rx = uniform(descriptor(a.x + (int64_t)m0 * a.K, rows * a.K));
+  const uint32_t ring = lds_address(s_ring), at_xs = lds_address(s_xs), at_ws = lds_address(s_ws);
+  // rows of the activations lie in LDS as in memory, 128 bytes each, 16-byte piece c at place c ^ row % 8
+  int xrow[LX];
+  const int xpiece = (lane % 8) ^ (lane / 8);
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < LX; ++i) xrow[i] = min((wave * LX + i) * 8 + lane / 8, rows - 1) * a.K;
+  // The part's blocks behind its last one are loaded as the last again, so that the loads in flight are always as many.
+  auto issue_w = [&](int i, int half, int j) {  // load j of the first or the second half of each wave column's tiles
+    const int kb = k0 + min(i, n - 1);
+    const int b = wave * LW + j, t = b / 2 / HALF * WN + half * HALF + b / 2 % HALF;
+    load_direct(rw, ring + i % RS * kStage + t * kTile8 + b % 2 * 1024, lane * 16, (min(t, tiles - 1) * a.KB + kb) * kTile8 + b % 2 * 1024);
+  };
+  auto issue_x = [&](int i, int j) {
+    const int kb = k0 + min(i, n - 1);
+    // behind a row's end: its first codes again, which the matrix's stored zeros take out
+    const int k = kb * kBlock8 + xpiece * 16, kk = k < a.K ? k : 0;
+    load_direct(rx, ring + i % RS * kStage + BN * kBlock8 + (wave * LX + j) * 1024, xrow[j] + kk, 0);
+  };
+  // Loads of a half step, in their order: half of the rows of step i + RS, and the second tiles of step i + RS - 1 or the first
+  // ones of step i + RS, whose places have been read when the half step begins.
+  constexpr int LH = LX / 2 + LW;
+  auto issue = [&](int i, int half, int q) {
+    if (q < LX / 2)
+      issue_x(i + RS, half * (LX / 2) + q);
+    else
+      issue_w(i + RS - 1 + half, 1 - half, q - LX / 2);
+  };
+  auto issue_scales = [&](int i) {  // of blocks i .. i + kScaleSteps - 1
+    const int to = i / kScaleSteps % 2;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int kb = 0; kb < a.KB; ++kb) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int t = wave * 2 + i / 2, h = i % 2;
-      const int nt = min(bn * 8 + t, a.NT - 1);
-      s_w[t][h][lane] = load16(a.w + ((int64_t)nt * a.KB + kb) * kTile8 + h * 1024 + lane * 16);
-      const int m = min(bm * 128 + t * 16 + lane % 16, a.M - 1), k = kb * kBlock8 + h * 64 + lane / 16 * 16;
-      s_x[t][h][lane] = load16(a.x + (int64_t)m * a.K + (k < a.K ? k : 0));
+    for (int p = 0; p < LS; ++p) {
+      const int q = (wave * LS + p) * kWave, kb = min(k0 + i + q / BM, a.KB - 1);
+      const u32x4 rs = uniform(descriptor(reinterpret_cast<const char*>(a.xs) + ((int64_t)kb * a.M + m0) * (E8 ? 1 : 4), rows * (E8 ? 1 : 4)));
+      load_direct_word<E8>(rs, at_xs + (to * kScaleSteps * BM + q) * 4, min(q % BM + lane, rows - 1) * (E8 ? 1 : 4), 0);
     }
-    __syncthreads();
-    const float ws = a.ws[(int64_t)bn * a.KB + kb];
-    f32x4 p[4][4];
+    if (wave == 0) {
+      const int kb = min(k0 + i + lane / (BN / 128), a.KB - 1), nb = min(t0 / 8 + lane % (BN / 128), w_blocks - 1);
+      const u32x4 rs = uniform(descriptor(a.ws + (int64_t)(t0 / 8) * a.KB, min(w_blocks - t0 / 8, BN / 128) * a.KB * 4));
+      load_direct_word<false>(rs, at_ws + to * kWave * 4, ((nb - t0 / 8) * a.KB + kb) * 4, 0);
+    }
+  };
+  const int wn = wave % GN, wm = wave / GN, g4 = lane / 16, r16 = lane % 16;
+  f32x4 acc[WN][WM];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+  for (int i = 0; i < WN; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) p[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < WM; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  struct Rows {  // fragments of a wave's rows for a step, and the products of their scales with the matrix's
+    u32x4 x[WM][2];
+    float sc[WM];
+  };
+  const int p0 = (g4 ^ (r16 % 8)) * 16, p1 = ((4 + g4) ^ (r16 % 8)) * 16;
+  auto read_row = [&](Rows& r, int i, int j) {
+    const char* sx = s_ring + i % RS * kStage + BN * kBlock8 + ((wm * WM + j) * 16 + r16) * kBlock8;
+    r.x[j][0] = *reinterpret_cast<const u32x4*>(sx + p0);
+    r.x[j][1] = *reinterpret_cast<const u32x4*>(sx + p1);
+  };
+  auto read_scales = [&](Rows& r, int i) {
+    const int half = i / kScaleSteps % 2, step = i % kScaleSteps;
+    const float w1 = s_ws[half][step * (BN / 128) + wn * WN / 8];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint4 w[4], x[4];
+    for (int j = 0; j < WM; ++j) {
+      const uint32_t xs = s_xs[half][step][(wm * WM + j) * 16 + r16];
+      r.sc[j] = (E8 ? e8m0_value(xs) : __builtin_bit_cast(float, xs)) * w1;
+    }
+  };
+  u32x4 w[2][2];
+  auto read_tile = [&](u32x4* f, int i, int t) {
+    const u32x4* sw = reinterpret_cast<const u32x4*>(s_ring + i % RS * kStage) + (wn * WN + t) * 128 + lane;
+    f[0] = sw[0], f[1] = sw[64];
+  };
+  // The half of a step's products that the tiles I0 .. I0 + HALF - 1 have with its rows; meanwhile the next tile's fragments are
+  // read (the first one of the next half too), and in the second half the next step's rows.  A product's sums are added two
+  // products later: a wave issues in order, and would wait for the products just asked for.
+  constexpr int kLag = 2;
+  auto multiply = [&](int step, const Rows& r, Rows& next, auto half_c) {
+    constexpr int I0 = decltype(half_c)::value * HALF;
+    constexpr int EVERY = HALF * WM / LH;  // products between two loads
+    static_assert(EVERY >= 1, "loads between the products");
+    f32x4 p[kLag + 1];
+    auto add = [&](int t) {
+      f32x4& c = acc[I0 + t / WM][t % WM];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = s_w[wn + i][h][lane], x[i] = s_x[wm + i][h][lane];
+      for (int e = 0; e < 4; ++e) c[e] = __builtin_fmaf(p[t % (kLag + 1)][e], r.sc[t % WM], c[e]);
+      asm volatile("" : "+v"(c));
+    };
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+    for (int t = 0; t < HALF * WM; ++t) {
+      const int i = I0 + t / WM, j = t % WM;
+      if (j == 0) read_tile(w[(i + 1) % 2], step + (i + 1) / WN, (i + 1) % WN);
+      if (I0 > 0 && t % HALF == 0 && t / HALF < WM) read_row(next, step + 1, t / HALF);
+      if (I0 > 0 && t == HALF * WM / 2) read_scales(next, step + 1);
+      // (one at a time: together they fill the queue to memory, and the products behind them wait)
+      if (t % EVERY == EVERY / 2 && t / EVERY < LH) issue(step, I0 > 0, t / EVERY);
+      const u32x4* f = w[i % 2];
+      f32x4& q = p[t % (kLag + 1)];
+      q = f32x4{0.f, 0.f, 0.f, 0.f};
+      if constexpr (FP8) {
+        q = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fragment(f[0], f[1]), fragment(r.x[j][0], r.x[j][1]), q, 0, 0, 0, 127, 0, 127);
+      } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          p[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(w[j].x, w[j].y), widen(x[i].x, x[i].y), p[i][j], 0, 0, 0);
-          p[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(w[j].z, w[j].w), widen(x[i].z, x[i].w), p[i][j], 0, 0, 0);
-        }
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int c = 0; c < 2; ++c)
+            q = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(f[h][2 * c], f[h][2 * c + 1]), widen(r.x[j][h][2 * c], r.x[j][h][2 * c + 1]), q, 0, 0, 0);
+      }
+      if (t >= kLag) add(t - kLag);
+      __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float sc = ws * x_scale<E8>(a, kb, min(bm * 128 + (wm + i) * 16 + lane % 16, a.M - 1));
+    for (int t = HALF * WM - kLag; t < HALF * WM; ++t) add(t);
+  };
+  // All but a wave's newest `left` loads have landed, in every wave, and what was read before has been read; the compiler learns
+  // that LDS changed.
+  auto turn = [&](auto left_c) {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%1) lgkmcnt(0)\n\ts_barrier" ::"v"(ring), "i"(decltype(left_c)::value) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // A step in two halves of the tiles, a barrier before each.  What a half reads ahead has to have landed by its own barrier: the
+  // second half's first tile by that before the first half, the next step's rows and first tile by that before the second; each
+  // time that leaves the loads of 2 RS - 3 half steps on their way.
+  constexpr int kLeft = (2 * RS - 3) * LH;
+  static_assert(kLeft + LH < 64, "loads that the counter holds");
+  issue_scales(0);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+  for (int i = 0; i < RS; ++i) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_fmaf(p[i][j][e], sc, acc[i][j][e]);
-    }
-    __syncthreads();
+    for (int q = 0; q < (i ? LH : LX / 2); ++q) issue(i - RS, 0, q);
+#pragma unroll
+    for (int q = 0; q < LH; ++q) issue(i - RS, 1, q);
   }
+  Rows r0, r1;
+  turn(std::integral_constant<int, kLeft + LH>());
+  read_tile(w[0], 0, 0);
+  read_scales(r0, 0);
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
+  for (int j = 0; j < WM; ++j) read_row(r0, 0, j);
+  auto one_step = [&](int i, Rows& r, Rows& next) {
+    turn(std::integral_constant<int, kLeft>());
+    multiply(i, r, next, std::integral_constant<int, 0>());
+    turn(std::integral_constant<int, kLeft>());
+    if (i % kScaleSteps == 0) issue_scales(i + kScaleSteps);
+    multiply(i, r, next, std::integral_constant<int, 1>());
+  };
+  for (int i = 0;;) {
+    one_step(i, r0, r1);
+    if (++i >= n) break;
+    one_step(i, r1, r0);
+    if (++i >= n) break;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::"v"(ring) : "memory");  // (nothing is on its way to LDS that the next workgroup has)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int nt = bn * 8 + wn + j;
-      if (nt < a.NT) store4<F32>(a, bm * 128 + (wm + i) * 16 + lane % 16, nt * 16 + lane / 16 * 4, acc[i][j]);
+  for (int i = 0; i < WN; ++i)
+#pragma unroll
+    for (int j = 0; j < WM; ++j) {
+      const int tile = t0 + wn * WN + i, m = m0 + (wm * WM + j) * 16 + r16, col = tile * 16 + g4 * 4;
+      if (tile >= a.NT) continue;
+      if (a.splits > 1) {
+        if (m < a.M) *reinterpret_cast<f32x4*>(a.part + ((int64_t)split * a.M + m) * (a.NT * 16) + col) = acc[i][j];
+      } else {
+        store4<F32>(a, m, col, acc[i][j]);
+      }
     }
 }
 
 // How a product is computed: by the call's shape alone.
 struct Plan {
-  int kind;  // 0: few rows, 1: shared rows, 2: many rows
-  int mt, nt, splits, per;
+  enum Kind { kFew, kShared, kTile128, kTile128Deep, kTile256 } kind;
+  int mt, nt, gk;   // kFew, kShared
+  int splits, per;  // parts of K, blocks of one
 };
-Plan plan_of(int M, int NT, int KB) {
-  Plan p = {2, 8, 8, 1, KB};
-  if (M <= 16) {
-    p.kind = 0, p.mt = 1, p.nt = NT >= 512 ? 2 : 1;
-  } else if (M <= 256) {
-    p.kind = 1;
-    p.mt = M <= 32 ? 2 : M <= 48 ? 3 : M <= 64 ? 4 : M <= 128 ? 8 : 16;
-    p.nt = p.mt >= 8 || NT >= 2048 ? 2 : 1;
+
+// Rows of which all calls up to here are computed alike.
+int row_class(int M) { return M <= 64 ? (int)ceil_div(M, 16) * 16 : (int)std::min<int64_t>(ceil_div(M, 128) * 128, kMaxM8); }
+
+// Many rows: the tile and the parts of K with the least time by the steps that the busiest compute unit takes.  Measured, us a
+// step of 128 columns: tiles of 256 x 256 1.35 alone and 2.0 on a full device; of 128 x 128 with four waves (two workgroups a
+// compute unit) 0.80 alone, 0.88 with one everywhere, 1.17 with two; with eight waves and a deep ring 0.53 alone and 0.72.  The
+// matrix at 6 TB/s, parts written and read at 4.5, 4 us a launch.  Over 24 shapes of 200 to 1023 rows the choice is 1.4% from the best.
+Plan plan_many(int M, int NT, int KB, bool f32) {
+  Plan best = {Plan::kTile128, 0, 0, 0, 1, KB};
+  double least = 1e30;
+  const double stream = (double)NT * 16 * KB * kBlock8 / 6.0e6;
+  for (int kind = Plan::kTile128; kind <= Plan::kTile256; ++kind) {
+    const bool big = kind == Plan::kTile256, deep = kind == Plan::kTile128Deep;
+    if (big && f32) continue;
+    const double blocks = (double)ceil_div(NT, big ? 16 : 8) * ceil_div(M, big ? 256 : 128);
+    const double slots = big || deep ? 256 : 512, t1 = big ? 1.35 : deep ? 0.53 : 0.80, t2 = big ? 2.0 : deep ? 0.72 : 1.17;
+    for (int s = 1; s <= 8 && (s == 1 || (M <= 4096 && KB / s >= 4)); ++s) {
+      const int per = (int)ceil_div(KB, s), parts = (int)ceil_div(KB, per);
+      if (parts != s) continue;
+      const double wgs = blocks * parts, full = std::floor(wgs / slots), rest = wgs - full * slots;
+      const double last = big || deep ? t1 + (t2 - t1) * rest / slots : rest <= 128 ? t1 : rest <= 256 ? 0.88 : t2;
+      double t = std::max(per * (full * t2 + (rest > 0 ? last : 0)), stream) + 4;
+      if (parts > 1) t += 3 + (double)parts * M * NT * 16 * 8 / 4.5e6;
+      if (t < least) least = t, best = Plan{(Plan::Kind)kind, 0, 0, 0, parts, per};
+    }
+  }
+  return best;
+}
+Plan plan_of(int M, int NT, int KB, bool f32) {
+  M = row_class(M);
+  if (M <= 16) return Plan{Plan::kFew, 1, NT >= 512 ? 2 : 1, 1, 1, KB};
+  if (M > 128) return plan_many(M, NT, KB, f32);
+  Plan p = {Plan::kShared, M / 16, NT >= 2048 ? 2 : 1, 1, 1, KB};
+  if (M <= 64 && NT <= 512 && KB <= 32) {
+    p.gk = 4;
+  } else {
     const int groups = (int)ceil_div(NT, 8 * p.nt);
-    p.splits = std::max(1, std::min(256 / groups, KB / 4));
-    p.per = (int)ceil_div(KB, p.splits);
+    p.per = (int)ceil_div(KB, std::max(1, std::min(256 / groups, KB / 4)));
     p.splits = (int)ceil_div(KB, p.per);
   }
   return p;
 }
 size_t plan_bytes(const Plan& p, int M, int NT) { return p.splits > 1 ? (size_t)p.splits * M * NT * 16 * 4 : 0; }
 
-template <int MT, int NT, bool E8, bool F32>
+template <int MT, int NT, int GK, bool E8, bool F32>
 void launch_shared(const MatArgs& a, hipStream_t st) {
-  constexpr int R = MT >= 8 ? 2 : 4;
-  const unsigned grid = (unsigned)(ceil_div(a.NT, 8 * NT) * a.splits * ceil_div(a.M, 16 * MT));
-  hipLaunchKernelGGL((shared_rows_kernel<MT, NT, R, !F32, E8, F32>), dim3(grid), dim3(512), 0, st, a);
+  const unsigned grid = (unsigned)(ceil_div(a.NT, 8 / GK * NT) * a.splits * ceil_div(a.M, 16 * MT));
+  hipLaunchKernelGGL((shared_rows_kernel<MT, NT, GK, !F32, E8, F32>), dim3(grid), dim3(kSharedThreads), 0, st, a);
+}
+template <int MT, bool E8, bool F32>
+void launch_shared(const MatArgs& a, const Plan& p, hipStream_t st) {
+  if (p.nt == 2) return launch_shared<MT, 2, 1, E8, F32>(a, st);
+  if constexpr (MT < 8)
+    if (p.gk == 4) return launch_shared<MT, 1, 4, E8, F32>(a, st);
+  launch_shared<MT, 1, 1, E8, F32>(a, st);
+}
+template <int WN, int WM, int GN, int GM, int RS, bool E8, bool F32>
+void launch_many(const MatArgs& a, hipStream_t st) {
+  const int64_t items = ceil_div(a.NT, WN * GN) * a.splits, m_blocks = ceil_div(a.M, 16 * WM * GM);
+  hipLaunchKernelGGL((many_rows_kernel<WN, WM, GN, GM, RS, !F32, E8, F32>), dim3((unsigned)(ceil_div(items, kXcds) * kXcds * m_blocks)),
+                     dim3(kWave * GN * GM), 0, st, a);
 }
 template <bool E8, bool F32>
 int launch_matmul(MatArgs a, const Plan& p, hipStream_t st) {
   a.splits = p.splits;
   a.per = p.per;
-  if (p.kind == 0) {
-    if (p.nt == 2)
-      hipLaunchKernelGGL((few_rows_kernel<1, 2, E8, F32>), dim3((a.NT + 1) / 2), dim3(kFewWaves * kWave), 0, st, a);
-    else
-      hipLaunchKernelGGL((few_rows_kernel<1, 1, E8, F32>), dim3(a.NT), dim3(kFewWaves * kWave), 0, st, a);
-  } else if (p.kind == 1) {
-    switch (p.mt * 4 + p.nt) {
-      case 9: launch_shared<2, 1, E8, F32>(a, st); break;
-      case 13: launch_shared<3, 1, E8, F32>(a, st); break;
-      case 17: launch_shared<4, 1, E8, F32>(a, st); break;
-      case 33: launch_shared<8, 1, E8, F32>(a, st); break;
-      case 65: launch_shared<16, 1, E8, F32>(a, st); break;
-      case 10: launch_shared<2, 2, E8, F32>(a, st); break;
-      case 14: launch_shared<3, 2, E8, F32>(a, st); break;
-      case 18: launch_shared<4, 2, E8, F32>(a, st); break;
-      case 34: launch_shared<8, 2, E8, F32>(a, st); break;
-      default: launch_shared<16, 2, E8, F32>(a, st);
-    }
-    if (p.splits > 1)
-      hipLaunchKernelGGL((join_kernel<F32>), dim3((unsigned)ceil_div((int64_t)a.M * a.NT * 4, 256)), dim3(256), 0, st, a);
-  } else {
-    hipLaunchKernelGGL((many_rows_kernel<E8, F32>), dim3((a.NT + 7) / 8 * (unsigned)ceil_div(a.M, 128)), dim3(256), 0, st, a);
+  switch (p.kind) {
+    case Plan::kFew:
+      if (p.nt == 2)
+        hipLaunchKernelGGL((few_rows_kernel<1, 2, E8, F32>), dim3((a.NT + 1) / 2), dim3(kFewWaves * kWave), 0, st, a);
+      else
+        hipLaunchKernelGGL((few_rows_kernel<1, 1, E8, F32>), dim3(a.NT), dim3(kFewWaves * kWave), 0, st, a);
+      break;
+    case Plan::kShared:
+      switch (p.mt) {
+        case 2: launch_shared<2, E8, F32>(a, p, st); break;
+        case 3: launch_shared<3, E8, F32>(a, p, st); break;
+        case 4: launch_shared<4, E8, F32>(a, p, st); break;
+        default: launch_shared<8, E8, F32>(a, p, st);
+      }
+      break;
+    case Plan::kTile128: launch_many<4, 4, 2, 2, 2, E8, F32>(a, st); break;
+    case Plan::kTile128Deep: launch_many<4, 2, 2, 4, 4, E8, F32>(a, st); break;
+    case Plan::kTile256:
+      if constexpr (!F32) launch_many<8, 4, 2, 4, 2, E8, F32>(a, st);
   }
+  if (p.splits > 1)
+    hipLaunchKernelGGL((join_kernel<F32>), dim3((unsigned)ceil_div(a.NT, 64), (unsigned)a.M), dim3(256), 0, st, a);
   return check_launch("matmul");
 }
 
@@ -495,10 +809,14 @@ extern "C" int sdd_e4m3_matmul_workspace_bytes(const sdd_e4m3_matrix* m, int M, 
   SDD_REQUIRE(bytes != nullptr, "bytes is NULL");
   if (int rc = check_matrix(m)) return rc;
   SDD_REQUIRE(M > 0 && M <= kMaxM8, "bad row count %d", M);
-  // (fewer rows may be cut into more parts)
+  // (fewer rows may be cut into more parts; over 4096 are in one)
   const int NT = (int)ceil_div(m->N, 16), KB = (int)ceil_div(m->K, kBlock8);
-  *bytes = plan_bytes(plan_of(M, NT, KB), M, NT);
-  for (int rows = 16; rows < M && rows <= 4096; rows += 16) *bytes = std::max(*bytes, plan_bytes(plan_of(rows, NT, KB), rows, NT));
+  *bytes = 0;
+  for (int rows = 16;; rows = row_class(rows + 1)) {
+    const int r = std::min(rows, M);
+    for (int f32 = 0; f32 < 2; ++f32) *bytes = std::max(*bytes, plan_bytes(plan_of(r, NT, KB, f32), r, NT));
+    if (rows >= M || rows > 4096) break;
+  }
   return SDD_OK;
 }
 
@@ -527,7 +845,7 @@ extern "C" int sdd_e4m3_matmul(const sdd_e4m3_matrix* m, const uint8_t* x, const
   a.stride = (int64_t)out_stride;
   a.vec = (uintptr_t)out % (4 * es) == 0 && out_stride % 4 == 0;
   SDD_REQUIRE(ceil_div(a.NT, 8) * ceil_div(M, 128) < ((int64_t)1 << 31), "too many rows (%d of %d)", M, m->N);
-  const Plan p = plan_of(M, a.NT, a.KB);
+  const Plan p = plan_of(M, a.NT, a.KB, out_dtype == SDD_F32);
   const size_t need = plan_bytes(p, M, a.NT);
   if (need) {
     SDD_REQUIRE(ws && (uintptr_t)ws % 16 == 0, "workspace is NULL or not 16-byte aligned");

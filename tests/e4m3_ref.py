@@ -95,9 +95,9 @@ def group_max(codes, scales, wc, ws):
     N = wc.shape[0]
     x = (codes.double() * spread(scales.double().t(), M, K, 1)).abs()
     w = (wc.double() * spread(ws.double(), N, K, 128)).abs()
-    out = torch.zeros(M, N, dtype=torch.float64)
+    out = torch.zeros(M, N, dtype=torch.float64, device=codes.device)
     for k in range(0, K, 8):
-        big = torch.zeros(M, N, dtype=torch.float64)
+        big = torch.zeros_like(out)
         for i in range(k, k + 8):
             big = torch.maximum(big, x[:, i:i + 1] * w[:, i])
         out += big

@@ -20,11 +20,11 @@ def gen(*seed):
     return g
 
 
-def check(S, M, N, K, scale, out, seed=0, wscale=None):
+def check(S, M, N, K, scale, out, seed=0, wscale=None, where="cpu"):
     g = gen(M, N, K, seed)
-    x, xs = R.random_codes(g, M, K, scale)
-    w, ws = R.random_codes(g, N, K, wscale or scale, matrix=True)
-    got = S.E4M3Matrix(w.cuda(), ws.cuda()).matmul(x.cuda(), xs.cuda(), dtype=DT[out]).cpu()
+    x, xs = (t.to(where) for t in R.random_codes(g, M, K, scale))
+    w, ws = (t.to(where) for t in R.random_codes(g, N, K, wscale or scale, matrix=True))
+    got = S.E4M3Matrix(w.cuda(), ws.cuda()).matmul(x.cuda(), xs.cuda(), dtype=DT[out]).to(where)
     want, mag = R.matmul(x, xs, w, ws)
     tol = R.matmul_tol(want, mag, K, DT[out], R.group_max(x, xs, w, ws) if out == "bf16" else None)
     err = (got.double() - want).abs()
@@ -36,7 +36,8 @@ def check(S, M, N, K, scale, out, seed=0, wscale=None):
 @pytest.mark.parametrize("scale", ["f32", "e8m0"])
 @pytest.mark.parametrize("M,N,K", [
     (1, 1, 16), (1, 16, 128), (1, 300, 3584), (2, 17, 144), (9, 512, 256), (15, 15, 240), (16, 130, 1040), (17, 256, 688), (32, 33, 2064),
-    (33, 512, 1296), (33, 1040, 256), (48, 100, 400), (49, 47, 128), (64, 257, 1152), (1, 20000, 64), (5, 16400, 272)])
+    (33, 512, 1296), (33, 1040, 256), (48, 100, 400), (49, 47, 128), (64, 257, 1152), (1, 20000, 64), (5, 16400, 272), (40, 33000, 64),
+    (60, 20, 6000), (33, 600, 4240), (30, 9000, 272)])
 def test_few_rows(S, M, N, K, scale, out):
     check(S, M, N, K, scale, out)
 
@@ -45,9 +46,16 @@ def test_few_rows(S, M, N, K, scale, out):
 @pytest.mark.parametrize("scale", ["f32", "e8m0"])
 @pytest.mark.parametrize("M,N,K", [
     (65, 1, 16), (65, 128, 128), (66, 300, 1296), (100, 17, 2064), (127, 130, 144), (128, 256, 512), (129, 255, 640), (200, 513, 272),
-    (257, 384, 1040), (264, 640, 1280), (511, 112, 2368), (600, 700, 64)])
+    (257, 384, 1040), (264, 640, 1280), (511, 112, 2368), (600, 700, 64), (130, 20, 9008), (100, 33000, 144)])
 def test_many_rows(S, M, N, K, scale, out):
     check(S, M, N, K, scale, out)
+
+
+@pytest.mark.parametrize("scale,out", [("f32", "bf16"), ("e8m0", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("M,N,K", [(1500, 8200, 1168), (4100, 2100, 2064), (600, 33000, 144), (2048, 4096, 272), (511, 3600, 4752), (130, 33000, 48)])
+def test_large(S, M, N, K, scale, out):
+    """Sizes that take the large tiles (the reference in float64 on the GPU)."""
+    check(S, M, N, K, scale, out, where="cuda")
 
 
 @pytest.mark.parametrize("M", [5, 90])
@@ -144,7 +152,7 @@ def test_workspace_serves_fewer_rows(S):
     w, ws = R.random_codes(g, 500, 2064, "f32", matrix=True)
     m = S.E4M3Matrix(w.cuda(), ws.cuda())
     room = m.workspace(600)
-    for M in (1, 33, 64, 65, 100, 128, 129, 200, 256, 300, 511, 600):
+    for M in (1, 33, 64, 65, 100, 128, 129, 200, 256, 300, 511, 600):  # (cut into other parts)
         x, xs = (t.cuda() for t in R.random_codes(g, M, 2064, "f32"))
         assert torch.equal(m.matmul(x, xs, ws=room), m.matmul(x, xs))
 
