@@ -402,16 +402,16 @@ int sdd_e4m3_swiglu(const void* x, int dtype, size_t row_stride, int M, int K, u
  * columns 64 half + 16 g .. + 15 of row r, zeros behind the matrix's ends; then the
  * scales as fp32. */
 typedef struct {
-  int N, K; /* K a multiple of 16, at most 2^20; N at most 2^24 */
-  void* data; /* device */
+  int N, K;        /* K a multiple of 16, at most 2^20; N at most 2^24 */
+  int scale_dtype; /* of the scales that sdd_e4m3_matrix_load is given */
+  void* data;      /* device */
 } sdd_e4m3_matrix;
 
 /* Errors: SDD_EINVAL.  (m->data is not read.) */
 int sdd_e4m3_matrix_bytes(const sdd_e4m3_matrix* m, size_t* bytes);
 /* Lays row-major codes [N][K] (16-byte aligned) and scales out into m->data; they
  * may be freed when the stream is through. */
-int sdd_e4m3_matrix_load(const sdd_e4m3_matrix* m, const uint8_t* codes, const void* scales, int scale_dtype,
-                         sdd_stream_t stream);
+int sdd_e4m3_matrix_load(const sdd_e4m3_matrix* m, const uint8_t* codes, const void* scales, sdd_stream_t stream);
 
 /* Workspace of sdd_e4m3_matmul for calls of at most M rows on matrices of this
  * shape (0: none is needed).  It needs no initialization and carries nothing from one call to the next; calls that

@@ -508,7 +508,7 @@ __device__ inline i32x8 fragment(const u32x4& a, const u32x4& b) {
 constexpr int kStripe = 4;
 constexpr int kScaleSteps = 8;  // blocks whose scales lie in LDS at a time (in two halves)
 
-template <int WN, int WM, int GN, int GM, int RS, bool FP8, bool E8, bool F32>
+template <int WN, int WM, int GN, int GM, int RS, bool FP8, bool E8, bool SCALED, bool F32>
 __global__ void __launch_bounds__(kWave * GN * GM, 2) many_rows_kernel(MatArgs a) {
   constexpr int kWaves = GN * GM, kThreads = kWave * kWaves, BN = 16 * WN * GN, BM = 16 * WM * GM;
   constexpr int LW = BN / 16 / kWaves, LX = BM / 8 / kWaves;  // KiB of a step that a wave loads, of each half of the tiles and of the rows
@@ -586,6 +586,7 @@ __global__ void __launch_bounds__(kWave * GN * GM, 2) many_rows_kernel(MatArgs a
   struct Rows {  // fragments of a wave's rows for a step, and the products of their scales with the matrix's
     u32x4 x[WM][2];
     float sc[WM];
+    int xs[WM], ws;  // (SCALED: their bytes)
   };
   const int p0 = (g4 ^ (r16 % 8)) * 16, p1 = ((4 + g4) ^ (r16 % 8)) * 16;
   auto read_row = [&](Rows& r, int i, int j) {
@@ -596,10 +597,14 @@ __global__ void __launch_bounds__(kWave * GN * GM, 2) many_rows_kernel(MatArgs a
   auto read_scales = [&](Rows& r, int i) {
     const int half = i / kScaleSteps % 2, step = i % kScaleSteps;
     const float w1 = s_ws[half][step * (BN / 128) + wn * WN / 8];
+    if constexpr (SCALED) r.ws = (int)(__builtin_bit_cast(uint32_t, w1) >> 23 & 255);
 #pragma unroll
     for (int j = 0; j < WM; ++j) {
       const uint32_t xs = s_xs[half][step][(wm * WM + j) * 16 + r16];
-      r.sc[j] = (E8 ? e8m0_value(xs) : __builtin_bit_cast(float, xs)) * w1;
+      if constexpr (SCALED)
+        r.xs[j] = (int)xs;
+      else
+        r.sc[j] = (E8 ? e8m0_value(xs) : __builtin_bit_cast(float, xs)) * w1;
     }
   };
   u32x4 w[2][2];
@@ -631,6 +636,13 @@ __global__ void __launch_bounds__(kWave * GN * GM, 2) many_rows_kernel(MatArgs a
       // (one at a time: together they fill the queue to memory, and the products behind them wait)
       if (t % EVERY == EVERY / 2 && t / EVERY < LH) issue(step, I0 > 0, t / EVERY);
       const u32x4* f = w[i % 2];
+      if constexpr (SCALED) {
+        f32x4& c = acc[i][j];
+        c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fragment(f[0], f[1]), fragment(r.x[j][0], r.x[j][1]), c, 0, 0, 0, r.ws, 0, r.xs[j]);
+        asm volatile("" : "+v"(c));
+        __builtin_amdgcn_sched_barrier(0);
+        continue;
+      }
       f32x4& q = p[t % (kLag + 1)];
       q = f32x4{0.f, 0.f, 0.f, 0.f};
       if constexpr (FP8) {
@@ -645,6 +657,7 @@ __global__ void __launch_bounds__(kWave * GN * GM, 2) many_rows_kernel(MatArgs a
       if (t >= kLag) add(t - kLag);
       __builtin_amdgcn_sched_barrier(0);
     }
+    if constexpr (SCALED) return;
 #pragma unroll
     for (int t = HALF * WM - kLag; t < HALF * WM; ++t) add(t);
   };
@@ -765,13 +778,13 @@ void launch_shared(const MatArgs& a, const Plan& p, hipStream_t st) {
     if (p.gk == 4) return launch_shared<MT, 1, 4, E8, F32>(a, st);
   launch_shared<MT, 1, 1, E8, F32>(a, st);
 }
-template <int WN, int WM, int GN, int GM, int RS, bool E8, bool F32>
+template <int WN, int WM, int GN, int GM, int RS, bool E8, bool SCALED, bool F32>
 void launch_many(const MatArgs& a, hipStream_t st) {
   const int64_t items = ceil_div(a.NT, WN * GN) * a.splits, m_blocks = ceil_div(a.M, 16 * WM * GM);
-  hipLaunchKernelGGL((many_rows_kernel<WN, WM, GN, GM, RS, !F32, E8, F32>), dim3((unsigned)(ceil_div(items, kXcds) * kXcds * m_blocks)),
+  hipLaunchKernelGGL((many_rows_kernel<WN, WM, GN, GM, RS, !F32, E8, SCALED, F32>), dim3((unsigned)(ceil_div(items, kXcds) * kXcds * m_blocks)),
                      dim3(kWave * GN * GM), 0, st, a);
 }
-template <bool E8, bool F32>
+template <bool E8, bool SCALED, bool F32>
 int launch_matmul(MatArgs a, const Plan& p, hipStream_t st) {
   a.splits = p.splits;
   a.per = p.per;
@@ -790,10 +803,10 @@ int launch_matmul(MatArgs a, const Plan& p, hipStream_t st) {
         default: launch_shared<8, E8, F32>(a, p, st);
       }
       break;
-    case Plan::kTile128: launch_many<4, 4, 2, 2, 2, E8, F32>(a, st); break;
-    case Plan::kTile128Deep: launch_many<4, 2, 2, 4, 4, E8, F32>(a, st); break;
+    case Plan::kTile128: launch_many<4, 4, 2, 2, 2, E8, SCALED, F32>(a, st); break;
+    case Plan::kTile128Deep: launch_many<4, 2, 2, 4, 4, E8, SCALED, F32>(a, st); break;
     case Plan::kTile256:
-      if constexpr (!F32) launch_many<8, 4, 2, 4, 2, E8, F32>(a, st);
+      if constexpr (!F32) launch_many<8, 4, 2, 4, 2, E8, SCALED, F32>(a, st);
   }
   if (p.splits > 1)
     hipLaunchKernelGGL((join_kernel<F32>), dim3((unsigned)ceil_div(a.NT, 64), (unsigned)a.M), dim3(256), 0, st, a);
@@ -855,10 +868,13 @@ extern "C" int sdd_e4m3_matmul(const sdd_e4m3_matrix* m, const uint8_t* x, const
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   prof_begin(PROF_GEMM8, st);
   int rc;
-  if (scale_dtype == SDD_E8M0)
-    rc = out_dtype == SDD_F32 ? launch_matmul<true, true>(a, p, st) : launch_matmul<true, false>(a, p, st);
+  const bool e8 = scale_dtype == SDD_E8M0;
+  if (out_dtype == SDD_F32)
+    rc = e8 ? launch_matmul<true, false, true>(a, p, st) : launch_matmul<false, false, true>(a, p, st);
+  else if (e8 && m->scale_dtype == SDD_E8M0)
+    rc = launch_matmul<true, true, false>(a, p, st);
   else
-    rc = out_dtype == SDD_F32 ? launch_matmul<false, true>(a, p, st) : launch_matmul<false, false>(a, p, st);
+    rc = e8 ? launch_matmul<true, false, false>(a, p, st) : launch_matmul<false, false, false>(a, p, st);
   prof_end(PROF_GEMM8, st);
   return rc;
 }

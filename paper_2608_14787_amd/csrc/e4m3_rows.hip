@@ -322,6 +322,7 @@ int check_matrix(const sdd_e4m3_matrix* m) {
   SDD_REQUIRE(m != nullptr, "matrix description is NULL");
   SDD_REQUIRE(m->N > 0 && m->N <= kMaxN8 && m->K > 0 && m->K <= kMaxK8 && m->K % 16 == 0,
               "bad matrix [%d][%d] (K a multiple of 16, at most 2^20; N at most 2^24)", m->N, m->K);
+  SDD_REQUIRE(m->scale_dtype == SDD_F32 || m->scale_dtype == SDD_E8M0, "a matrix's scales must be fp32 or E8M0 (dtype %d)", m->scale_dtype);
   return SDD_OK;
 }
 
@@ -392,13 +393,11 @@ extern "C" int sdd_e4m3_matrix_bytes(const sdd_e4m3_matrix* m, size_t* bytes) {
   return SDD_OK;
 }
 
-extern "C" int sdd_e4m3_matrix_load(const sdd_e4m3_matrix* m, const uint8_t* codes, const void* scales, int scale_dtype,
-                                    sdd_stream_t stream) {
+extern "C" int sdd_e4m3_matrix_load(const sdd_e4m3_matrix* m, const uint8_t* codes, const void* scales, sdd_stream_t stream) {
   if (int rc = check_matrix(m)) return rc;
   SDD_REQUIRE(m->data && codes && scales, "NULL pointer");
-  SDD_REQUIRE(scale_dtype == SDD_F32 || scale_dtype == SDD_E8M0, "scales must be fp32 or E8M0 (dtype %d)", scale_dtype);
   SDD_REQUIRE((uintptr_t)m->data % 256 == 0 && aligned16(codes), "the matrix must be 256-byte aligned, its codes 16-byte");
-  SDD_REQUIRE(scale_dtype == SDD_E8M0 || (uintptr_t)scales % 4 == 0, "scales must be 4-byte aligned");
+  SDD_REQUIRE(m->scale_dtype == SDD_E8M0 || (uintptr_t)scales % 4 == 0, "scales must be 4-byte aligned");
   const int KB = (int)ceil_div(m->K, kBlock8);
   const int64_t n = matrix_code_bytes(m) / 16, ns = ceil_div(m->N, kBlock8) * KB;
   SDD_REQUIRE(n / 256 < ((int64_t)1 << 31) - 1, "matrix [%d][%d] is too large", m->N, m->K);
@@ -406,7 +405,7 @@ extern "C" int sdd_e4m3_matrix_load(const sdd_e4m3_matrix* m, const uint8_t* cod
   prof_begin(PROF_ROWS8, st);
   hipLaunchKernelGGL(load_codes_kernel, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, codes, reinterpret_cast<uint4*>(m->data),
                      m->N, m->K, KB, n);
-  hipLaunchKernelGGL(load_scales_kernel, dim3((unsigned)ceil_div(ns, 256)), dim3(256), 0, st, scales, scale_dtype == SDD_E8M0,
+  hipLaunchKernelGGL(load_scales_kernel, dim3((unsigned)ceil_div(ns, 256)), dim3(256), 0, st, scales, m->scale_dtype == SDD_E8M0,
                      reinterpret_cast<float*>(reinterpret_cast<char*>(m->data) + matrix_code_bytes(m)), ns);
   prof_end(PROF_ROWS8, st);
   return check_launch("load_codes_kernel");

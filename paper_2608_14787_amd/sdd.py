@@ -89,7 +89,7 @@ _SIGS = {
     "sdd_e4m3_rmsnorm": (I, [P, I, SZ, P, P, I, P, F, I, I, P, P, I, P, P]),
     "sdd_e4m3_swiglu": (I, [P, I, SZ, I, I, P, P, I, P]),
     "sdd_e4m3_matrix_bytes": (I, [P, P]),
-    "sdd_e4m3_matrix_load": (I, [P, P, P, I, P]),
+    "sdd_e4m3_matrix_load": (I, [P, P, P, P]),
     "sdd_e4m3_matmul_workspace_bytes": (I, [P, I, P]),
     "sdd_e4m3_matmul": (I, [P, P, P, I, I, P, I, SZ, P, SZ, P]),
     "sdd_profile_start": (I, [C.c_uint, I, I]),
@@ -624,7 +624,7 @@ def e4m3_rmsnorm(x: torch.Tensor, gain: torch.Tensor, *, eps: float = 1e-6, resi
 
 
 class MatrixDesc(C.Structure):
-    _fields_ = [("N", C.c_int), ("K", C.c_int), ("data", P)]
+    _fields_ = [("N", C.c_int), ("K", C.c_int), ("scale_dtype", C.c_int), ("data", P)]
 
 
 class E4M3Matrix:
@@ -638,13 +638,13 @@ class E4M3Matrix:
         _need(scales.is_contiguous() and tuple(scales.shape) == (-(-N // 128), -(-K // 128)),
               "scales must be contiguous [ceil(N / 128), ceil(K / 128)]")
         self.shape = (N, K)
-        self.desc = MatrixDesc(N, K, None)
+        self.desc = MatrixDesc(N, K, sd, None)
         n = _size_out(lib().sdd_e4m3_matrix_bytes, C.byref(self.desc))
         with torch.cuda.stream(stream):  # (None: the current one)
             self.buf = codes.new_empty(n, dtype=torch.uint8)
             self.desc.data = self.buf.data_ptr()
             st = _here(codes, scales, self.buf)
-            _check(lib().sdd_e4m3_matrix_load(C.byref(self.desc), codes.data_ptr(), scales.data_ptr(), sd, st))
+            _check(lib().sdd_e4m3_matrix_load(C.byref(self.desc), codes.data_ptr(), scales.data_ptr(), st))
         self._desc = C.byref(self.desc)
 
     def workspace(self, max_rows: int) -> torch.Tensor:

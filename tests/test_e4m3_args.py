@@ -55,13 +55,13 @@ def test_rmsnorm_rows_too_long(S):  # noqa: F811
                                       ((1 << 24) + 1, 16, -1), (16, 0, -1), (16, 24, -1), (16, (1 << 20) + 16, -1), (16, -16, -1)])
 def test_matrix_shapes(S, N, K, code):  # noqa: F811
     out = C.c_size_t(77)
-    d = S.MatrixDesc(N, K, None)
+    d = S.MatrixDesc(N, K, S.F32, None)
     assert S.lib().sdd_e4m3_matrix_bytes(C.byref(d), C.byref(out)) == code
     if code == 0:
         kb, scales = -(-K // 128), -(-N // 128) * -(-K // 128) * 4
         assert out.value == -(-N // 16) * kb * 2048 + -(-scales // 256) * 256
     assert S.lib().sdd_e4m3_matrix_bytes(None, C.byref(out)) == S.EINVAL
-    assert S.lib().sdd_e4m3_matrix_bytes(C.byref(S.MatrixDesc(16, 16, None)), None) == S.EINVAL
+    assert S.lib().sdd_e4m3_matrix_bytes(C.byref(S.MatrixDesc(16, 16, S.F32, None)), None) == S.EINVAL
 
 
 @pytest.mark.parametrize("kw", [dict(data=None), dict(codes=None), dict(scales=None), dict(sd=1), dict(sd=2), dict(data=A + 128), dict(codes=A + 8),
@@ -69,19 +69,19 @@ def test_matrix_shapes(S, N, K, code):  # noqa: F811
 def test_matrix_load_refusals(S, kw):  # noqa: F811
     a = dict(N=100, K=256, data=A, codes=A, scales=A, sd=S.F32)
     a.update(kw)
-    d = S.MatrixDesc(a["N"], a["K"], a["data"])
-    assert S.lib().sdd_e4m3_matrix_load(C.byref(d), a["codes"], a["scales"], a["sd"], None) == S.EINVAL, kw
+    d = S.MatrixDesc(a["N"], a["K"], a["sd"], a["data"])
+    assert S.lib().sdd_e4m3_matrix_load(C.byref(d), a["codes"], a["scales"], None) == S.EINVAL, kw
 
 
 def matmul(S, **kw):  # noqa: F811
-    a = dict(N=100, K=256, data=A, x=A, xs=A, sd=S.F32, M=7, out=A, od=S.BF16, stride=100, ws=A, n=1 << 40)
+    a = dict(N=100, K=256, wd=S.F32, data=A, x=A, xs=A, sd=S.F32, M=7, out=A, od=S.BF16, stride=100, ws=A, n=1 << 40)
     a.update(kw)
-    d = S.MatrixDesc(a["N"], a["K"], a["data"])
+    d = S.MatrixDesc(a["N"], a["K"], a["wd"], a["data"])
     return S.lib().sdd_e4m3_matmul(C.byref(d), a["x"], a["xs"], a["sd"], a["M"], a["out"], a["od"], a["stride"], a["ws"], a["n"], None)
 
 
 @pytest.mark.parametrize("kw", [
-    dict(data=None), dict(x=None), dict(xs=None), dict(out=None), dict(sd=1), dict(sd=2), dict(M=0), dict(M=-3), dict(M=(1 << 24) + 1), dict(od=2),
+    dict(data=None), dict(x=None), dict(xs=None), dict(out=None), dict(wd=1), dict(wd=2), dict(sd=1), dict(sd=2), dict(M=0), dict(M=-3), dict(M=(1 << 24) + 1), dict(od=2),
     dict(od=3), dict(stride=99), dict(stride=0), dict(stride=1 << 40), dict(data=A + 64), dict(x=A + 8), dict(out=A + 1), dict(out=A + 2, od=0),
     dict(xs=A + 1), dict(N=0), dict(K=17), dict(N=1 << 24, M=1 << 24, stride=1 << 24)])
 def test_matmul_refusals(S, kw):  # noqa: F811
@@ -92,14 +92,14 @@ def test_matmul_workspace(S):  # noqa: F811
     """More rows never need less; sizes asked for without a device."""
     out = C.c_size_t()
     for N, K in ((4608, 3584), (5120, 25600), (51200, 5120), (3584, 18944), (100, 16), (17, 4096)):
-        d = S.MatrixDesc(N, K, None)
+        d = S.MatrixDesc(N, K, S.F32, None)
         last = 0
         for M in (1, 16, 33, 64, 65, 100, 128, 129, 264, 511, 1000, 4095, 100000):
             assert S.lib().sdd_e4m3_matmul_workspace_bytes(C.byref(d), M, C.byref(out)) == S.OK
             assert out.value >= last
             last = out.value
-    d = S.MatrixDesc(100, 256, None)
-    for args in ((None, 5, C.byref(out)), (C.byref(d), 0, C.byref(out)), (C.byref(d), 5, None), (C.byref(S.MatrixDesc(100, 250, None)), 5, C.byref(out))):
+    d = S.MatrixDesc(100, 256, S.E8M0, None)
+    for args in ((None, 5, C.byref(out)), (C.byref(d), 0, C.byref(out)), (C.byref(d), 5, None), (C.byref(S.MatrixDesc(100, 250, S.F32, None)), 5, C.byref(out))):
         assert S.lib().sdd_e4m3_matmul_workspace_bytes(*args) == S.EINVAL
 
 
