@@ -2,9 +2,9 @@
 // a residual's addition and an RMS norm, or after SwiGLU, and of matrices in blocks of 128 x 128.
 //
 // A block y with a = max |y|: s = max(a / 448, 2^-126), or the least power of two with a <= 448 s; codes = e4m3(y / s).  The
-// quotient is a product with 1 / s (exact for powers of two; otherwise off by an fp32 rounding before the one to 3 bits).
-// Bound: the memory, and for few rows the chain load, sum, maximum, store.  A lane holds 16 consecutive columns (16 bytes of
-// codes; 32 or 64 of input), eight lanes a block: its maximum is three steps inside a row of lanes, and no value changes lanes.
+// quotient is fp32's.
+// Bound: the memory, and for few rows the chain load, sum, maximum, store.  A lane holds 16 or 8 consecutive columns, 8 or 16
+// lanes a block: its maximum is a few steps inside a row of lanes, and no value changes lanes.
 #include <algorithm>
 
 #include "e4m3.h"
@@ -12,42 +12,62 @@
 namespace sdd {
 namespace {
 
-constexpr int kPer = 16;                    // columns of a lane
-constexpr int kLanes = kBlock8 / kPer;      // lanes of a block
-constexpr int kWaveCols = kWave * kPer;     // columns of a wave
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+// Columns of a lane.  16: its codes are 16 bytes; rows of quantize and SwiGLU, matrices.  8: its bf16 values are, and its fp32
+// values 32; the norm, which moves up to four times the codes' bytes in other types.
 constexpr int kMaxNormThreads = 1024, kMaxNormK = 65536;
 
-template <typename T>
-struct Raw {  // 16 elements as they lie in memory
-  uint4 v[sizeof(T)];
+template <typename T, int P>
+struct Raw {  // P elements as they lie in memory
+  static constexpr int N = P * (int)sizeof(T) / 16;
+  uint4 v[N];
   __device__ inline void load(const T* p) {
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T); ++i) v[i] = load16(reinterpret_cast<const char*>(p) + 16 * i);
+    for (int i = 0; i < N; ++i) v[i] = load16(reinterpret_cast<const char*>(p) + 16 * i);
   }
   __device__ inline void zero() {
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T); ++i) v[i] = make_uint4(0, 0, 0, 0);
+    for (int i = 0; i < N; ++i) v[i] = make_uint4(0, 0, 0, 0);
   }
   __device__ inline void values(float* y) const {
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T); ++i) unpack16(v[i], y + i * (16 / sizeof(T)), T());
+    for (int i = 0; i < N; ++i) unpack16(v[i], y + i * (16 / sizeof(T)), T());
   }
 };
+template <typename T, int P>
+__device__ inline void store_values(T* p, const float* y) {
+  constexpr int E = 16 / sizeof(T);
+#pragma unroll
+  for (int i = 0; i < P / E; ++i) {
+    const float* v = y + i * E;
+    uint4 w;
+    if constexpr (sizeof(T) == 2)
+      w = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+    else
+      w = make_uint4(__builtin_bit_cast(uint32_t, v[0]), __builtin_bit_cast(uint32_t, v[1]), __builtin_bit_cast(uint32_t, v[2]),
+                     __builtin_bit_cast(uint32_t, v[3]));
+    reinterpret_cast<uint4*>(p)[i] = w;
+  }
+}
 
 // max |y|, or infinity where a value is not finite
-__device__ inline float amax16(const float* y) {
+template <int P>
+__device__ inline float amax_of(const float* y) {
   float m = 0.f, z = 0.f;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
+  for (int i = 0; i < P; ++i) {
     m = fmaxf(m, fabsf(y[i]));
     z = __builtin_fmaf(y[i], 0.f, z);  // 0 for finite values, NaN otherwise
   }
   return z == 0.f ? m : INFINITY;
 }
-__device__ inline float amax_block(float m) {  // over the eight lanes of a block
+template <int P>
+__device__ inline float amax_block(float m) {  // over the 128 / P lanes of a block
   m = fmaxf(m, dpp_f<kDppXor1>(m));
   m = fmaxf(m, dpp_f<kDppXor2>(m));
-  return fmaxf(m, dpp_f<kDppHalfMirror>(m));
+  m = fmaxf(m, dpp_f<kDppHalfMirror>(m));
+  return P == 16 ? m : fmaxf(m, dpp_f<kDppMirror>(m));
 }
 
 struct Scale {
@@ -63,17 +83,33 @@ __device__ inline Scale scale_of(float a, bool e8) {
     const uint32_t u = __builtin_bit_cast(uint32_t, a);
     const int x = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u);
     const int byte = max(1, min(254, x + 127));
-    return Scale{__builtin_bit_cast(float, byte == 254 ? 0x00400000u : (uint32_t)(254 - byte) << 23), 0.f, byte};
+    return Scale{__builtin_bit_cast(float, byte == 254 ? 0x00400000u : (uint32_t)(254 - byte) << 23),
+                 __builtin_bit_cast(float, (uint32_t)byte << 23), byte};
   }
   const float s = fmaxf(a / 448.f, 0x1p-126f);
   return Scale{1.f / s, s, 0};
 }
-__device__ inline uint4 encode16(const float* y, float inv) {
-  if (inv != inv) return make_uint4(0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu);
-  uint32_t w[4];
+// P codes of y / s, stored past the caches (they are not read again before the product, and 100 to 300 MB of rows take 5 to 15%
+// less time so).  The quotient is a product with 1 / s
+// corrected by its remainder, as fp32's division rounds it.
+template <int P>
+__device__ inline void store_codes(uint8_t* to, const float* y, const Scale& sc) {
+  uint32_t w[P / 4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = codes4(y[4 * i] * inv, y[4 * i + 1] * inv, y[4 * i + 2] * inv, y[4 * i + 3] * inv);
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  for (int i = 0; i < P / 4; ++i) {
+    float q[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float v = y[4 * i + j];
+      q[j] = v * sc.inv;
+      q[j] = __builtin_fmaf(__builtin_fmaf(-q[j], sc.s, v), sc.inv, q[j]);
+    }
+    w[i] = sc.inv != sc.inv ? 0x7f7f7f7fu : codes4(q[0], q[1], q[2], q[3]);
+  }
+  if constexpr (P == 16)
+    __builtin_nontemporal_store(u32x4{w[0], w[1], w[2], w[3]}, reinterpret_cast<u32x4*>(to));
+  else
+    __builtin_nontemporal_store(u32x2{w[0], w[1]}, reinterpret_cast<u32x2*>(to));
 }
 __device__ inline void store_scale(void* scales, bool e8, int64_t i, const Scale& sc) {
   if (e8)
@@ -97,81 +133,77 @@ struct RowsArgs {
   float eps;
 };
 
-// The lane's 16 columns from `col` of row m, y, to codes; the first lane of a block stores its scale.
+// The lane's P columns from `col` of row m, y, to codes; the first lane of a block stores its scale.
+template <int P>
 __device__ inline void store_rows(const RowsArgs& a, int64_t m, int col, const float* y) {
-  const Scale sc = scale_of(amax_block(amax16(y)), a.e8);
+  const Scale sc = scale_of(amax_block<P>(amax_of<P>(y)), a.e8);
   if (col >= a.K) return;
-  *reinterpret_cast<uint4*>(a.codes + m * a.K + col) = encode16(y, sc.inv);
+  store_codes<P>(a.codes + m * a.K + col, y, sc);
   if (col % kBlock8 == 0) store_scale(a.scales, a.e8, (int64_t)(col / kBlock8) * a.M + m, sc);
 }
 
 // Rows as they are, or after SwiGLU: a wave takes 1024 columns of a row.
 template <typename T, bool SWIGLU>
 __global__ void __launch_bounds__(256) rows_kernel(RowsArgs a, int segs) {
+  constexpr int P = 16;
   const int lane = threadIdx.x % kWave;
   const int64_t item = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
   const int64_t m = item / segs;
   if (m >= a.M) return;
-  const int col = (int)(item - m * segs) * kWaveCols + lane * kPer;
+  const int col = ((int)(item - m * segs) * kWave + lane) * P;
   const T* x = reinterpret_cast<const T*>(a.x) + m * a.stride + col;
-  Raw<T> r, u;
+  Raw<T, P> r, u;
   r.zero(), u.zero();
   if (col < a.K) {
     r.load(x);
     if constexpr (SWIGLU) u.load(x + a.K);
   }
-  float y[kPer];
+  float y[P];
   r.values(y);
   if constexpr (SWIGLU) {
-    float up[kPer];
+    float up[P];
     u.values(up);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) y[i] = y[i] * __builtin_amdgcn_rcpf(1.f + __expf(-y[i])) * up[i];
+    for (int i = 0; i < P; ++i) y[i] = y[i] * __builtin_amdgcn_rcpf(1.f + __expf(-y[i])) * up[i];
   }
-  store_rows(a, m, col, y);
+  store_rows<P>(a, m, col, y);
 }
 
-// A workgroup takes a row, C vectors of 16 columns a thread, kept in registers between the sum and the conversion.
+// A workgroup takes a row, C vectors of 8 columns a thread, kept in registers between the sum and the conversion.
 template <typename T, typename RT, bool RES, int C>
 __global__ void __launch_bounds__(kMaxNormThreads) norm_kernel(RowsArgs a) {
+  constexpr int P = 8;
   __shared__ float s_sum[kMaxNormThreads / kWave];
   const int64_t m = blockIdx.x;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
   const T* x = reinterpret_cast<const T*>(a.x) + m * a.stride;
-  float y[C][kPer];
+  float y[C][P];
   float sum = 0.f;
+  Raw<T, P> r[C];
+  Raw<RT, P> q[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const int col = (c * (int)blockDim.x + (int)threadIdx.x) * kPer;
-    Raw<T> r;
-    r.zero();
-    if (col < a.K) r.load(x + col);
-    r.values(y[c]);
+    const int col = (c * (int)blockDim.x + (int)threadIdx.x) * P;
+    r[c].zero();
+    q[c].zero();
+    if (col < a.K) {
+      r[c].load(x + col);
+      if constexpr (RES) q[c].load(reinterpret_cast<const RT*>(a.res) + m * a.K + col);
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const int col = (c * (int)blockDim.x + (int)threadIdx.x) * P;
+    r[c].values(y[c]);
     if constexpr (RES) {
-      Raw<RT> q;
-      q.zero();
-      if (col < a.K) q.load(reinterpret_cast<const RT*>(a.res) + m * a.K + col);
-      float z[kPer];
-      q.values(z);
+      float z[P];
+      q[c].values(z);
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) y[c][i] += z[i];
-      if (col < a.K) {
-        RT* o = reinterpret_cast<RT*>(a.res_out) + m * a.K + col;
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(RT); ++i) {
-          const float* v = y[c] + i * (16 / sizeof(RT));
-          uint4 w;
-          if constexpr (sizeof(RT) == 2)
-            w = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-          else
-            w = make_uint4(__builtin_bit_cast(uint32_t, v[0]), __builtin_bit_cast(uint32_t, v[1]), __builtin_bit_cast(uint32_t, v[2]),
-                           __builtin_bit_cast(uint32_t, v[3]));
-          reinterpret_cast<uint4*>(o)[i] = w;
-        }
-      }
+      for (int i = 0; i < P; ++i) y[c][i] += z[i];
+      if (col < a.K) store_values<RT, P>(reinterpret_cast<RT*>(a.res_out) + m * a.K + col, y[c]);
     }
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) sum = __builtin_fmaf(y[c][i], y[c][i], sum);
+    for (int i = 0; i < P; ++i) sum = __builtin_fmaf(y[c][i], y[c][i], sum);
   }
   sum = wave_sum(sum);
   if (lane == 0) s_sum[wave] = sum;
@@ -181,37 +213,31 @@ __global__ void __launch_bounds__(kMaxNormThreads) norm_kernel(RowsArgs a) {
   const float rs = 1.f / sqrtf(sum / (float)a.K + a.eps);
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const int col = (c * (int)blockDim.x + (int)threadIdx.x) * kPer;
+    const int col = (c * (int)blockDim.x + (int)threadIdx.x) * P;
     if (col < a.K) {
-      Raw<float> g;
+      Raw<float, P> g;
       g.load(a.gain + col);
-      float gv[kPer];
+      float gv[P];
       g.values(gv);
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) y[c][i] = y[c][i] * rs * gv[i];
-      if (a.y) {
-        uint4* o = reinterpret_cast<uint4*>(a.y + m * a.K + col);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float* v = y[c] + 8 * i;
-          o[i] = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-        }
-      }
+      for (int i = 0; i < P; ++i) y[c][i] = y[c][i] * rs * gv[i];
+      if (a.y) store_values<uint16_t, P>(a.y + m * a.K + col, y[c]);
     } else {  // (zeros times a norm that is not finite)
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) y[c][i] = 0.f;
+      for (int i = 0; i < P; ++i) y[c][i] = 0.f;
     }
-    store_rows(a, m, col, y[c]);
+    store_rows<P>(a, m, col, y[c]);
   }
 }
 
 // A workgroup takes a block of 128 x 128, four vectors of 16 columns a thread.
 template <typename T>
 __global__ void __launch_bounds__(256) matrix_kernel(RowsArgs a, int KB) {
+  constexpr int P = 16, kLanes = kBlock8 / P;
   __shared__ float s_max[4];
   const int nb = blockIdx.x / KB, kb = blockIdx.x - nb * KB;
-  const int col = kb * kBlock8 + threadIdx.x % kLanes * kPer;
-  Raw<T> r[4];
+  const int col = kb * kBlock8 + threadIdx.x % kLanes * P;
+  Raw<T, P> r[4];
   float mx = 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -221,9 +247,9 @@ __global__ void __launch_bounds__(256) matrix_kernel(RowsArgs a, int KB) {
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    float y[kPer];
+    float y[P];
     r[i].values(y);
-    mx = fmaxf(mx, amax16(y));
+    mx = fmaxf(mx, amax_of<P>(y));
   }
   mx = wave_max(mx);
   if (threadIdx.x % kWave == 0) s_max[threadIdx.x / kWave] = mx;
@@ -233,9 +259,9 @@ __global__ void __launch_bounds__(256) matrix_kernel(RowsArgs a, int KB) {
   for (int i = 0; i < 4; ++i) {
     const int64_t row = (int64_t)nb * kBlock8 + i * 32 + threadIdx.x / kLanes;
     if (row >= a.M || col >= a.K) continue;
-    float y[kPer];
+    float y[P];
     r[i].values(y);
-    *reinterpret_cast<uint4*>(a.codes + row * a.K + col) = encode16(y, sc.inv);
+    store_codes<P>(a.codes + row * a.K + col, y, sc);
   }
   if (threadIdx.x == 0) store_scale(a.scales, a.e8, (int64_t)nb * KB + kb, sc);
 }
@@ -285,7 +311,7 @@ RowsArgs rows_args(const void* x, size_t stride, int M, int K, uint8_t* codes, v
 
 template <bool SWIGLU>
 int launch_rows(const RowsArgs& a, int dtype, hipStream_t st) {
-  const int segs = (int)ceil_div(a.K, kWaveCols);
+  const int segs = (int)ceil_div(a.K, 16 * kWave);
   const int64_t blocks = ceil_div((int64_t)a.M * segs, 4);
   SDD_REQUIRE(blocks < ((int64_t)1 << 31), "too many rows (%d of %d)", a.M, a.K);
   prof_begin(PROF_ROWS8, st);
@@ -299,15 +325,17 @@ int launch_rows(const RowsArgs& a, int dtype, hipStream_t st) {
 
 template <typename T, typename RT, bool RES>
 void launch_norm(const RowsArgs& a, hipStream_t st) {
-  const int vecs = a.K / kPer;
+  const int vecs = a.K / 8;
   const int threads = (int)std::min<int64_t>(kMaxNormThreads, ceil_div(vecs, kWave) * kWave);
   const int c = (int)ceil_div(vecs, threads);
   if (c == 1)
     hipLaunchKernelGGL((norm_kernel<T, RT, RES, 1>), dim3(a.M), dim3(threads), 0, st, a);
   else if (c == 2)
     hipLaunchKernelGGL((norm_kernel<T, RT, RES, 2>), dim3(a.M), dim3(threads), 0, st, a);
-  else
+  else if (c <= 4)
     hipLaunchKernelGGL((norm_kernel<T, RT, RES, 4>), dim3(a.M), dim3(threads), 0, st, a);
+  else
+    hipLaunchKernelGGL((norm_kernel<T, RT, RES, 8>), dim3(a.M), dim3(threads), 0, st, a);
 }
 template <typename T>
 void launch_norm(const RowsArgs& a, int residual_dtype, hipStream_t st) {

@@ -513,19 +513,17 @@ def _scale_code(t: torch.Tensor) -> int:
     raise TypeError(f"scales must be float32 or float8_e8m0fnu, got {t.dtype}")
 
 
-def _codes_out(x, M, K, scale, out, matrix=False):
-    """(codes, scales) to write into, checked where they are given, and the scales' code."""
+def _codes_out(x, M, K, scale, out, shape):
+    """(codes, scales of `shape`) to write into, checked where they are given, and the scales' code."""
     if scale not in _SCALES:
         raise ValueError(f"scale must be f32 or e8m0, got {scale}")
     code, dtype = _SCALES[scale]
-    blocks = -(-K // 128)
-    shape = (-(-M // 128), blocks) if matrix else (blocks, M)
     if out is None:
         return x.new_empty((M, K), dtype=torch.float8_e4m3fn), x.new_empty(shape, dtype=dtype), code
     codes, scales = out
     _codes(codes, "codes")
-    _need(tuple(codes.shape) == (M, K), f"codes must be [{M}, {K}]")
-    _need(scales.dtype == dtype and scales.is_contiguous() and tuple(scales.shape) == shape, f"scales must be contiguous {dtype} {list(shape)}")
+    _need(codes.shape == (M, K), f"codes must be [{M}, {K}]")
+    _need(scales.dtype == dtype and scales.is_contiguous() and scales.shape == shape, f"scales must be contiguous {dtype} {list(shape)}")
     return codes, scales, code
 
 
@@ -535,9 +533,11 @@ def _codes(t, name):
 
 
 def _rows2(x, name):
+    """(rows, columns, row stride, dtype code) of x."""
     if x.dim() != 2 or x.shape[0] == 0 or x.stride(1) != 1:
         raise ValueError(f"{name} must be [rows, columns] with unit column stride")
-    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+    M, K = x.shape
+    return M, K, x.stride(0) if M > 1 else K, _dtype_code(x)
 
 
 def e4m3_quantize(x: torch.Tensor, *, scale: str = "f32", out=None, stream=None):
@@ -547,10 +547,9 @@ def e4m3_quantize(x: torch.Tensor, *, scale: str = "f32", out=None, stream=None)
     if stream is not None:  # (what the call makes is that stream's)
         with torch.cuda.stream(stream):
             return e4m3_quantize(x, scale=scale, out=out)
-    s0, dt = _rows2(x, "x"), _dtype_code(x)
-    M, K = x.shape
-    codes, scales, code = _codes_out(x, M, K, scale, out)
-    st = _here(x, codes, scales)
+    M, K, s0, dt = _rows2(x, "x")
+    codes, scales, code = _codes_out(x, M, K, scale, out, (-(-K // 128), M))
+    st = _here(x) if out is None else _here(x, codes, scales)
     _check(lib().sdd_e4m3_quantize(x.data_ptr(), dt, s0, M, K, codes.data_ptr(), scales.data_ptr(), code, st))
     return codes, scales
 
@@ -560,10 +559,9 @@ def e4m3_quantize_matrix(x: torch.Tensor, *, scale: str = "f32", out=None, strea
     if stream is not None:
         with torch.cuda.stream(stream):
             return e4m3_quantize_matrix(x, scale=scale, out=out)
-    s0, dt = _rows2(x, "x"), _dtype_code(x)
-    N, K = x.shape
-    codes, scales, code = _codes_out(x, N, K, scale, out, matrix=True)
-    st = _here(x, codes, scales)
+    N, K, s0, dt = _rows2(x, "x")
+    codes, scales, code = _codes_out(x, N, K, scale, out, (-(-N // 128), -(-K // 128)))
+    st = _here(x) if out is None else _here(x, codes, scales)
     _check(lib().sdd_e4m3_quantize_matrix(x.data_ptr(), dt, s0, N, K, codes.data_ptr(), scales.data_ptr(), code, st))
     return codes, scales
 
@@ -573,12 +571,11 @@ def e4m3_swiglu(x: torch.Tensor, *, scale: str = "f32", out=None, stream=None):
     if stream is not None:
         with torch.cuda.stream(stream):
             return e4m3_swiglu(x, scale=scale, out=out)
-    s0, dt = _rows2(x, "x"), _dtype_code(x)
-    M, K = x.shape
+    M, K, s0, dt = _rows2(x, "x")
     _need(K % 2 == 0, "x must be [M, 2 K]")
     K //= 2
-    codes, scales, code = _codes_out(x, M, K, scale, out)
-    st = _here(x, codes, scales)
+    codes, scales, code = _codes_out(x, M, K, scale, out, (-(-K // 128), M))
+    st = _here(x) if out is None else _here(x, codes, scales)
     _check(lib().sdd_e4m3_swiglu(x.data_ptr(), dt, s0, M, K, codes.data_ptr(), scales.data_ptr(), code, st))
     return codes, scales
 
@@ -592,34 +589,34 @@ def e4m3_rmsnorm(x: torch.Tensor, gain: torch.Tensor, *, eps: float = 1e-6, resi
     if stream is not None:
         with torch.cuda.stream(stream):
             return e4m3_rmsnorm(x, gain, eps=eps, residual=residual, residual_out=residual_out, y=y, scale=scale, out=out)
-    s0, dt = _rows2(x, "x"), _dtype_code(x)
-    M, K = x.shape
+    M, K, s0, dt = _rows2(x, "x")
     if gain.dtype != torch.float32 or not gain.is_contiguous() or gain.numel() != K:
         raise ValueError("gain must be contiguous fp32 [K]")
-    codes, scales, code = _codes_out(x, M, K, scale, out)
-    used = [x, gain, codes, scales]
-    rd = F32
+    codes, scales, code = _codes_out(x, M, K, scale, out, (-(-K // 128), M))
+    used = [x, gain] if out is None else [x, gain, codes, scales]
+    rd, res, res_out = F32, None, None
     if residual is not None:
         if residual_out is None:
             residual_out = residual
         rd = _dtype_code(residual)
         for t, nm in ((residual, "residual"), (residual_out, "residual_out")):
-            if t.dtype != residual.dtype or not t.is_contiguous() or tuple(t.shape) != (M, K):
+            if t.dtype != residual.dtype or not t.is_contiguous() or t.shape != x.shape:
                 raise ValueError(f"{nm} must be contiguous {residual.dtype} [{M}, {K}]")
-        used += [residual, residual_out]
+            used.append(t)
+        res, res_out = residual.data_ptr(), residual_out.data_ptr()
     else:
         _need(residual_out is None, "residual_out needs a residual")
     if y is True:
         y = x.new_empty((M, K), dtype=torch.bfloat16)
-    elif y is False:
+    elif y is False or y is None:
         y = None
-    if y is not None:
-        if y.dtype != torch.bfloat16 or not y.is_contiguous() or tuple(y.shape) != (M, K):
+    else:
+        if y.dtype != torch.bfloat16 or not y.is_contiguous() or y.shape != x.shape:
             raise ValueError(f"y must be contiguous bf16 [{M}, {K}]")
         used.append(y)
     st = _here(*used)
-    _check(lib().sdd_e4m3_rmsnorm(x.data_ptr(), dt, s0, _addr(residual), _addr(residual_out), rd, gain.data_ptr(), eps, M, K,
-                                  codes.data_ptr(), scales.data_ptr(), code, _addr(y), st))
+    _check(lib().sdd_e4m3_rmsnorm(x.data_ptr(), dt, s0, res, res_out, rd, gain.data_ptr(), eps, M, K, codes.data_ptr(), scales.data_ptr(),
+                                  code, _addr(y), st))
     return codes, scales, residual_out, y
 
 
@@ -637,7 +634,7 @@ class E4M3Matrix:
         sd = _scale_code(scales)
         _need(scales.is_contiguous() and tuple(scales.shape) == (-(-N // 128), -(-K // 128)),
               "scales must be contiguous [ceil(N / 128), ceil(K / 128)]")
-        self.shape = (N, K)
+        self.shape, self.blocks = (N, K), -(-K // 128)
         self.desc = MatrixDesc(N, K, sd, None)
         n = _size_out(lib().sdd_e4m3_matrix_bytes, C.byref(self.desc))
         with torch.cuda.stream(stream):  # (None: the current one)
@@ -664,19 +661,22 @@ class E4M3Matrix:
         M = codes.shape[0]
         if codes.shape[1] != K:
             raise ValueError(f"codes must be [M, {K}]")
-        if not scales.is_contiguous() or tuple(scales.shape) != (-(-K // 128), M):
-            raise ValueError(f"scales must be contiguous [{-(-K // 128)}, {M}]")
-        if out is None:
-            out = codes.new_empty((M, N), dtype=dtype)
-        elif tuple(out.shape) != (M, N) or out.stride(1) != 1:
-            raise ValueError(f"out must be [{M}, {N}] with unit column stride")
+        if not scales.is_contiguous() or scales.shape != (self.blocks, M):
+            raise ValueError(f"scales must be contiguous [{self.blocks}, {M}]")
+        sd = _scale_code(scales)
         if ws is None:
             ws = self.workspace(M)
         _need(ws.is_contiguous(), "ws must be contiguous")
-        sd, od = _scale_code(scales), _dtype_code(out)
-        st = _here(self.buf, codes, scales, out, ws)
-        _check(lib().sdd_e4m3_matmul(self._desc, codes.data_ptr(), scales.data_ptr(), sd, M, out.data_ptr(), od,
-                                     out.stride(0) if M > 1 else N, ws.data_ptr(), ws.nbytes, st))
+        if out is None:
+            out, s0 = codes.new_empty((M, N), dtype=dtype), N
+            st = _here(self.buf, codes, scales, ws)
+        else:
+            if out.shape != (M, N) or out.stride(1) != 1:
+                raise ValueError(f"out must be [{M}, {N}] with unit column stride")
+            s0 = out.stride(0) if M > 1 else N
+            st = _here(self.buf, codes, scales, ws, out)
+        _check(lib().sdd_e4m3_matmul(self._desc, codes.data_ptr(), scales.data_ptr(), sd, M, out.data_ptr(), _dtype_code(out), s0, ws.data_ptr(),
+                                     ws.nbytes, st))
         return out
 
 
