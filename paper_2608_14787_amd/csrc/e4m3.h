@@ -25,5 +25,7 @@ __device__ inline float e8m0_value(uint32_t byte) {
 // Stored matrix: codes, then from this byte on the scales as fp32 [ceil(N / 128)][ceil(K / 128)].
 inline int64_t matrix_code_bytes(const sdd_e4m3_matrix* m) { return ceil_div(m->N, 16) * ceil_div(m->K, kBlock8) * kTile8; }
 int check_matrix(const sdd_e4m3_matrix* m);
+// A launch counts its threads in 32 bits.
+int check_grid(double blocks, int threads);
 
 }  // namespace sdd

@@ -607,13 +607,16 @@ __global__ void __launch_bounds__(kWave * GN * GM, 2) many_rows_kernel(MatArgs a
         r.sc[j] = (E8 ? e8m0_value(xs) : __builtin_bit_cast(float, xs)) * w1;
     }
   };
-  u32x4 w[2][2];
+  // tiles read ahead, and the registers that they turn through (256 x 256 has none left for more)
+  constexpr int LOOK = WN * WM <= 16 ? 2 : 1, WR = LOOK > 1 ? 4 : 2;
+  static_assert(WN % WR == 0 && HALF >= LOOK, "a step's tiles in whole turns, a half step's landed tiles ahead at most");
+  u32x4 w[WR][2];
   auto read_tile = [&](u32x4* f, int i, int t) {
     const u32x4* sw = reinterpret_cast<const u32x4*>(s_ring + i % RS * kStage) + (wn * WN + t) * 128 + lane;
     f[0] = sw[0], f[1] = sw[64];
   };
-  // The half of a step's products that the tiles I0 .. I0 + HALF - 1 have with its rows; meanwhile the next tile's fragments are
-  // read (the first one of the next half too), and in the second half the next step's rows.  A product's sums are added two
+  // The half of a step's products that the tiles I0 .. I0 + HALF - 1 have with its rows; meanwhile the next tiles' fragments are
+  // read (those of the next half too), and in the second half the next step's rows.  A product's sums are added two
   // products later: a wave issues in order, and would wait for the products just asked for.
   constexpr int kLag = 2;
   auto multiply = [&](int step, const Rows& r, Rows& next, auto half_c) {
@@ -630,12 +633,12 @@ __global__ void __launch_bounds__(kWave * GN * GM, 2) many_rows_kernel(MatArgs a
 #pragma unroll
     for (int t = 0; t < HALF * WM; ++t) {
       const int i = I0 + t / WM, j = t % WM;
-      if (j == 0) read_tile(w[(i + 1) % 2], step + (i + 1) / WN, (i + 1) % WN);
+      if (j == 0) read_tile(w[(i + LOOK) % WR], step + (i + LOOK) / WN, (i + LOOK) % WN);
       if (I0 > 0 && t % HALF == 0 && t / HALF < WM) read_row(next, step + 1, t / HALF);
       if (I0 > 0 && t == HALF * WM / 2) read_scales(next, step + 1);
       // (one at a time: together they fill the queue to memory, and the products behind them wait)
       if (t % EVERY == EVERY / 2 && t / EVERY < LH) issue(step, I0 > 0, t / EVERY);
-      const u32x4* f = w[i % 2];
+      const u32x4* f = w[i % WR];
       if constexpr (SCALED) {
         f32x4& c = acc[i][j];
         c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fragment(f[0], f[1]), fragment(r.x[j][0], r.x[j][1]), c, 0, 0, 0, r.ws, 0, r.xs[j]);
@@ -683,7 +686,8 @@ __global__ void __launch_bounds__(kWave * GN * GM, 2) many_rows_kernel(MatArgs a
   }
   Rows r0, r1;
   turn(std::integral_constant<int, kLeft + LH>());
-  read_tile(w[0], 0, 0);
+#pragma unroll
+  for (int i = 0; i < LOOK; ++i) read_tile(w[i], 0, i);
   read_scales(r0, 0);
 #pragma unroll
   for (int j = 0; j < WM; ++j) read_row(r0, 0, j);
@@ -857,8 +861,12 @@ extern "C" int sdd_e4m3_matmul(const sdd_e4m3_matrix* m, const uint8_t* x, const
   a.out = reinterpret_cast<char*>(out);
   a.stride = (int64_t)out_stride;
   a.vec = (uintptr_t)out % (4 * es) == 0 && out_stride % 4 == 0;
-  SDD_REQUIRE(ceil_div(a.NT, 8) * ceil_div(M, 128) < ((int64_t)1 << 31), "too many rows (%d of %d)", M, m->N);
   const Plan p = plan_of(M, a.NT, a.KB, out_dtype == SDD_F32);
+  if (p.kind >= Plan::kTile128) {
+    const bool big = p.kind == Plan::kTile256;
+    const double blocks = (double)ceil_div(ceil_div(a.NT, big ? 16 : 8) * p.splits, kXcds) * kXcds * ceil_div(M, big ? 256 : 128);
+    if (int rc = check_grid(blocks, p.kind == Plan::kTile128 ? 256 : 512)) return rc;
+  }
   const size_t need = plan_bytes(p, M, a.NT);
   if (need) {
     SDD_REQUIRE(ws && (uintptr_t)ws % 16 == 0, "workspace is NULL or not 16-byte aligned");

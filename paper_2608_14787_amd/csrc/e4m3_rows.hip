@@ -266,15 +266,15 @@ __global__ void __launch_bounds__(256) matrix_kernel(RowsArgs a, int KB) {
   if (threadIdx.x == 0) store_scale(a.scales, a.e8, (int64_t)nb * KB + kb, sc);
 }
 
-// Row-major codes and scales to the stored order: a thread moves 16 bytes.
+// Row-major codes and scales to the stored order: a thread moves 16 bytes at a time.
 __global__ void __launch_bounds__(256) load_codes_kernel(const uint8_t* codes, uint4* to, int N, int K, int KB, int64_t n) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
-  const int lane = (int)(i % kWave), half = (int)(i / kWave % 2);
-  const int64_t tile = i / (2 * kWave);
-  const int64_t nt = tile / KB, row = nt * 16 + lane % 16;
-  const int col = (int)(tile - nt * KB) * kBlock8 + half * 64 + lane / 16 * 16;
-  to[i] = row < N && col < K ? load16(codes + row * K + col) : make_uint4(0, 0, 0, 0);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int lane = (int)(i % kWave), half = (int)(i / kWave % 2);
+    const int64_t tile = i / (2 * kWave);
+    const int64_t nt = tile / KB, row = nt * 16 + lane % 16;
+    const int col = (int)(tile - nt * KB) * kBlock8 + half * 64 + lane / 16 * 16;
+    to[i] = row < N && col < K ? load16(codes + row * K + col) : make_uint4(0, 0, 0, 0);
+  }
 }
 __global__ void __launch_bounds__(256) load_scales_kernel(const void* scales, int e8, float* to, int64_t n) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -313,7 +313,7 @@ template <bool SWIGLU>
 int launch_rows(const RowsArgs& a, int dtype, hipStream_t st) {
   const int segs = (int)ceil_div(a.K, 16 * kWave);
   const int64_t blocks = ceil_div((int64_t)a.M * segs, 4);
-  SDD_REQUIRE(blocks < ((int64_t)1 << 31), "too many rows (%d of %d)", a.M, a.K);
+  if (int rc = check_grid((double)blocks, 256)) return rc;
   prof_begin(PROF_ROWS8, st);
   if (dtype == SDD_F32)
     hipLaunchKernelGGL((rows_kernel<float, SWIGLU>), dim3((unsigned)blocks), dim3(256), 0, st, a, segs);
@@ -346,6 +346,11 @@ void launch_norm(const RowsArgs& a, int residual_dtype, hipStream_t st) {
 
 }  // namespace
 
+int check_grid(double blocks, int threads) {
+  SDD_REQUIRE(blocks * threads < 4294967296.0, "%.0f workgroups of %d threads are too many for a launch", blocks, threads);
+  return SDD_OK;
+}
+
 int check_matrix(const sdd_e4m3_matrix* m) {
   SDD_REQUIRE(m != nullptr, "matrix description is NULL");
   SDD_REQUIRE(m->N > 0 && m->N <= kMaxN8 && m->K > 0 && m->K <= kMaxK8 && m->K % 16 == 0,
@@ -376,7 +381,7 @@ extern "C" int sdd_e4m3_quantize_matrix(const void* x, int dtype, size_t row_str
   if (int rc = check_rows(x, dtype, row_stride, N, K, K, codes, scales, scale_dtype)) return rc;
   const int KB = (int)ceil_div(K, kBlock8);
   const int64_t blocks = ceil_div(N, kBlock8) * KB;
-  SDD_REQUIRE(blocks < ((int64_t)1 << 31), "matrix [%d][%d] is too large", N, K);
+  if (int rc = check_grid((double)blocks, 256)) return rc;
   const RowsArgs a = rows_args(x, row_stride, N, K, codes, scales, scale_dtype);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   prof_begin(PROF_ROWS8, st);
@@ -398,6 +403,7 @@ extern "C" int sdd_e4m3_rmsnorm(const void* x, int dtype, size_t row_stride, con
   SDD_REQUIRE(aligned16(residual) && aligned16(residual_out) && aligned16(y_out), "residual and y must be 16-byte aligned");
   SDD_REQUIRE(eps >= 0.f && eps < INFINITY, "eps %g", (double)eps);
   if (K > kMaxNormK) return fail(SDD_EUNSUPPORTED, "rows of %d (at most %d are built)", K, kMaxNormK);
+  if (int rc = check_grid(M, (int)std::min<int64_t>(kMaxNormThreads, ceil_div(K / 8, kWave) * kWave))) return rc;
   RowsArgs a = rows_args(x, row_stride, M, K, codes, scales, scale_dtype);
   a.res = reinterpret_cast<const char*>(residual);
   a.res_out = reinterpret_cast<char*>(residual_out);
@@ -428,10 +434,9 @@ extern "C" int sdd_e4m3_matrix_load(const sdd_e4m3_matrix* m, const uint8_t* cod
   SDD_REQUIRE(m->scale_dtype == SDD_E8M0 || (uintptr_t)scales % 4 == 0, "scales must be 4-byte aligned");
   const int KB = (int)ceil_div(m->K, kBlock8);
   const int64_t n = matrix_code_bytes(m) / 16, ns = ceil_div(m->N, kBlock8) * KB;
-  SDD_REQUIRE(n / 256 < ((int64_t)1 << 31) - 1, "matrix [%d][%d] is too large", m->N, m->K);
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   prof_begin(PROF_ROWS8, st);
-  hipLaunchKernelGGL(load_codes_kernel, dim3((unsigned)ceil_div(n, 256)), dim3(256), 0, st, codes, reinterpret_cast<uint4*>(m->data),
+  hipLaunchKernelGGL(load_codes_kernel, dim3((unsigned)std::min<int64_t>(ceil_div(n, 256), 1 << 20)), dim3(256), 0, st, codes, reinterpret_cast<uint4*>(m->data),
                      m->N, m->K, KB, n);
   hipLaunchKernelGGL(load_scales_kernel, dim3((unsigned)ceil_div(ns, 256)), dim3(256), 0, st, scales, m->scale_dtype == SDD_E8M0,
                      reinterpret_cast<float*>(reinterpret_cast<char*>(m->data) + matrix_code_bytes(m)), ns);

@@ -102,24 +102,37 @@ def test_what_a_value_that_is_no_number_reaches(S, M, out):
     assert torch.isnan(got[bad]).all() and torch.equal(got[~bad], want[~bad])
 
 
-@pytest.mark.parametrize("M", [2, 80])
-def test_zero_and_extreme_scales(S, M):
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("M", [2, 40, 80, 200])
+def test_zero_and_extreme_scales(S, M, out):
     g = gen(M, 3)
     x, xs = R.random_codes(g, M, 256, "f32")
     w, ws = R.random_codes(g, 40, 256, "f32", matrix=True)
     xs[:, 0] = 0
     xs[:, 1] = 2.0 ** -100
-    got = S.E4M3Matrix(w.cuda(), ws.cuda()).matmul(x.cuda(), xs.cuda(), dtype=torch.float32).cpu()
+    got = S.E4M3Matrix(w.cuda(), ws.cuda()).matmul(x.cuda(), xs.cuda(), dtype=DT[out]).cpu()
     want, mag = R.matmul(x, xs, w, ws)
-    assert (got[0] == 0).all() and ((got.double() - want).abs() <= R.matmul_tol(want, mag, 256, torch.float32)).all()
-    # the smallest and largest bytes, and the byte that is no number
+    tol = R.matmul_tol(want, mag, 256, DT[out], R.group_max(x, xs, w, ws) if out == "bf16" else None)
+    assert (got[0] == 0).all() and ((got.double() - want).abs() <= tol).all()
+    # powers of two on both sides: the smallest byte, large ones, and the byte that is no number
+    w, ws = R.random_codes(g, 200, 256, "e8m0", matrix=True)
     b = torch.full((2, M), 127, dtype=torch.uint8)
     b[:, 0], b[0, 1] = 0, 255
+    if M > 2:
+        b[:, 2] = 200
     xs = b.view(torch.float8_e8m0fnu)
-    got = S.E4M3Matrix(w.cuda(), ws.cuda()).matmul(x.cuda(), xs.cuda(), dtype=torch.float32).cpu()
+    got = S.E4M3Matrix(w.cuda(), ws.cuda()).matmul(x.cuda(), xs.cuda(), dtype=DT[out]).cpu()
     assert torch.isnan(got[1]).all()
-    want, mag = R.matmul(x[:1], xs[:, :1].contiguous(), w, ws)
-    assert ((got[:1].double() - want).abs() <= R.matmul_tol(want, mag, 256, torch.float32) + mag * 2.0 ** -20).all()
+    keep = torch.tensor([m for m in range(M) if m != 1])
+    xk, sk = x.view(torch.uint8)[keep].view(torch.float8_e4m3fn), b[:, keep].contiguous().view(torch.float8_e8m0fnu)
+    want, mag = R.matmul(xk, sk, w, ws)
+    tol = R.matmul_tol(want, mag, 256, DT[out], R.group_max(xk, sk, w, ws) if out == "bf16" else None)
+    # (2^-149: results among the smallest numbers)
+    assert ((got[keep].double() - want).abs() <= tol + 2.0 ** -133).all()
+    wb = ws.view(torch.uint8).clone()
+    wb[1, 1] = 255
+    got2 = S.E4M3Matrix(w.cuda(), wb.view(torch.float8_e8m0fnu).cuda()).matmul(x.cuda(), xs.cuda(), dtype=DT[out]).cpu()
+    assert torch.isnan(got2[:, 128:]).all() and torch.equal(got2[keep][:, :128], got[keep][:, :128])
 
 
 @pytest.mark.parametrize("M", [1, 33, 64, 65, 264])
