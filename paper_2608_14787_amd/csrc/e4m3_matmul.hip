@@ -69,62 +69,23 @@ __device__ inline void store4(const MatArgs& a, int m, int n, const f32x4& v) {
 
 // ---- few rows ---------------------------------------------------------------------------------------------
 //
-// A workgroup takes NT row tiles of the matrix and all (up to 16 MT) rows; its eight waves take every eighth block of 128
+// A workgroup takes NT row tiles of the matrix and all (up to 16) rows; its eight waves take every eighth block of 128
 // columns, each its own loads (no barrier in the loop), and join in LDS in wave order.
 
-constexpr int kFewWaves = 8;
+constexpr int kFewWaves = 8, kFewRows = 4;
 
 template <int NT>
-struct WStep {
-  u32x4 w[NT][2];
+struct Few {  // a wave's codes and scales of one block of columns
+  u32x4 w[NT][2], x[2];
   float ws[NT];
+  uint32_t xs;
 };
-template <int MT>
-struct XStep {
-  u32x4 x[MT][2];
-  uint32_t xs[MT];
-};
-
-// widened on its way to the products; p: a block's sums
-template <int MT, int NT, bool E8>
-__device__ inline void multiply(const WStep<NT>& s, const XStep<MT>& r, f32x4 (*acc)[NT]) {
-  f32x4 p[MT][NT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) p[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      bf16x8 w[NT];
-#pragma unroll
-      for (int j = 0; j < NT; ++j) w[j] = widen(s.w[j][h][2 * c], s.w[j][h][2 * c + 1]);
-#pragma unroll
-      for (int i = 0; i < MT; ++i) {
-        const bf16x8 x = widen(r.x[i][h][2 * c], r.x[i][h][2 * c + 1]);
-#pragma unroll
-        for (int j = 0; j < NT; ++j) p[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[j], x, p[i][j], 0, 0, 0);
-      }
-    }
-#pragma unroll
-  for (int i = 0; i < MT; ++i) {
-    const float xs = E8 ? e8m0_value(r.xs[i]) : __builtin_bit_cast(float, r.xs[i]);
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const float sc = xs * s.ws[j];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_fmaf(p[i][j][e], sc, acc[i][j][e]);
-    }
-  }
-}
 
 constexpr int kNowhere = 0x7ffffff0;  // an offset past every descriptor's end: zeros, and no memory is read
 
-template <int MT, int NT, bool E8, bool F32>
+template <int NT, bool E8, bool F32>
 __global__ void __launch_bounds__(kFewWaves * kWave, 2) few_rows_kernel(MatArgs a) {
-  constexpr int WS = 2, XS = 2;
-  __shared__ __align__(16) f32x4 s_part[kFewWaves][MT * NT][kWave];
+  __shared__ __align__(16) f32x4 s_part[kFewWaves][NT][kWave];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const int t0 = blockIdx.x * NT;
   const int steps = (a.KB - wave + kFewWaves - 1) / kFewWaves;  // (KB < wave: none)
@@ -137,66 +98,66 @@ __global__ void __launch_bounds__(kFewWaves * kWave, 2) few_rows_kernel(MatArgs 
   }
   const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void*)a.x, 0, a.M * a.K, kBufferRsrcWord3);
   const __amdgpu_buffer_rsrc_t rxs = __builtin_amdgcn_make_buffer_rsrc((void*)a.xs, 0, a.KB * a.M * (E8 ? 1 : 4), kBufferRsrcWord3);
-  int row[MT];
-#pragma unroll
-  for (int t = 0; t < MT; ++t) row[t] = min(t * 16 + lane % 16, a.M - 1);
-  auto load_w = [&](WStep<NT>& s, int step) {
+  const int row = min(lane % 16, a.M - 1);
+  auto load = [&](Few<NT>& s, int step) {
     const int kb = wave + kFewWaves * step;  // past KB: past the descriptors' ends
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int k = kb * kBlock8 + h * 64 + lane / 16 * 16;
+      s.x[h] = __builtin_amdgcn_raw_buffer_load_b128(rx, k < a.K ? row * a.K + k : kNowhere, 0, 0);
+    }
+    const int at = kb < a.KB ? kb * a.M + row : kNowhere / 4;
+    s.xs = E8 ? (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rxs, at, 0, 0) : __builtin_amdgcn_raw_buffer_load_b32(rxs, at * 4, 0, 0);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) s.w[t][h] = __builtin_amdgcn_raw_buffer_load_b128(rw[t], kb * kTile8 + h * 1024 + lane * 16, 0, kNtCpol);
       s.ws[t] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rws[t], kb * 4, 0, 0));
     }
+    __builtin_amdgcn_sched_barrier(0);  // (loads stay in their order: the waits count them)
   };
-  auto load_x = [&](XStep<MT>& s, int step) {
-    const int kb = wave + kFewWaves * step;
+  f32x4 acc[NT];
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
+  for (int j = 0; j < NT; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto multiply = [&](const Few<NT>& s) {
+    f32x4 p[NT];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int k = kb * kBlock8 + h * 64 + lane / 16 * 16;
-        s.x[t][h] = __builtin_amdgcn_raw_buffer_load_b128(rx, k < a.K ? row[t] * a.K + k : kNowhere, 0, 0);
+    for (int j = 0; j < NT; ++j) p[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const bf16x8 x = widen(s.x[h][2 * c], s.x[h][2 * c + 1]);
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+          p[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(s.w[j][h][2 * c], s.w[j][h][2 * c + 1]), x, p[j], 0, 0, 0);
       }
-      const int at = kb < a.KB ? kb * a.M + row[t] : kNowhere / 4;
-      s.xs[t] = E8 ? (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(rxs, at, 0, 0) : __builtin_amdgcn_raw_buffer_load_b32(rxs, at * 4, 0, 0);
+    const float xs = E8 ? e8m0_value(s.xs) : __builtin_bit_cast(float, s.xs);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      const float sc = xs * s.ws[j];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[j][e] = __builtin_fmaf(p[j][e], sc, acc[j][e]);
     }
-  };
-  f32x4 acc[MT][NT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  WStep<NT> w[WS];
-  XStep<MT> x[XS];
-  static_assert(WS % XS == 0, "rings turn together");
-#pragma unroll
-  for (int i = 0; i < WS - 1; ++i) {
-    load_w(w[i], i);
-    if (i >= WS - XS) load_x(x[i - (WS - XS)], i - (WS - XS));
     __builtin_amdgcn_sched_barrier(0);
-  }
-  for (int i = 0; i < steps; i += WS) {
-#pragma unroll
-    for (int j = 0; j < WS; ++j) {
-      load_x(x[(j + XS - 1) % XS], i + j + XS - 1);
-      load_w(w[(j + WS - 1) % WS], i + j + WS - 1);
-      __builtin_amdgcn_sched_barrier(0);  // (loads stay in their order: the waits count them)
-      multiply<MT, NT, E8>(w[j], x[j % XS], acc);
-      __builtin_amdgcn_sched_barrier(0);
-    }
+  };
+  Few<NT> s[2];
+  load(s[0], 0);
+  for (int i = 0; i < steps; i += 2) {
+    load(s[1], i + 1);
+    multiply(s[0]);
+    load(s[0], i + 2);
+    multiply(s[1]);  // (behind the last block: zeros)
   }
 #pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) s_part[wave][i * NT + j][lane] = acc[i][j];
+  for (int j = 0; j < NT; ++j) s_part[wave][j][lane] = acc[j];
   __syncthreads();
-  for (int item = threadIdx.x; item < MT * NT * kWave; item += kFewWaves * kWave) {
-    const int t = item / kWave, l = item % kWave, i = t / NT, j = t % NT;
-    f32x4 v = s_part[0][t][l];
+  for (int item = threadIdx.x; item < NT * kWave; item += kFewWaves * kWave) {
+    const int j = item / kWave, l = item % kWave;
+    f32x4 v = s_part[0][j][l];
 #pragma unroll
-    for (int w = 1; w < kFewWaves; ++w) v += s_part[w][t][l];
-    if (t0 + j < a.NT) store4<F32>(a, i * 16 + l % 16, (t0 + j) * 16 + l / 16 * 4, v);
+    for (int w = 1; w < kFewWaves; ++w) v += s_part[w][j][l];
+    if (t0 + j < a.NT) store4<F32>(a, l % 16, (t0 + j) * 16 + l / 16 * 4, v);
   }
 }
 
@@ -214,7 +175,7 @@ constexpr int kSharedThreads = 512;
 template <int MT, int NT, int GK, bool FP8, bool E8, bool F32>
 __global__ void __launch_bounds__(kSharedThreads, 2) shared_rows_kernel(MatArgs a) {
   constexpr int R = MT >= 8 ? 2 : 4;           // blocks of a wave in registers
-  constexpr int CB = GK == 8 ? 8 : MT >= 8 ? 2 : 4;  // blocks of a chunk
+  constexpr int CB = MT >= 8 ? 2 : 4;          // blocks of a chunk
   constexpr int SPC = CB / GK;                 // of them a wave's
   constexpr int U = R / SPC;                   // chunks until a wave's registers come round
   constexpr int GN = 8 / GK, kRows = 16 * MT;
@@ -234,7 +195,7 @@ __global__ void __launch_bounds__(kSharedThreads, 2) shared_rows_kernel(MatArgs 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const int wn = wave % GN, wk = wave / GN;
   const int groups = (a.NT + GN * NT - 1) / (GN * NT);
-  const int group = blockIdx.x % groups, rest = blockIdx.x / groups, split = rest % a.splits, m0 = rest / a.splits * kRows;
+  const int group = blockIdx.x % groups, split = blockIdx.x / groups;
   const int k0 = split * a.per, n = min(a.KB, k0 + a.per) - k0;  // blocks of this part
   __amdgpu_buffer_rsrc_t rw[NT], rws[NT];
 #pragma unroll
@@ -243,8 +204,7 @@ __global__ void __launch_bounds__(kSharedThreads, 2) shared_rows_kernel(MatArgs 
     rw[t] = __builtin_amdgcn_make_buffer_rsrc((void*)(a.w + ((int64_t)tile * a.KB + k0) * kTile8), 0, n * kTile8, kBufferRsrcWord3);
     rws[t] = __builtin_amdgcn_make_buffer_rsrc((void*)(a.ws + (int64_t)(tile / 8) * a.KB + k0), 0, n * 4, kBufferRsrcWord3);
   }
-  const int rows = min(kRows, a.M - m0);
-  const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void*)(a.x + (int64_t)m0 * a.K), 0, rows * a.K, kBufferRsrcWord3);
+  const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void*)a.x, 0, a.M * a.K, kBufferRsrcWord3);
   struct W {
     u32x4 w[NT][2];
     float ws[NT];
@@ -271,7 +231,7 @@ __global__ void __launch_bounds__(kSharedThreads, 2) shared_rows_kernel(MatArgs 
     for (int p = 0; p < PIECES; ++p) {
       const int r = pr + p * STEP, k = (k0 + i) * kBlock8 + pc * 16;
       int at = r * a.K + k;
-      at = i * 8 + pc < n * 8 && k < a.K && r < rows ? at : kNowhere;
+      at = i * 8 + pc < n * 8 && k < a.K && r < a.M ? at : kNowhere;
       asm volatile("" : "+v"(at));  // (a select, not a branch around the load)
       v.piece[p] = __builtin_amdgcn_raw_buffer_load_b128(rx, at, 0, 0);
     }
@@ -279,7 +239,7 @@ __global__ void __launch_bounds__(kSharedThreads, 2) shared_rows_kernel(MatArgs 
     for (int p = 0; p < XS; ++p) {
       const int at = threadIdx.x + p * kSharedThreads, kb = at / kRows, r = at % kRows;
       const bool ok = kb < CB && i + kb < n;
-      const float xs = x_scale<E8>(a, ok ? k0 + i + kb : k0, m0 + min(r, rows - 1));
+      const float xs = x_scale<E8>(a, ok ? k0 + i + kb : k0, min(r, a.M - 1));
       v.scale[p] = ok ? xs : 0.f;
     }
   };
@@ -303,7 +263,7 @@ __global__ void __launch_bounds__(kSharedThreads, 2) shared_rows_kernel(MatArgs 
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int g4 = lane / 16, r16 = lane % 16;
   // Row tiles go in groups of G: a group's fragments are read while the one before it is multiplied.
-  constexpr int G = MT <= 4 ? MT : MT % 4 == 0 ? 4 : 3;
+  constexpr int G = MT <= 4 ? MT : 4;
   static_assert(MT % G == 0, "whole groups");
   struct F {
     u32x4 x[G][2];
@@ -416,7 +376,7 @@ done:
     __syncthreads();
   }
   auto put = [&](int i, int tile, int l, f32x4 v) {
-    const int m = m0 + i * 16 + l % 16, col = tile * 16 + l / 16 * 4;
+    const int m = i * 16 + l % 16, col = tile * 16 + l / 16 * 4;
     if (tile >= a.NT) return;
     if (a.splits > 1) {
       if (m < a.M) *reinterpret_cast<f32x4*>(a.part + ((int64_t)split * a.M + m) * (a.NT * 16) + col) = v;
@@ -505,7 +465,7 @@ __device__ inline i32x8 fragment(const u32x4& a, const u32x4& b) {
   return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
 }
 
-constexpr int kStripe = 4;
+constexpr int kStripe = 12;
 constexpr int kScaleSteps = 8;  // blocks whose scales lie in LDS at a time (in two halves)
 
 template <int WN, int WM, int GN, int GM, int RS, bool FP8, bool E8, bool SCALED, bool F32>
@@ -722,12 +682,15 @@ __global__ void __launch_bounds__(kWave * GN * GM, 2) many_rows_kernel(MatArgs a
 // How a product is computed: by the call's shape alone.
 struct Plan {
   enum Kind { kFew, kShared, kTile128, kTile128Deep, kTile256 } kind;
-  int mt, nt, gk;   // kFew, kShared
+  int mt, nt, gk;   // kFew, kShared: row tiles of the activations, of the matrix a wave, waves that share a tile
   int splits, per;  // parts of K, blocks of one
 };
 
 // Rows of which all calls up to here are computed alike.
-int row_class(int M) { return M <= 64 ? (int)ceil_div(M, 16) * 16 : (int)std::min<int64_t>(ceil_div(M, 128) * 128, kMaxM8); }
+int row_class(int M) {
+  if (M <= kFewRows) return kFewRows;
+  return M <= 64 ? (int)ceil_div(M, 16) * 16 : (int)std::min<int64_t>(ceil_div(M, 128) * 128, kMaxM8);
+}
 
 // Many rows: the tile and the parts of K with the least time by the steps that the busiest compute unit takes.  Measured, us a
 // step of 128 columns: tiles of 256 x 256 1.35 alone and 2.0 on a full device; of 128 x 128 with four waves (two workgroups a
@@ -754,11 +717,22 @@ Plan plan_many(int M, int NT, int KB, bool f32) {
   }
   return best;
 }
+// Up to 128 rows, measured in us:
+// Up to 4 rows: no barrier and no second launch, but a workgroup has its tiles to itself: 1 x 4608 x 3584 6.5 (shared 7.5),
+// 1 x 8192 x 5120 9.7 (11.8), 1 x 3584 x 18944 14.1 (16.7).  Not between 256 and 512 tiles, where some compute units get two
+// workgroups and others one, and a long row: 1 x 5120 x 25600 30.9 (26.4).  Above 4 the rows are read too often:
+// 16 x 51200 x 5120 55.3 (51.4), 16 x 5120 x 25600 41.6 (26.4).
+// Tiles a wave of shared rows: two from 2048 row tiles on (33 x 51200 x 5120 48.5, with one 52.9); at 2048 one tile a wave makes 256
+// workgroups (33 x 32768 x 4096 27.7, with two 34.6).
+// Waves on one tile: four where there are few tiles and blocks (33 x 8192 x 4096 10.9, cut over K and joined 14.4; 33 x 5120 x 8192
+// 16.5 and 14.7).
+// 65 to 128 rows: shared where that is one launch of two tiles a wave (128 x 51200 x 5120 66, many rows' kernel 73); else many
+// rows' (128 x 10240 x 5120 25.6, shared 28.4; fp32 results 128 x 51200 x 5120 91 and 111).
 Plan plan_of(int M, int NT, int KB, bool f32) {
   M = row_class(M);
-  if (M <= 16) return Plan{Plan::kFew, 1, NT >= 512 ? 2 : 1, 1, 1, KB};
-  if (M > 128) return plan_many(M, NT, KB, f32);
-  Plan p = {Plan::kShared, M / 16, NT >= 2048 ? 2 : 1, 1, 1, KB};
+  if (M <= kFewRows && !(NT > 256 && NT < 512 && KB > 64)) return Plan{Plan::kFew, 1, NT >= 512 ? 2 : 1, 1, 1, KB};
+  if (M > 128 || (M > 64 && (NT <= 2048 || f32))) return plan_many(M, NT, KB, f32);
+  Plan p = {Plan::kShared, (int)ceil_div(M, 16), NT > 2048 ? 2 : 1, 1, 1, KB};
   if (M <= 64 && NT <= 512 && KB <= 32) {
     p.gk = 4;
   } else {
@@ -772,14 +746,13 @@ size_t plan_bytes(const Plan& p, int M, int NT) { return p.splits > 1 ? (size_t)
 
 template <int MT, int NT, int GK, bool E8, bool F32>
 void launch_shared(const MatArgs& a, hipStream_t st) {
-  const unsigned grid = (unsigned)(ceil_div(a.NT, 8 / GK * NT) * a.splits * ceil_div(a.M, 16 * MT));
-  hipLaunchKernelGGL((shared_rows_kernel<MT, NT, GK, !F32, E8, F32>), dim3(grid), dim3(kSharedThreads), 0, st, a);
+  const unsigned grid = (unsigned)(ceil_div(a.NT, 8 / GK * NT) * a.splits);
+  hipLaunchKernelGGL((shared_rows_kernel<MT, NT, GK, !F32 && (MT > 1), E8, F32>), dim3(grid), dim3(kSharedThreads), 0, st, a);
 }
 template <int MT, bool E8, bool F32>
 void launch_shared(const MatArgs& a, const Plan& p, hipStream_t st) {
   if (p.nt == 2) return launch_shared<MT, 2, 1, E8, F32>(a, st);
-  if constexpr (MT < 8)
-    if (p.gk == 4) return launch_shared<MT, 1, 4, E8, F32>(a, st);
+  if (p.gk == 4) return launch_shared<MT, 1, 4, E8, F32>(a, st);
   launch_shared<MT, 1, 1, E8, F32>(a, st);
 }
 template <int WN, int WM, int GN, int GM, int RS, bool E8, bool SCALED, bool F32>
@@ -795,16 +768,18 @@ int launch_matmul(MatArgs a, const Plan& p, hipStream_t st) {
   switch (p.kind) {
     case Plan::kFew:
       if (p.nt == 2)
-        hipLaunchKernelGGL((few_rows_kernel<1, 2, E8, F32>), dim3((a.NT + 1) / 2), dim3(kFewWaves * kWave), 0, st, a);
+        hipLaunchKernelGGL((few_rows_kernel<2, E8, F32>), dim3((a.NT + 1) / 2), dim3(kFewWaves * kWave), 0, st, a);
       else
-        hipLaunchKernelGGL((few_rows_kernel<1, 1, E8, F32>), dim3(a.NT), dim3(kFewWaves * kWave), 0, st, a);
+        hipLaunchKernelGGL((few_rows_kernel<1, E8, F32>), dim3(a.NT), dim3(kFewWaves * kWave), 0, st, a);
       break;
     case Plan::kShared:
       switch (p.mt) {
+        case 1: launch_shared<1, E8, F32>(a, p, st); break;
         case 2: launch_shared<2, E8, F32>(a, p, st); break;
         case 3: launch_shared<3, E8, F32>(a, p, st); break;
         case 4: launch_shared<4, E8, F32>(a, p, st); break;
-        default: launch_shared<8, E8, F32>(a, p, st);
+        default:
+          if constexpr (!F32) launch_shared<8, 2, 1, E8, F32>(a, st);
       }
       break;
     case Plan::kTile128: launch_many<4, 4, 2, 2, 2, E8, SCALED, F32>(a, st); break;
@@ -829,7 +804,7 @@ extern "C" int sdd_e4m3_matmul_workspace_bytes(const sdd_e4m3_matrix* m, int M, 
   // (fewer rows may be cut into more parts; over 4096 are in one)
   const int NT = (int)ceil_div(m->N, 16), KB = (int)ceil_div(m->K, kBlock8);
   *bytes = 0;
-  for (int rows = 16;; rows = row_class(rows + 1)) {
+  for (int rows = kFewRows;; rows = row_class(rows + 1)) {
     const int r = std::min(rows, M);
     for (int f32 = 0; f32 < 2; ++f32) *bytes = std::max(*bytes, plan_bytes(plan_of(r, NT, KB, f32), r, NT));
     if (rows >= M || rows > 4096) break;

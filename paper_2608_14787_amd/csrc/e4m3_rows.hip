@@ -102,7 +102,7 @@ __device__ inline void store_codes(uint8_t* to, const float* y, const Scale& sc)
     for (int j = 0; j < 4; ++j) {
       const float v = y[4 * i + j];
       q[j] = v * sc.inv;
-      q[j] = __builtin_fmaf(__builtin_fmaf(-q[j], sc.s, v), sc.inv, q[j]);
+      q[j] = __builtin_fmaf(-__builtin_fmaf(q[j], sc.s, -v), sc.inv, q[j]);  // (in this form -0 stays -0)
     }
     w[i] = sc.inv != sc.inv ? 0x7f7f7f7fu : codes4(q[0], q[1], q[2], q[3]);
   }

@@ -37,7 +37,8 @@ def check(S, M, N, K, scale, out, seed=0, wscale=None, where="cpu"):
 @pytest.mark.parametrize("M,N,K", [
     (1, 1, 16), (1, 16, 128), (1, 300, 3584), (2, 17, 144), (9, 512, 256), (15, 15, 240), (16, 130, 1040), (17, 256, 688), (32, 33, 2064),
     (33, 512, 1296), (33, 1040, 256), (48, 100, 400), (49, 47, 128), (64, 257, 1152), (1, 20000, 64), (5, 16400, 272), (40, 33000, 64),
-    (60, 20, 6000), (33, 600, 4240), (30, 9000, 272)])
+    (60, 20, 6000), (33, 600, 4240), (30, 9000, 272),
+    (1, 5000, 8208), (4, 4200, 8464), (5, 300, 3584), (7, 33000, 272), (16, 600, 4240), (3, 33000, 400), (33, 32768, 144)])
 def test_few_rows(S, M, N, K, scale, out):
     check(S, M, N, K, scale, out)
 
@@ -46,7 +47,8 @@ def test_few_rows(S, M, N, K, scale, out):
 @pytest.mark.parametrize("scale", ["f32", "e8m0"])
 @pytest.mark.parametrize("M,N,K", [
     (65, 1, 16), (65, 128, 128), (66, 300, 1296), (100, 17, 2064), (127, 130, 144), (128, 256, 512), (129, 255, 640), (200, 513, 272),
-    (257, 384, 1040), (264, 640, 1280), (511, 112, 2368), (600, 700, 64), (130, 20, 9008), (100, 33000, 144)])
+    (257, 384, 1040), (264, 640, 1280), (511, 112, 2368), (600, 700, 64), (130, 20, 9008), (100, 33000, 144), (128, 33000, 400),
+    (70, 32768, 272)])
 def test_many_rows(S, M, N, K, scale, out):
     check(S, M, N, K, scale, out)
 
@@ -160,12 +162,24 @@ def test_same_bits_again_and_in_a_graph(S, M):
     assert torch.equal(out, m.matmul(x, xs))
 
 
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("few,more", [(1, 4), (5, 16), (17, 32), (40, 48), (49, 64), (65, 128), (130, 256), (300, 384)])
+def test_bits_do_not_depend_on_the_rows_beside(S, few, more, out):
+    g = gen(few, more)
+    x, xs = R.random_codes(g, more, 1296, "f32")
+    w, ws = R.random_codes(g, 700, 1296, "f32", matrix=True)
+    m = S.E4M3Matrix(w.cuda(), ws.cuda())
+    want = m.matmul(x.cuda(), xs.cuda(), dtype=DT[out])
+    got = m.matmul(x[more - few:].cuda(), xs[:, more - few:].contiguous().cuda(), dtype=DT[out])
+    assert torch.equal(got, want[more - few:])
+
+
 def test_workspace_serves_fewer_rows(S):
     g = gen(5)
     w, ws = R.random_codes(g, 500, 2064, "f32", matrix=True)
     m = S.E4M3Matrix(w.cuda(), ws.cuda())
     room = m.workspace(600)
-    for M in (1, 33, 64, 65, 100, 128, 129, 200, 256, 300, 511, 600):  # (cut into other parts)
+    for M in (1, 4, 5, 16, 33, 64, 65, 100, 128, 129, 200, 256, 300, 511, 600):  # (cut into other parts)
         x, xs = (t.cuda() for t in R.random_codes(g, M, 2064, "f32"))
         assert torch.equal(m.matmul(x, xs, ws=room), m.matmul(x, xs))
 

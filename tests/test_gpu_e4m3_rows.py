@@ -90,6 +90,19 @@ def test_ties_to_even(S):
     assert torch.equal(codes.view(torch.uint8), x.to(torch.float8_e4m3fn).view(torch.uint8))
 
 
+@pytest.mark.parametrize("scale", ["f32", "e8m0"])
+@pytest.mark.parametrize("K", [16, 144])
+def test_zeros_keep_their_sign(S, K, scale):
+    x = torch.zeros(3, K)
+    x[:, 1::2] = -0.0
+    x[1, 4], x[2, 5] = 3.0, -2.0 ** 100
+    want = torch.where(x.signbit(), 0x80, 0)
+    for codes in (S.e4m3_quantize(x.cuda(), scale=scale)[0], S.e4m3_quantize_matrix(x.cuda(), scale=scale)[0]):
+        codes = codes.view(torch.uint8).cpu()
+        zero = x == 0
+        assert (codes[zero] == want[zero]).all()
+
+
 @pytest.mark.parametrize("scale,res,y", [("f32", "f32", True), ("e8m0", "bf16", False), ("f32", None, True), ("e8m0", None, False),
                                          ("f32", "bf16", True)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
