@@ -4,7 +4,9 @@
 // A block y with a = max |y|: s = max(a / 448, 2^-126), or the least power of two with a <= 448 s; codes = e4m3(y / s).  The
 // quotient is fp32's.
 // Bound: the memory, and for few rows the chain load, sum, maximum, store.  A lane holds 16 or 8 consecutive columns, 8 or 16
-// lanes a block: its maximum is a few steps inside a row of lanes, and no value changes lanes.
+// lanes a block: its maximum is a few steps inside a row of lanes, and no value changes lanes.  Read and written together (a
+// copy reaches 4.8 TB/s, a read stream 6.3 to 6.8): matrix 10240 x 5120 of bf16 24 us (6.6 TB/s), rows 2047 x 18944 after SwiGLU 33 (5.9),
+// 4095 x 5120 with an fp32 residual and y 49 (5.6); one row 2.6, 33 x 8192 2.8.
 #include <algorithm>
 
 #include "e4m3.h"
@@ -89,9 +91,8 @@ __device__ inline Scale scale_of(float a, bool e8) {
   const float s = fmaxf(a / 448.f, 0x1p-126f);
   return Scale{1.f / s, s, 0};
 }
-// P codes of y / s, stored past the caches (they are not read again before the product, and 100 to 300 MB of rows take 5 to 15%
-// less time so).  The quotient is a product with 1 / s
-// corrected by its remainder, as fp32's division rounds it.
+// P codes of y / s, stored past the caches (100 to 300 MB of rows take 5 to 15% less time so).  The quotient is a product with
+// 1 / s corrected by its remainder, as fp32's division rounds it.
 template <int P>
 __device__ inline void store_codes(uint8_t* to, const float* y, const Scale& sc) {
   uint32_t w[P / 4];

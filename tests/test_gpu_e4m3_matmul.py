@@ -26,7 +26,7 @@ def check(S, M, N, K, scale, out, seed=0, wscale=None, where="cpu"):
     w, ws = (t.to(where) for t in R.random_codes(g, N, K, wscale or scale, matrix=True))
     got = S.E4M3Matrix(w.cuda(), ws.cuda()).matmul(x.cuda(), xs.cuda(), dtype=DT[out]).to(where)
     want, mag = R.matmul(x, xs, w, ws)
-    tol = R.matmul_tol(want, mag, K, DT[out], R.group_max(x, xs, w, ws) if out == "bf16" else None)
+    tol = R.matmul_tol(want, mag, K, DT[out], R.group_max(x, xs, w, ws) if out == "bf16" and M > 16 else None)
     err = (got.double() - want).abs()
     assert got.shape == (M, N) and got.dtype == DT[out]
     assert (err <= tol).all(), (err / tol).max()
