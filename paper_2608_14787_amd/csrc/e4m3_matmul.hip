@@ -9,7 +9,7 @@
 // result, far below bf16's rounding of up to 2^-8 of it, so bf16 results take them (at half the time of bf16 products); fp32
 // results, and those of up to 16 rows, which wait for memory anyway, widen the codes to bf16, exactly, and sum in fp32.
 // Where both scales are powers of two and the result bf16, tiles of many rows hand them to the instruction, which then also
-// adds to the accumulators: no fp32 work is left beside the products (4095 x 51200 x 5120 915 us, 1048 with fp32 scales).
+// adds to the accumulators: no fp32 work is left beside the products (4095 x 51200 x 5120 920 us, 1048 with fp32 scales).
 //
 // Bound: up to about 300 rows the matrix's bytes (6.3 to 6.8 TB/s of a plain read stream on this card), then the products (2.5
 // to 3.1 PFLOP/s in large library products of fp8).
@@ -444,7 +444,7 @@ __global__ void __launch_bounds__(256) join_kernel(MatArgs a) {
 // of columns at a time, in a ring of RS that is loaded directly.  Scales come eight blocks at a time.
 // Bound by the products: 256 x 256 reads LDS 96 KiB for 256 products of 16x16x128, 32 clocks each on four cores, half of what LDS
 // could give meanwhile, and L2 64 KiB at 55 bytes a clock.  4095 x 51200 x 5120 1030 us (2.1 PFLOP/s), with powers of two as scales
-// 915 (2.3; 4096 x 8192 x 8192 218, 2.5), fp32 results 4095 x 5120 x 25600 937 (1.15: bf16 products).  At 128 x 128 loads, LDS
+// 920 (2.3; 4096 x 8192 x 8192 218, 2.5), fp32 results 4095 x 5120 x 25600 937 (1.15: bf16 products).  At 128 x 128 loads, LDS
 // and products take about as long each and overlap only in part: 511 x 3584 x 18944 39 us and 6.5 in the join (1.5 PFLOP/s),
 // 264 x 10240 x 5120 27 (31 by itself).
 
