@@ -82,7 +82,7 @@ __device__ inline void store4(const MatArgs& a, int m, int n, const f32x4& v) {
 // A workgroup takes NT row tiles of the matrix and all (up to 16) rows; its eight waves take every eighth block of 128
 // columns, each its own loads (no barrier in the loop), and join in LDS in wave order.  Bound by the matrix's bytes: each is read
 // once, 1 KiB of a wave at a time, past the caches (nothing else reads them).  1 x 51200 x 5120 46 us (5.7 TB/s), 1 x 18944 x 3584 15
-// (4.5), 1 x 4608 x 3584 5.7.  Two blocks in registers are enough: eight waves, two workgroups a compute unit.
+// (4.5), 1 x 4608 x 3584 6.5.  Two blocks of a wave in registers: with three these take 47, 17 and 7.3, with four 58, 18 and 7.7.
 
 constexpr int kFewWaves = 8, kFewRows = 4;
 
