@@ -545,6 +545,11 @@ def _rows2(x, name):
     return M, K, x.stride(0) if M > 1 else K, _dtype_code(x)
 
 
+def _like_rows(t, dtype, x, name):
+    if t.dtype != dtype or not t.is_contiguous() or t.shape != x.shape:
+        raise ValueError(f"{name} must be contiguous {dtype} {list(x.shape)}")
+
+
 def e4m3_quantize(x: torch.Tensor, *, scale: str = "f32", out=None, stream=None):
     """sdd_e4m3_quantize of rows x [M, K] (bf16 or fp32): (codes float8_e4m3fn [M, K], scales [ceil(K / 128), M]).
 
@@ -601,13 +606,14 @@ def e4m3_rmsnorm(x: torch.Tensor, gain: torch.Tensor, *, eps: float = 1e-6, resi
     used = [x, gain] if out is None else [x, gain, codes, scales]
     rd, res, res_out = F32, None, None
     if residual is not None:
+        rd = _dtype_code(residual)
+        _like_rows(residual, residual.dtype, x, "residual")
+        used.append(residual)
         if residual_out is None:
             residual_out = residual
-        rd = _dtype_code(residual)
-        for t, nm in ((residual, "residual"), (residual_out, "residual_out")):
-            if t.dtype != residual.dtype or not t.is_contiguous() or t.shape != x.shape:
-                raise ValueError(f"{nm} must be contiguous {residual.dtype} [{M}, {K}]")
-            used.append(t)
+        elif residual_out is not residual:
+            _like_rows(residual_out, residual.dtype, x, "residual_out")
+            used.append(residual_out)
         res, res_out = residual.data_ptr(), residual_out.data_ptr()
     else:
         _need(residual_out is None, "residual_out needs a residual")
@@ -616,8 +622,7 @@ def e4m3_rmsnorm(x: torch.Tensor, gain: torch.Tensor, *, eps: float = 1e-6, resi
     elif y is False or y is None:
         y = None
     else:
-        if y.dtype != torch.bfloat16 or not y.is_contiguous() or y.shape != x.shape:
-            raise ValueError(f"y must be contiguous bf16 [{M}, {K}]")
+        _like_rows(y, torch.bfloat16, x, "y")
         used.append(y)
     st = _here(*used)
     _check(lib().sdd_e4m3_rmsnorm(x.data_ptr(), dt, s0, res, res_out, rd, gain.data_ptr(), eps, M, K, codes.data_ptr(), scales.data_ptr(),
