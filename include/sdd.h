@@ -385,8 +385,11 @@ int sdd_e4m3_quantize_matrix(const void* x, int dtype, size_t row_stride, int N,
  * [M][K], SDD_BF16 or SDD_F32, NULL: r = x), written to residual_out in the
  * residual's type; y = r / sqrt(mean r^2 + eps) * gain (gain fp32 [K]) in fp32
  * from r before it is rounded, converted to codes and scales; y_out (may be
- * NULL) also receives y as bf16 [M][K].  K at most 65536.  Errors: as above, and
- * SDD_EUNSUPPORTED for a larger K. */
+ * NULL) also receives y as bf16 [M][K].  Squares that leave fp32's range do not
+ * matter: such a row is computed times a power of two.  An infinity
+ * makes NaN codes of its own block and zeros of the row's others; a row of zeros with
+ * eps 0 is 0 / 0, NaN codes.  K at most 65536.  Errors: as above, and SDD_EUNSUPPORTED
+ * for a larger K. */
 int sdd_e4m3_rmsnorm(const void* x, int dtype, size_t row_stride, const void* residual, void* residual_out,
                      int residual_dtype, const float* gain, float eps, int M, int K, uint8_t* codes, void* scales,
                      int scale_dtype, uint16_t* y_out, sdd_stream_t stream);

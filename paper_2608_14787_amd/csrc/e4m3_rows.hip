@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(256) rows_kernel(RowsArgs a, int segs) {
 template <typename T, typename RT, bool RES, int C>
 __global__ void __launch_bounds__(kMaxNormThreads) norm_kernel(RowsArgs a) {
   constexpr int P = 8;
-  __shared__ float s_sum[kMaxNormThreads / kWave];
+  __shared__ float s_sum[kMaxNormThreads / kWave], s_max[kMaxNormThreads / kWave];
   const int64_t m = blockIdx.x;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, waves = blockDim.x / kWave;
   const T* x = reinterpret_cast<const T*>(a.x) + m * a.stride;
@@ -211,7 +211,40 @@ __global__ void __launch_bounds__(kMaxNormThreads) norm_kernel(RowsArgs a) {
   __syncthreads();
   sum = 0.f;
   for (int w = 0; w < waves; ++w) sum += s_sum[w];
-  const float rs = 1.f / sqrtf(sum / (float)a.K + a.eps);
+  float eps = a.eps;
+  // Squares out of fp32's range (the whole workgroup sees the same sum): above, or so far below that those lost count.  At most
+  // 65536 squares lose 2^-150 each, 2^-34 of a sum of 2^-100; a mean below that is 2^-40 of an eps of 2^-60.  The row then starts
+  // again times a power of two that brings the larger of its maximum and sqrt(eps) to 1: y = r f / sqrt(mean (r f)^2 + eps f^2).
+  if (sum == INFINITY || (sum < 0x1p-100f && eps < 0x1p-60f)) {
+    float mx = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int i = 0; i < P; ++i) mx = fmaxf(mx, fabsf(y[c][i]));
+    mx = wave_max(mx);
+    if (lane == 0) s_max[wave] = mx;
+    __syncthreads();  // (s_sum has been read, too)
+    for (int w = 0; w < waves; ++w) mx = fmaxf(mx, s_max[w]);
+    mx = fmaxf(mx, sqrtf(eps));
+    if (mx > 0.f && mx < INFINITY) {
+      const float f = __builtin_bit_cast(float, (uint32_t)(127 - max(-126, min(126, __builtin_amdgcn_frexp_expf(mx)))) << 23);
+      sum = 0.f;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+          y[c][i] *= f;
+          sum = __builtin_fmaf(y[c][i], y[c][i], sum);
+        }
+      sum = wave_sum(sum);
+      if (lane == 0) s_sum[wave] = sum;
+      __syncthreads();
+      sum = 0.f;
+      for (int w = 0; w < waves; ++w) sum += s_sum[w];
+      eps = eps * f * f;
+    }
+  }
+  const float rs = 1.f / sqrtf(sum / (float)a.K + eps);
 #pragma unroll
   for (int c = 0; c < C; ++c) {
     const int col = (c * (int)blockDim.x + (int)threadIdx.x) * P;

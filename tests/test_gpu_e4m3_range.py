@@ -1,0 +1,64 @@
+"""Values at the ends of fp32's range in the 8-bit operators: tiny blocks, norms whose squares leave it, far gates, far scales."""
+import pytest
+import torch
+
+import e4m3_ref as R
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def S():
+    from paper_2608_14787_amd import sdd
+    return sdd
+
+
+def gen(*seed):
+    g = torch.Generator()
+    g.manual_seed(sum(s * 7919 ** i for i, s in enumerate(seed)) & 0x7fffffff)
+    return g
+
+
+NORM_ROWS = {  # factor of rows of size 1, eps
+    "large": (1e20, 2.0 ** -20), "largest": (2.0 ** 124, 2.0 ** -20), "one_large": (1.0, 2.0 ** -20), "small": (1e-25, 0.0),
+    "smallest": (2.0 ** -130, 0.0), "small_beside_eps": (2.0 ** -70, 2.0 ** -140), "eps_above": (2.0 ** -90, 2.0 ** -149),
+    "border": (2.0 ** 63, 2.0 ** -20), "low_border": (2.0 ** -53, 0.0)}
+
+
+@pytest.mark.parametrize("scale", ["f32", "e8m0"])
+@pytest.mark.parametrize("res", [None, "bf16", "f32"])
+@pytest.mark.parametrize("what", NORM_ROWS)
+@pytest.mark.parametrize("M,K,dtype", [(1, 16, "f32"), (3, 400, "bf16"), (2, 3584, "bf16"), (2, 40000, "f32")])
+def test_rmsnorm_squares_out_of_range(S, M, K, dtype, what, res, scale):
+    """Rows of finite values whose squares are none: the same y as of rows of size 1."""
+    size, eps = NORM_ROWS[what]
+    g = gen(M, K, len(what))
+    x = torch.randn(M, K, generator=g).clamp(-4, 4) * size
+    if what == "one_large":
+        x[:, K // 3] = 1e30
+    x = x.to(DT[dtype])
+    gain = 1 + 0.1 * torch.randn(K, generator=g)
+    r = None if res is None else (2 * size * torch.randn(M, K, generator=g).clamp(-4, 4)).to(DT[res])
+    held = None if r is None else r.cuda()
+    codes, scales, ro, yo = S.e4m3_rmsnorm(x.cuda(), gain.cuda(), eps=eps, residual=held, y=True, scale=scale)
+    codes, scales, yo = codes.cpu(), scales.cpu(), yo.cpu()
+    wr, wy, rel_r, rel_y = R.rmsnorm(x, r, gain, eps)
+    # a value far below its row's largest is a subnormal number, as it is in the row itself: half of 2^-149 times at most 1.5 * 256
+    R.check_codes(wy, codes, scales.t(), scale, rel=rel_y, least=2.0 ** -140)
+    assert ((yo.double() - wy).abs() <= wy.abs() * (rel_y + R.HALF[torch.bfloat16] * 1.01) + 2.0 ** -133).all()
+    if r is not None:
+        assert ((ro.cpu().double() - wr).abs() <= wr.abs() * (rel_r + R.HALF[DT[res]] * 1.01) + 2.0 ** -133).all()
+
+
+def test_rmsnorm_zero_rows_beside_far_ones(S):
+    """A row of zeros has no size: zeros with any eps above 0, no number with 0 (0 / 0); rows beside it do not matter."""
+    x = torch.zeros(4, 160)
+    x[1], x[3] = 1e25, 1e-30
+    gain = torch.ones(160).cuda()
+    codes, scales, _, y = (t if t is None else t.cpu() for t in S.e4m3_rmsnorm(x.cuda(), gain, eps=2.0 ** -120, y=True))
+    assert (codes[0::2].float() == 0).all() and (scales[:, 0::2] == 1).all() and (y[0::2] == 0).all()
+    assert ((y[1].float() - 1).abs() <= 2.0 ** -8).all() and ((y[3].float() - 1e-30 * 2.0 ** 60).abs() <= 2.0 ** -39 * 2.0 ** -8).all()
+    codes, scales, _, y = (t if t is None else t.cpu() for t in S.e4m3_rmsnorm(x.cuda(), gain, eps=0.0, y=True))
+    assert torch.isnan(y[0::2].float()).all() and torch.isnan(codes[0::2].float()).all() and (scales[:, 0::2] == 1).all()
+    assert ((y[1::2].float() - 1).abs() <= 2.0 ** -8).all()
