@@ -395,7 +395,9 @@ int sdd_e4m3_rmsnorm(const void* x, int dtype, size_t row_stride, const void* re
                      int scale_dtype, uint16_t* y_out, sdd_stream_t stream);
 
 /* SwiGLU before the down projection: row m of x holds K gate values and then K
- * of the up projection; y = g / (1 + e^-g) * u in fp32, converted. */
+ * of the up projection; y = g / (1 + e^-g) * u in fp32, converted.  e^-g is the fast
+ * exponential, off by up to (2 |g| + 2) 2^-24 of itself, 1e-5 at the most; where it
+ * passes fp32's range (g below -88.7) y is 0. */
 int sdd_e4m3_swiglu(const void* x, int dtype, size_t row_stride, int M, int K, uint8_t* codes, void* scales,
                     int scale_dtype, sdd_stream_t stream);
 

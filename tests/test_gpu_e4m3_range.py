@@ -62,3 +62,20 @@ def test_rmsnorm_zero_rows_beside_far_ones(S):
     codes, scales, _, y = (t if t is None else t.cpu() for t in S.e4m3_rmsnorm(x.cuda(), gain, eps=0.0, y=True))
     assert torch.isnan(y[0::2].float()).all() and torch.isnan(codes[0::2].float()).all() and (scales[:, 0::2] == 1).all()
     assert ((y[1::2].float() - 1).abs() <= 2.0 ** -8).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_swiglu_gates_next_to_the_end(S, dtype):
+    """Gates for which 1 + e^-g is next to fp32's largest number, with values that bring the result back: not zero."""
+    gates = [-86.0, -87.0, -87.5, -88.0, -88.5]
+    x = torch.zeros(len(gates), 2 * 256)
+    for m, g in enumerate(gates):
+        x[m, 3], x[m, 256 + 3] = g, 1e30
+        x[m, 200], x[m, 256 + 200] = g, -2.0
+    x = x.to(DT[dtype])
+    codes, scales = (t.cpu() for t in S.e4m3_swiglu(x.cuda()))
+    y, rel, _ = R.swiglu(x)
+    # the reciprocal's quarter may be a subnormal number of 22 bits; 2^-149: a step of products among the smallest numbers
+    R.check_codes(y, codes, scales.t(), "f32", rel=rel + 2.0 ** -22, least=2.0 ** -148)
+    v = codes.double() * R.spread(scales.double().t(), len(gates), 256, 1)
+    assert (v[:, 3] != 0).all() and ((v - y).abs() <= y.abs() * 2.0 ** -4 * 1.01 + 2.0 ** -135).all()
