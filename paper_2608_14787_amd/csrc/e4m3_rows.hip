@@ -72,38 +72,48 @@ __device__ inline float amax_block(float m) {  // over the 128 / P lanes of a bl
   return P == 16 ? m : fmaxf(m, dpp_f<kDppMirror>(m));
 }
 
+constexpr float kTinyScale = 0x1p-90f;
 struct Scale {
-  float inv;    // 1 / s; NaN: the block is not finite
+  float inv;    // 1 / by; NaN: the block is not finite
+  float by;     // what the values are divided by: s, or 2^64 s (and they are taken times 2^64)
   float s;
   int byte;     // of a power of two
 };
 __device__ inline Scale scale_of(float a, bool e8) {
-  if (a == INFINITY) return Scale{__builtin_nanf(""), 1.f, 127};
-  if (a == 0.f) return Scale{1.f, 1.f, 127};
+  if (a == INFINITY) return Scale{__builtin_nanf(""), 1.f, 1.f, 127};
+  if (a == 0.f) return Scale{1.f, 1.f, 1.f, 127};
   if (e8) {
     // a = f 2^x, f in [1, 2); 448 = 1.75 2^8
     const uint32_t u = __builtin_bit_cast(uint32_t, a);
     const int x = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u);
     const int byte = max(1, min(254, x + 127));
-    return Scale{__builtin_bit_cast(float, byte == 254 ? 0x00400000u : (uint32_t)(254 - byte) << 23),
-                 __builtin_bit_cast(float, (uint32_t)byte << 23), byte};
+    const float s = __builtin_bit_cast(float, (uint32_t)byte << 23);
+    return Scale{__builtin_bit_cast(float, byte == 254 ? 0x00400000u : (uint32_t)(254 - byte) << 23), s, s, byte};
   }
   const float s = fmaxf(a / 448.f, 0x1p-126f);
-  return Scale{1.f / s, s, 0};
+  const float by = s < kTinyScale ? s * 0x1p64f : s;
+  return Scale{1.f / by, by, s, 0};
 }
 // P codes of y / s, stored past the caches (100 to 300 MB of rows take 5 to 15% less time so).  The quotient is a product with
-// 1 / s corrected by its remainder, as fp32's division rounds it.
+// 1 / s corrected by its remainder, as fp32's division rounds it.  The lowest border between two codes is 2^-10, so that a remainder
+// that matters is a multiple of 2^-33 2^-23 s: below kTinyScale it could be lost under 2^-149, and the block is divided times 2^64.
 template <int P>
 __device__ inline void store_codes(uint8_t* to, const float* y, const Scale& sc) {
   uint32_t w[P / 4];
+  float v[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) v[i] = y[i];
+  if (sc.by != sc.s) {
+#pragma unroll
+    for (int i = 0; i < P; ++i) v[i] *= 0x1p64f;
+  }
 #pragma unroll
   for (int i = 0; i < P / 4; ++i) {
     float q[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const float v = y[4 * i + j];
-      q[j] = v * sc.inv;
-      q[j] = __builtin_fmaf(-__builtin_fmaf(q[j], sc.s, -v), sc.inv, q[j]);  // (in this form -0 stays -0)
+      q[j] = v[4 * i + j] * sc.inv;
+      q[j] = __builtin_fmaf(-__builtin_fmaf(q[j], sc.by, -v[4 * i + j]), sc.inv, q[j]);  // (in this form -0 stays -0)
     }
     w[i] = sc.inv != sc.inv ? 0x7f7f7f7fu : codes4(q[0], q[1], q[2], q[3]);
   }

@@ -79,3 +79,29 @@ def test_swiglu_gates_next_to_the_end(S, dtype):
     R.check_codes(y, codes, scales.t(), "f32", rel=rel + 2.0 ** -22, least=2.0 ** -148)
     v = codes.double() * R.spread(scales.double().t(), len(gates), 256, 1)
     assert (v[:, 3] != 0).all() and ((v - y).abs() <= y.abs() * 2.0 ** -4 * 1.01 + 2.0 ** -135).all()
+
+
+@pytest.mark.parametrize("top", [-124, -118, -116, -114, -110, -106, -100, -94, -60, 0, 100])
+def test_codes_are_the_nearest_of_fp32s_quotient(S, top):
+    """y / s next to every border between two codes, with the block's maximum between 2^top and 2^(top + 1): the codes that IEEE's
+    division and one rounding give, in blocks of the smallest numbers too."""
+    g = gen(top + 200)
+    M, K = 64, 1024
+    a = torch.ldexp(1 + torch.rand(M, K // 128, generator=g), torch.tensor(top))
+    s = torch.maximum(a / torch.full_like(a, 448), torch.tensor(2.0 ** -126))
+    c = torch.arange(0, 127, dtype=torch.uint8).view(torch.float8_e4m3fn).double()
+    mid = ((c[1:] + c[:-1]) / 2)[torch.randint(0, 126, (M, K), generator=g)]
+    x = (mid * s.double().repeat_interleave(128, 1)).float()
+    x = (x.view(torch.int32) + torch.randint(-2, 3, (M, K), generator=g).int()).clamp(min=0).view(torch.float32)
+    x = torch.minimum(x, a.repeat_interleave(128, 1))
+    x[:, ::128] = a
+    want = (x / s.repeat_interleave(128, 1)).to(torch.float8_e4m3fn).view(torch.uint8)
+    codes, scales = S.e4m3_quantize(x.cuda())
+    assert torch.equal(scales.cpu().t(), s)
+    assert torch.equal(codes.cpu().view(torch.uint8), want)
+    # a matrix of one block a tile of 128 rows: the same rule with the tile's maximum
+    xm = x[:, :128]
+    sm = torch.maximum(xm.max() / torch.tensor(448.0), torch.tensor(2.0 ** -126))
+    codes, scales = S.e4m3_quantize_matrix(xm.cuda())
+    assert scales.item() == sm.item()
+    assert torch.equal(codes.cpu().view(torch.uint8), (xm / sm).to(torch.float8_e4m3fn).view(torch.uint8))
