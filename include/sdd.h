@@ -427,10 +427,11 @@ int sdd_e4m3_matmul_workspace_bytes(const sdd_e4m3_matrix* m, int M, size_t* byt
  * r < M: codes x [M][K] (16-byte aligned) and scales xs [ceil(K / 128)][M] as the
  * operators above leave them; out SDD_BF16 or SDD_F32, rows out_stride elements
  * apart (elements between them are left alone).
- * Products of a block are summed by the matrix cores, blocks in fp32 with xs ws,
- * one fp32 product (both scales SDD_E8M0 and out SDD_BF16: in the matrix cores).  The
- * result is rounded once.  Of fp32 results, and of up to 16 rows, all sums are fp32; of bf16
- * results of more rows the products of 8 consecutive columns are summed to 13 bits
+ * Products of a block are summed by the matrix cores, blocks in fp32 with xs ws.  That is
+ * one fp32 product and has to lie in fp32's range (past it: infinity, and NaN where a block's sum is
+ * 0; below it: 0), but where both scales are SDD_E8M0: then it is the sum times both that counts
+ * (of scales with a product up to 2^200).  The result is rounded once.  Of fp32 results, and
+ * of up to 16 rows, all sums are fp32; of bf16 results of more rows the products of 8 consecutive columns are summed to 13 bits
  * below the largest of them (about 1e-5 of a result).
  * The order of sums is fixed by the shapes, types and the count of rows, as one of 4, 16, 32,
  * 48, 64 or a multiple of 128 (the next one up): results are bit-reproducible, and a

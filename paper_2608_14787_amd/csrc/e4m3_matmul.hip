@@ -8,8 +8,9 @@
 // exponents, E, and cut what lies under 2^(E - 13); the groups' sums are added in 24 bits or more.  That is an error about 1e-5 of a
 // result, far below bf16's rounding of up to 2^-8 of it, so bf16 results take them (at half the time of bf16 products); fp32
 // results, and those of up to 16 rows, which wait for memory anyway, widen the codes to bf16, exactly, and sum in fp32.
-// Where both scales are powers of two and the result bf16, tiles of many rows hand them to the instruction, which then also
-// adds to the accumulators: no fp32 work is left beside the products (4095 x 51200 x 5120 920 us, 1048 with fp32 scales).
+// Where both scales are powers of two the fp8 instruction takes them; in tiles of many rows it then also adds to the accumulators,
+// and no fp32 work is left beside the products (4095 x 51200 x 5120 920 us, 1048 with fp32 scales).  Widened codes take the
+// matrix's scale with them.
 //
 // Bound: up to about 300 rows the matrix's bytes (6.3 to 6.8 TB/s of a plain read stream on this card), then the products (2.5
 // to 3.1 PFLOP/s in large library products of fp8).
@@ -37,18 +38,24 @@ struct MatArgs {
   float* part;
 };
 
-template <bool E8>
-__device__ inline float x_scale(const MatArgs& a, int kb, int m) {
-  const int64_t i = (int64_t)kb * a.M + m;
-  return E8 ? e8m0_value(reinterpret_cast<const uint8_t*>(a.xs)[i]) : reinterpret_cast<const float*>(a.xs)[i];
+// A power of two w as a product of two, b in 2^-100 .. 2^100 and a = w / b (NaN where w is).  Where both scales are powers of two
+// xs ws may lie outside fp32's range and the result not: the matrix's codes are then widened times b, and a block's sum is
+// multiplied by xs a.  Up to xs ws = 2^200 neither overflows before the result does (128 x 448^2 is less than 2^25).
+struct Factors {
+  float a, b;
+};
+__device__ inline Factors factors(float w) {
+  const float b = fminf(fmaxf(w, 0x1p-100f), 0x1p100f);
+  return Factors{w * __builtin_bit_cast(float, 0x7f000000u - __builtin_bit_cast(uint32_t, b)), b};
 }
+__device__ inline int byte_of(float power) { return (int)(__builtin_bit_cast(uint32_t, power) >> 23 & 255); }
 
-// Eight codes to bf16, exactly.
-__device__ inline bf16x8 widen(uint32_t lo, uint32_t hi) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, 1.f, false);
-  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, 1.f, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, 1.f, false);
-  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, 1.f, true);
+// Eight codes times a power of two (2^-100 .. 2^100) to bf16, exactly.
+__device__ inline bf16x8 widen(uint32_t lo, uint32_t hi, float by = 1.f) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, by, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)lo, by, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, by, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)hi, by, true);
   return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
@@ -95,7 +102,7 @@ struct Few {  // a wave's codes and scales of one block of columns
 
 constexpr int kNowhere = 0x7ffffff0;  // an offset past every descriptor's end: zeros, and no memory is read
 
-template <int NT, bool E8, bool F32>
+template <int NT, bool E8, bool BOTH, bool F32>
 __global__ void __launch_bounds__(kFewWaves * kWave, 2) few_rows_kernel(MatArgs a) {
   __shared__ __align__(16) f32x4 s_part[kFewWaves][NT][kWave];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
@@ -132,6 +139,10 @@ __global__ void __launch_bounds__(kFewWaves * kWave, 2) few_rows_kernel(MatArgs 
 #pragma unroll
   for (int j = 0; j < NT; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   auto multiply = [&](const Few<NT>& s) {
+    const float xs = E8 ? e8m0_value(s.xs) : __builtin_bit_cast(float, s.xs);
+    Factors ws[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) ws[j] = BOTH ? factors(s.ws[j]) : Factors{s.ws[j], 1.f};
     f32x4 p[NT];
 #pragma unroll
     for (int j = 0; j < NT; ++j) p[j] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -142,12 +153,11 @@ __global__ void __launch_bounds__(kFewWaves * kWave, 2) few_rows_kernel(MatArgs 
         const bf16x8 x = widen(s.x[h][2 * c], s.x[h][2 * c + 1]);
 #pragma unroll
         for (int j = 0; j < NT; ++j)
-          p[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(s.w[j][h][2 * c], s.w[j][h][2 * c + 1]), x, p[j], 0, 0, 0);
+          p[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(s.w[j][h][2 * c], s.w[j][h][2 * c + 1], ws[j].b), x, p[j], 0, 0, 0);
       }
-    const float xs = E8 ? e8m0_value(s.xs) : __builtin_bit_cast(float, s.xs);
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
-      const float sc = xs * s.ws[j];
+      const float sc = xs * ws[j].a;
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[j][e] = __builtin_fmaf(p[j][e], sc, acc[j][e]);
     }
@@ -186,7 +196,7 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kSharedThreads = 512;
 
-template <int MT, int NT, int GK, bool FP8, bool E8, bool F32>
+template <int MT, int NT, int GK, bool FP8, bool E8, bool BOTH, bool F32>
 __global__ void __launch_bounds__(kSharedThreads, 2) shared_rows_kernel(MatArgs a) {
   constexpr int R = MT >= 8 ? 2 : 4;           // blocks of a wave in registers
   constexpr int CB = MT >= 8 ? 2 : 4;          // blocks of a chunk
@@ -198,10 +208,11 @@ __global__ void __launch_bounds__(kSharedThreads, 2) shared_rows_kernel(MatArgs 
   constexpr int PIECES = kRows * CB * 8 / kSharedThreads;  // 16-byte pieces of a chunk a thread moves
   static_assert(kRows * CB * 8 % kSharedThreads == 0, "pieces of a chunk over the threads");
   constexpr int XS = (CB * kRows + kSharedThreads - 1) / kSharedThreads;
+  constexpr bool SCALED = BOTH && FP8;  // the instruction takes the scales
   union Shared {
     struct {
       u32x4 x[2][MT][CB][2][kWave];
-      float xs[2][CB][kRows];
+      uint32_t xs[2][CB][kRows];  // the scales, fp32 (SCALED: their bytes)
     } in;
     f32x4 part[GK > 1 ? 8 : 1][MT * NT][kWave];
   };
@@ -238,7 +249,7 @@ __global__ void __launch_bounds__(kSharedThreads, 2) shared_rows_kernel(MatArgs 
   constexpr int STEP = kSharedThreads / (CB * 8);
   struct X {
     u32x4 piece[PIECES];
-    float scale[XS];
+    uint32_t scale[XS];  // as in memory; behind the part's end 0
   };
   auto load_x = [&](X& v, int i) {
 #pragma unroll
@@ -253,8 +264,11 @@ __global__ void __launch_bounds__(kSharedThreads, 2) shared_rows_kernel(MatArgs 
     for (int p = 0; p < XS; ++p) {
       const int at = threadIdx.x + p * kSharedThreads, kb = at / kRows, r = at % kRows;
       const bool ok = kb < CB && i + kb < n;
-      const float xs = x_scale<E8>(a, ok ? k0 + i + kb : k0, min(r, a.M - 1));
-      v.scale[p] = ok ? xs : 0.f;
+      const int64_t from = (int64_t)(ok ? k0 + i + kb : k0) * a.M + min(r, a.M - 1);
+      if constexpr (E8)
+        v.scale[p] = ok ? reinterpret_cast<const uint8_t*>(a.xs)[from] : 0u;
+      else
+        v.scale[p] = ok ? reinterpret_cast<const uint32_t*>(a.xs)[from] : 0u;
     }
   };
   auto store_x = [&](const X& v, int buf) {
@@ -267,7 +281,8 @@ __global__ void __launch_bounds__(kSharedThreads, 2) shared_rows_kernel(MatArgs 
 #pragma unroll
     for (int p = 0; p < XS; ++p) {
       const int at = threadIdx.x + p * kSharedThreads;
-      if (at < CB * kRows) s.in.xs[buf][at / kRows][at % kRows] = v.scale[p];
+      if (at >= CB * kRows) continue;
+      s.in.xs[buf][at / kRows][at % kRows] = E8 && !SCALED ? __builtin_bit_cast(uint32_t, e8m0_value(v.scale[p])) : v.scale[p];
     }
   };
   f32x4 acc[MT][NT];
@@ -281,7 +296,7 @@ __global__ void __launch_bounds__(kSharedThreads, 2) shared_rows_kernel(MatArgs 
   static_assert(MT % G == 0, "whole groups");
   struct F {
     u32x4 x[G][2];
-    float xs[G];
+    uint32_t xs[G];
   };
   auto read_x = [&](F& f, int buf, int kb, int g) {
 #pragma unroll
@@ -292,6 +307,9 @@ __global__ void __launch_bounds__(kSharedThreads, 2) shared_rows_kernel(MatArgs 
     }
   };
   auto multiply = [&](const W& r, int buf, int kb) {
+    Factors ws[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) ws[j] = BOTH && !SCALED ? factors(r.ws[j]) : Factors{r.ws[j], 1.f};
     F f[2];
     read_x(f[0], buf, kb, 0);
 #pragma unroll
@@ -309,7 +327,10 @@ __global__ void __launch_bounds__(kSharedThreads, 2) shared_rows_kernel(MatArgs 
                               (int)r.w[j][1][0], (int)r.w[j][1][1], (int)r.w[j][1][2], (int)r.w[j][1][3]};
             const i32x8 xf = {(int)v.x[i][0][0], (int)v.x[i][0][1], (int)v.x[i][0][2], (int)v.x[i][0][3],
                               (int)v.x[i][1][0], (int)v.x[i][1][1], (int)v.x[i][1][2], (int)v.x[i][1][3]};
-            p[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf, xf, p[i][j], 0, 0, 0, 127, 0, 127);
+            if constexpr (SCALED)
+              p[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf, xf, p[i][j], 0, 0, 0, byte_of(r.ws[j]), 0, (int)v.xs[i]);
+            else
+              p[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf, xf, p[i][j], 0, 0, 0, 127, 0, 127);
           }
         }
       if constexpr (!FP8) {
@@ -319,7 +340,7 @@ __global__ void __launch_bounds__(kSharedThreads, 2) shared_rows_kernel(MatArgs 
           for (int c = 0; c < 2; ++c) {
             bf16x8 wf[NT];
 #pragma unroll
-            for (int j = 0; j < NT; ++j) wf[j] = widen(r.w[j][h][2 * c], r.w[j][h][2 * c + 1]);
+            for (int j = 0; j < NT; ++j) wf[j] = widen(r.w[j][h][2 * c], r.w[j][h][2 * c + 1], ws[j].b);
 #pragma unroll
             for (int i = 0; i < G; ++i) {
               const bf16x8 xf = widen(v.x[i][h][2 * c], v.x[i][h][2 * c + 1]);
@@ -332,9 +353,15 @@ __global__ void __launch_bounds__(kSharedThreads, 2) shared_rows_kernel(MatArgs 
       for (int i = 0; i < G; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
-          const float sc = v.xs[i] * r.ws[j];
+          f32x4& c = acc[g * G + i][j];
+          if constexpr (SCALED) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) acc[g * G + i][j][e] = __builtin_fmaf(p[i][j][e], sc, acc[g * G + i][j][e]);
+            for (int e = 0; e < 4; ++e) c[e] += p[i][j][e];
+          } else {
+            const float sc = __builtin_bit_cast(float, v.xs[i]) * ws[j].a;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c[e] = __builtin_fmaf(p[i][j][e], sc, c[e]);
+          }
         }
     }
     // (the products stay in their step: unpinned, they are moved behind the loads and barriers of later ones)
@@ -486,8 +513,9 @@ __device__ inline i32x8 fragment(const u32x4& a, const u32x4& b) {
 constexpr int kStripe = 12;
 constexpr int kScaleSteps = 8;  // blocks whose scales lie in LDS at a time (in two halves)
 
-template <int WN, int WM, int GN, int GM, int RS, bool FP8, bool E8, bool SCALED, bool F32>
+template <int WN, int WM, int GN, int GM, int RS, bool FP8, bool E8, bool BOTH, bool F32>
 __global__ void __launch_bounds__(kWave * GN * GM, 2) many_rows_kernel(MatArgs a) {
+  constexpr bool SCALED = BOTH && FP8;  // the instruction takes the scales
   constexpr int kWaves = GN * GM, kThreads = kWave * kWaves, BN = 16 * WN * GN, BM = 16 * WM * GM;
   constexpr int LW = BN / 16 / kWaves, LX = BM / 8 / kWaves;  // KiB of a step that a wave loads, of each half of the tiles and of the rows
   constexpr int HALF = WN / 2;                                // a wave's tiles of a half
@@ -565,6 +593,7 @@ __global__ void __launch_bounds__(kWave * GN * GM, 2) many_rows_kernel(MatArgs a
   struct Rows {  // fragments of a wave's rows for a step, and the products of their scales with the matrix's
     u32x4 x[WM][2];
     float sc[WM];
+    float wb;        // (BOTH: what the matrix's codes are widened times)
     int xs[WM], ws;  // (SCALED: their bytes)
   };
   const int p0 = (g4 ^ (r16 % 8)) * 16, p1 = ((4 + g4) ^ (r16 % 8)) * 16;
@@ -576,14 +605,16 @@ __global__ void __launch_bounds__(kWave * GN * GM, 2) many_rows_kernel(MatArgs a
   auto read_scales = [&](Rows& r, int i) {
     const int half = i / kScaleSteps % 2, step = i % kScaleSteps;
     const float w1 = s_ws[half][step * (BN / 128) + wn * WN / 8];
-    if constexpr (SCALED) r.ws = (int)(__builtin_bit_cast(uint32_t, w1) >> 23 & 255);
+    if constexpr (SCALED) r.ws = byte_of(w1);
+    const Factors w = BOTH && !SCALED ? factors(w1) : Factors{w1, 1.f};
+    r.wb = w.b;
 #pragma unroll
     for (int j = 0; j < WM; ++j) {
       const uint32_t xs = s_xs[half][step][(wm * WM + j) * 16 + r16];
       if constexpr (SCALED)
         r.xs[j] = (int)xs;
       else
-        r.sc[j] = (E8 ? e8m0_value(xs) : __builtin_bit_cast(float, xs)) * w1;
+        r.sc[j] = (E8 ? e8m0_value(xs) : __builtin_bit_cast(float, xs)) * w.a;
     }
   };
   // tiles read ahead, and the registers that they turn through (256 x 256 has none left for more)
@@ -634,7 +665,8 @@ __global__ void __launch_bounds__(kWave * GN * GM, 2) many_rows_kernel(MatArgs a
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int c = 0; c < 2; ++c)
-            q = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(f[h][2 * c], f[h][2 * c + 1]), widen(r.x[j][h][2 * c], r.x[j][h][2 * c + 1]), q, 0, 0, 0);
+            q = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(f[h][2 * c], f[h][2 * c + 1], BOTH ? r.wb : 1.f),
+                                                        widen(r.x[j][h][2 * c], r.x[j][h][2 * c + 1]), q, 0, 0, 0);
       }
       if (t >= kLag) add(t - kLag);
       __builtin_amdgcn_sched_barrier(0);
@@ -764,48 +796,48 @@ Plan plan_of(int M, int NT, int KB, bool f32) {
 }
 size_t plan_bytes(const Plan& p, int M, int NT) { return p.splits > 1 ? (size_t)p.splits * M * NT * 16 * 4 : 0; }
 
-template <int MT, int NT, int GK, bool E8, bool F32>
+template <int MT, int NT, int GK, bool E8, bool BOTH, bool F32>
 void launch_shared(const MatArgs& a, hipStream_t st) {
   const unsigned grid = (unsigned)(ceil_div(a.NT, 8 / GK * NT) * a.splits);
-  hipLaunchKernelGGL((shared_rows_kernel<MT, NT, GK, !F32 && (MT > 1), E8, F32>), dim3(grid), dim3(kSharedThreads), 0, st, a);
+  hipLaunchKernelGGL((shared_rows_kernel<MT, NT, GK, !F32 && (MT > 1), E8, BOTH, F32>), dim3(grid), dim3(kSharedThreads), 0, st, a);
 }
-template <int MT, bool E8, bool F32>
+template <int MT, bool E8, bool BOTH, bool F32>
 void launch_shared(const MatArgs& a, const Plan& p, hipStream_t st) {
-  if (p.nt == 2) return launch_shared<MT, 2, 1, E8, F32>(a, st);
-  if (p.gk == 4) return launch_shared<MT, 1, 4, E8, F32>(a, st);
-  launch_shared<MT, 1, 1, E8, F32>(a, st);
+  if (p.nt == 2) return launch_shared<MT, 2, 1, E8, BOTH, F32>(a, st);
+  if (p.gk == 4) return launch_shared<MT, 1, 4, E8, BOTH, F32>(a, st);
+  launch_shared<MT, 1, 1, E8, BOTH, F32>(a, st);
 }
-template <int WN, int WM, int GN, int GM, int RS, bool E8, bool SCALED, bool F32>
+template <int WN, int WM, int GN, int GM, int RS, bool E8, bool BOTH, bool F32>
 void launch_many(const MatArgs& a, hipStream_t st) {
   const int64_t items = ceil_div(a.NT, WN * GN) * a.splits, m_blocks = ceil_div(a.M, 16 * WM * GM);
-  hipLaunchKernelGGL((many_rows_kernel<WN, WM, GN, GM, RS, !F32, E8, SCALED, F32>), dim3((unsigned)(ceil_div(items, kXcds) * kXcds * m_blocks)),
+  hipLaunchKernelGGL((many_rows_kernel<WN, WM, GN, GM, RS, !F32, E8, BOTH, F32>), dim3((unsigned)(ceil_div(items, kXcds) * kXcds * m_blocks)),
                      dim3(kWave * GN * GM), 0, st, a);
 }
-template <bool E8, bool SCALED, bool F32>
+template <bool E8, bool BOTH, bool F32>
 int launch_matmul(MatArgs a, const Plan& p, hipStream_t st) {
   a.splits = p.splits;
   a.per = p.per;
   switch (p.kind) {
     case Plan::kFew:
       if (p.nt == 2)
-        hipLaunchKernelGGL((few_rows_kernel<2, E8, F32>), dim3((a.NT + 1) / 2), dim3(kFewWaves * kWave), 0, st, a);
+        hipLaunchKernelGGL((few_rows_kernel<2, E8, BOTH, F32>), dim3((a.NT + 1) / 2), dim3(kFewWaves * kWave), 0, st, a);
       else
-        hipLaunchKernelGGL((few_rows_kernel<1, E8, F32>), dim3(a.NT), dim3(kFewWaves * kWave), 0, st, a);
+        hipLaunchKernelGGL((few_rows_kernel<1, E8, BOTH, F32>), dim3(a.NT), dim3(kFewWaves * kWave), 0, st, a);
       break;
     case Plan::kShared:
       switch (p.mt) {
-        case 1: launch_shared<1, E8, F32>(a, p, st); break;
-        case 2: launch_shared<2, E8, F32>(a, p, st); break;
-        case 3: launch_shared<3, E8, F32>(a, p, st); break;
-        case 4: launch_shared<4, E8, F32>(a, p, st); break;
+        case 1: launch_shared<1, E8, BOTH, F32>(a, p, st); break;
+        case 2: launch_shared<2, E8, BOTH, F32>(a, p, st); break;
+        case 3: launch_shared<3, E8, BOTH, F32>(a, p, st); break;
+        case 4: launch_shared<4, E8, BOTH, F32>(a, p, st); break;
         default:
-          if constexpr (!F32) launch_shared<8, 2, 1, E8, F32>(a, st);
+          if constexpr (!F32) launch_shared<8, 2, 1, E8, BOTH, F32>(a, st);
       }
       break;
-    case Plan::kTile128: launch_many<4, 4, 2, 2, 2, E8, SCALED, F32>(a, st); break;
-    case Plan::kTile128Deep: launch_many<4, 2, 2, 4, 4, E8, SCALED, F32>(a, st); break;
+    case Plan::kTile128: launch_many<4, 4, 2, 2, 2, E8, BOTH, F32>(a, st); break;
+    case Plan::kTile128Deep: launch_many<4, 2, 2, 4, 4, E8, BOTH, F32>(a, st); break;
     case Plan::kTile256:
-      if constexpr (!F32) launch_many<8, 4, 2, 4, 2, E8, SCALED, F32>(a, st);
+      if constexpr (!F32) launch_many<8, 4, 2, 4, 2, E8, BOTH, F32>(a, st);
   }
   if (p.splits > 1)
     hipLaunchKernelGGL((join_kernel<F32>), dim3((unsigned)ceil_div(a.NT, 64), (unsigned)a.M), dim3(256), 0, st, a);
@@ -871,13 +903,13 @@ extern "C" int sdd_e4m3_matmul(const sdd_e4m3_matrix* m, const uint8_t* x, const
   hipStream_t st = reinterpret_cast<hipStream_t>(stream);
   prof_begin(PROF_GEMM8, st);
   int rc;
-  const bool e8 = scale_dtype == SDD_E8M0;
-  if (out_dtype == SDD_F32)
-    rc = e8 ? launch_matmul<true, false, true>(a, p, st) : launch_matmul<false, false, true>(a, p, st);
-  else if (e8 && m->scale_dtype == SDD_E8M0)
-    rc = launch_matmul<true, true, false>(a, p, st);
+  const bool f32 = out_dtype == SDD_F32;
+  if (scale_dtype == SDD_F32)
+    rc = f32 ? launch_matmul<false, false, true>(a, p, st) : launch_matmul<false, false, false>(a, p, st);
+  else if (m->scale_dtype == SDD_E8M0)
+    rc = f32 ? launch_matmul<true, true, true>(a, p, st) : launch_matmul<true, true, false>(a, p, st);
   else
-    rc = e8 ? launch_matmul<true, false, false>(a, p, st) : launch_matmul<false, false, false>(a, p, st);
+    rc = f32 ? launch_matmul<true, false, true>(a, p, st) : launch_matmul<true, false, false>(a, p, st);
   prof_end(PROF_GEMM8, st);
   return rc;
 }

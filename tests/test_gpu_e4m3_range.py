@@ -105,3 +105,53 @@ def test_codes_are_the_nearest_of_fp32s_quotient(S, top):
     codes, scales = S.e4m3_quantize_matrix(xm.cuda())
     assert scales.item() == sm.item()
     assert torch.equal(codes.cpu().view(torch.uint8), (xm / sm).to(torch.float8_e4m3fn).view(torch.uint8))
+
+
+def far_pairs(M, N, K):
+    """Codes and power-of-two scales: block 0 has pairs of scales whose product passes fp32's range at either end, block 1 ordinary ones.
+    Rows by m % 4: zeros in block 0, one product of the smallest codes, two that cancel, scales far down."""
+    g = gen(M, N, K)
+    x = torch.zeros(M, K)
+    x[:, 128:] = torch.randint(-4, 5, (M, K - 128), generator=g).float()
+    w = torch.zeros(N, K)
+    w[:, 128:] = torch.randint(-4, 5, (N, K - 128), generator=g).float()
+    w[:, 1], w[:, 5], w[:, 9] = 2.0 ** -9, 1.5, 1.5
+    w[:, 16:128] = 448.0
+    xb = torch.full((R.blocks(K), M), 127)
+    x[1::4, 1] = 2.0 ** -9
+    x[2::4, 5], x[2::4, 9] = 3.0, -3.0
+    x[3::4, 16:128] = 448.0
+    x[3::4, 128:] = 0
+    xb[0, :] = 127 + 100
+    xb[0, 3::4] = 127 - 100 - 80
+    wb = torch.full((R.blocks(N), R.blocks(K)), 127)
+    wb[:, 0] = 127 + 30
+    f8 = lambda t: t.to(torch.float8_e4m3fn)  # noqa: E731
+    e8 = lambda t: t.clamp(0, 254).to(torch.uint8).view(torch.float8_e8m0fnu)  # noqa: E731
+    return f8(x), e8(xb), f8(w), e8(wb)
+
+
+@pytest.mark.parametrize("out", ["bf16", "f32"])
+@pytest.mark.parametrize("M,N", [(1, 40), (4, 300), (4, 9000), (4, 6000), (16, 300), (33, 300), (33, 33000), (64, 1040), (100, 33000), (70, 200), (200, 300),
+                                 (300, 2100)])
+def test_powers_of_two_whose_product_is_out_of_range(S, M, N, out):
+    """Scales of 2^100 and 2^30 (and of 2^-127 and 2^-23): a block's sum times
+    both is what counts, however many rows there are."""
+    K = 272
+    x, xs, w, ws = far_pairs(M, N, K)
+    for wb0 in (157, 127 - 23):  # 2^30, 2^-23
+        b = ws.view(torch.uint8).clone()
+        b[:, 0] = wb0
+        ws = b.view(torch.float8_e8m0fnu)
+        got = S.E4M3Matrix(w.cuda(), ws.cuda()).matmul(x.cuda(), xs.cuda(), dtype=DT[out]).cpu()
+        want, mag = R.matmul(x, xs, w, ws)
+        assert torch.isfinite(got).all()
+        tol = R.matmul_tol(want, mag, K, DT[out], R.group_max(x, xs, w, ws) if out == "bf16" and M > 16 else None)
+        err = (got.double() - want).abs()
+        assert (err <= tol).all(), (err / tol).max()
+    b[:, 0] = 227  # 2^100 both: zeros and sums that cancel stay what they are, what passes the type's range is infinite
+    got = S.E4M3Matrix(w.cuda(), b.view(torch.float8_e8m0fnu).cuda()).matmul(x.cuda(), xs.cuda(), dtype=DT[out]).cpu()
+    plain, _ = R.matmul(x[:, 128:], xs[1:], w[:, 128:], ws[:, 1:])
+    plain = plain.to(DT[out])  # (whole numbers under 2^12, which every sum holds)
+    assert torch.equal(got[0::4], plain[0::4]) and torch.equal(got[2::4], plain[2::4])
+    assert (got[1::4] == float("inf")).all()
