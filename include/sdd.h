@@ -430,9 +430,14 @@ int sdd_e4m3_matmul_workspace_bytes(const sdd_e4m3_matrix* m, int M, size_t* byt
  * Products of a block are summed by the matrix cores, blocks in fp32 with xs ws.  That is
  * one fp32 product and has to lie in fp32's range (past it: infinity, and NaN where a block's sum is
  * 0; below it: 0), but where both scales are SDD_E8M0: then it is the sum times both that counts
- * (of scales with a product up to 2^200).  The result is rounded once.  Of fp32 results, and
- * of up to 16 rows, all sums are fp32; of bf16 results of more rows the products of 8 consecutive columns are summed to 13 bits
- * below the largest of them (about 1e-5 of a result).
+ * (of scales with a product up to 2^200).  The result is rounded once.
+ * Of fp32 results, and of up to 16 rows, all sums are fp32.  Of bf16 results of more rows each
+ * group of 8 columns (8 i .. 8 i + 7) has its products cut toward zero at 2^(E - 13), E the largest
+ * sum of two codes' exponents in it: the group is off by less than 7 2^-13 of its largest |product|.  That is
+ * an error relative to the products, not to the result; where large ones cancel, nothing may
+ * be left of a small result.  As a whole, with signs at random and 2% of a row's columns twenty times
+ * as large, its root mean square is 4.5e-5 of that of the results.  A row's errors are thus of another kind
+ * in calls of 17 rows than of 16; fp32 results have none of it.
  * The order of sums is fixed by the shapes, types and the count of rows, as one of 4, 16, 32,
  * 48, 64 or a multiple of 128 (the next one up): results are bit-reproducible, and a
  * row's do not depend on what the other rows hold.  A NaN code or scale makes NaN of
