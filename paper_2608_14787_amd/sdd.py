@@ -636,7 +636,8 @@ class MatrixDesc(C.Structure):
 
 class E4M3Matrix:
     """A matrix [N, K] (PyTorch Linear [out][in]) of e4m3 codes with a scale for each 128 x 128 block, laid out once for the
-    product in a torch-owned device buffer (codes and scales are not referenced afterwards)."""
+    product in a torch-owned device buffer.  codes and scales may be dropped at once, also where the layout runs on `stream`
+    (but not written to before that is through).  The buffer belongs to the stream that it is made on."""
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, stream=None):
         _codes(codes, "codes")
@@ -652,6 +653,9 @@ class E4M3Matrix:
             self.desc.data = self.buf.data_ptr()
             st = _here(codes, scales, self.buf)
             _check(lib().sdd_e4m3_matrix_load(C.byref(self.desc), codes.data_ptr(), scales.data_ptr(), st))
+        if stream is not None:  # (memory that is dropped goes back to the stream it came from, which knows nothing of this one)
+            codes.record_stream(stream)
+            scales.record_stream(stream)
         self._desc = C.byref(self.desc)
 
     def workspace(self, max_rows: int) -> torch.Tensor:
