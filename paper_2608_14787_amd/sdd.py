@@ -505,6 +505,14 @@ class PagePool:
 _SCALES = {"f32": (F32, torch.float32), "e8m0": (E8M0, torch.float8_e8m0fnu)}
 
 
+_INT_MAX = (1 << 31) - 1
+
+
+def _too_large(*sizes):
+    """Refuses sizes that a C int does not hold: ctypes would cut them to their lowest 32 bits and say nothing."""
+    raise SDDError(EINVAL, f"sizes {sizes} are past 2^31 - 1")
+
+
 def _scale_code(t: torch.Tensor) -> int:
     if t.dtype == torch.float32:
         return F32
@@ -542,6 +550,8 @@ def _rows2(x, name):
     if x.dim() != 2 or x.shape[0] == 0 or x.stride(1) != 1:
         raise ValueError(f"{name} must be [rows, columns] with unit column stride")
     M, K = x.shape
+    if M > _INT_MAX or K > _INT_MAX:
+        _too_large(M, K)
     return M, K, x.stride(0) if M > 1 else K, _dtype_code(x)
 
 
@@ -642,6 +652,8 @@ class E4M3Matrix:
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, stream=None):
         _codes(codes, "codes")
         N, K = codes.shape
+        if N > _INT_MAX or K > _INT_MAX:
+            _too_large(N, K)
         sd = _scale_code(scales)
         _need(scales.is_contiguous() and tuple(scales.shape) == (-(-N // 128), -(-K // 128)),
               "scales must be contiguous [ceil(N / 128), ceil(K / 128)]")
@@ -660,6 +672,8 @@ class E4M3Matrix:
 
     def workspace(self, max_rows: int) -> torch.Tensor:
         """Workspace for products of up to max_rows rows on this matrix, one call at a time."""
+        if not -_INT_MAX <= max_rows <= _INT_MAX:
+            _too_large(max_rows)
         n = _size_out(lib().sdd_e4m3_matmul_workspace_bytes, self._desc, max_rows)
         return self.buf.new_empty(n)
 
@@ -678,6 +692,8 @@ class E4M3Matrix:
         M = codes.shape[0]
         if codes.shape[1] != K:
             raise ValueError(f"codes must be [M, {K}]")
+        if M > _INT_MAX:
+            _too_large(M)
         if not scales.is_contiguous() or scales.shape != (self.blocks, M):
             raise ValueError(f"scales must be contiguous [{self.blocks}, {M}]")
         sd = _scale_code(scales)
