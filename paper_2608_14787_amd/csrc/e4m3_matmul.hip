@@ -478,20 +478,24 @@ __global__ void __launch_bounds__(256) join_kernel(MatArgs a) {
 // 264 x 10240 x 5120 27 (31 by itself).
 
 // 16 bytes a lane from descriptor rs at voffset + soffset to LDS at `to` + 16 lane.  Not the builtin: behind that the compiler
-// holds every LDS read back until all such loads have landed, those of the other buffer too.
+// holds every LDS read back until all such loads have landed, those of the other buffer too.  m0 is the compiler's own register: it sets
+// it for each use of its own, and has to hear that it changes here (that is what it warns of).
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ inline void load_direct(u32x4 rs, uint32_t to, int voffset, int soffset) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(voffset), "s"(rs), "s"(soffset)
-               : "memory");
+               : "memory", "m0");
 }
 template <bool BYTE>  // a word a lane to `to` + 4 lane: four bytes of memory, or one
 __device__ inline void load_direct_word(u32x4 rs, uint32_t to, int voffset, int soffset) {
   if constexpr (BYTE)
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_ubyte %1, %2, %3 offen lds" ::"s"(to), "v"(voffset), "s"(rs), "s"(soffset)
-                 : "memory");
+                 : "memory", "m0");
   else
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds" ::"s"(to), "v"(voffset), "s"(rs), "s"(soffset)
-                 : "memory");
+                 : "memory", "m0");
 }
+#pragma clang diagnostic pop
 __device__ inline u32x4 descriptor(const void* p, int bytes) {
   const uint64_t at = (uint64_t)p;
   return u32x4{(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)bytes, (uint32_t)kBufferRsrcWord3};
