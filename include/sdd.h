@@ -430,7 +430,8 @@ int sdd_e4m3_matmul_workspace_bytes(const sdd_e4m3_matrix* m, int M, size_t* byt
  * Products of a block are summed by the matrix cores, blocks in fp32 with xs ws.  That is
  * one fp32 product and has to lie in fp32's range (past it: infinity, and NaN where a block's sum is
  * 0; below it: 0), but where both scales are SDD_E8M0: then it is the sum times both that counts
- * (of scales with a product up to 2^200).  The result is rounded once.
+ * (of scales with a product up to 2^200), and bf16 results of more than 128 rows (of matrices up to
+ * 32768 rows: 64) have their blocks added in the matrix cores too.  The result is rounded once.
  * Of fp32 results, and of up to 16 rows, all sums are fp32.  Of bf16 results of more rows each
  * group of 8 columns (8 i .. 8 i + 7) has its products cut toward zero at 2^(E - 13), E the largest
  * sum of two codes' exponents in it: the group is off by less than 7 2^-13 of its largest |product|.  That is

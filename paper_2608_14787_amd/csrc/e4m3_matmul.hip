@@ -11,11 +11,15 @@
 // it.  bf16 results of more than 16 rows take them, at half the time of bf16 products.  fp32 results, and those of up to 16 rows, which
 // wait for memory anyway, widen the codes to bf16, exactly, and sum in fp32.
 // Where both scales are powers of two the fp8 instruction takes them; in tiles of many rows it then also adds to the accumulators,
-// and no fp32 work is left beside the products (4095 x 51200 x 5120 920 us, 1048 with fp32 scales).  Widened codes take the
+// and no fp32 work is left beside the products (4095 x 51200 x 5120 916 us, 1051 with fp32 scales).  Widened codes take the
 // matrix's scale with them.
 //
 // Bound: up to about 300 rows the matrix's bytes (6.3 to 6.8 TB/s of a plain read stream on this card), then the products (2.5
-// to 3.1 PFLOP/s in large library products of fp8).
+// PFLOP/s in a library product of fp8 of 8192^3, 3.1 of 16384^3).
+//
+// Times in this file: a call among others in a captured graph, matrices in turn that together pass the caches; "alone" a kernel's
+// own time where each launch stands alone.  Where the matrices lie in memory makes up to a fifth: 33 x 51200 x 5120 takes 43 us from
+// some buffers and 54 from others, so that only times of one sentence compare.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -90,8 +94,9 @@ __device__ inline void store4(const MatArgs& a, int m, int n, const f32x4& v) {
 //
 // A workgroup takes NT row tiles of the matrix and all (up to 16) rows; its eight waves take every eighth block of 128
 // columns, each its own loads (no barrier in the loop), and join in LDS in wave order.  Bound by the matrix's bytes: each is read
-// once, 1 KiB of a wave at a time, past the caches (nothing else reads them).  1 x 51200 x 5120 46 us (5.7 TB/s), 1 x 18944 x 3584 15
-// (4.5), 1 x 4608 x 3584 6.5.  Two blocks of a wave in registers: with three these take 47, 17 and 7.3, with four 58, 18 and 7.7.
+// once, 1 KiB of a wave at a time, past the caches (nothing else reads them).  1 x 51200 x 5120 45 us (5.8 TB/s), 1 x 18944 x 3584 16
+// (4.3), 1 x 4608 x 3584 7.0 (5.8 alone).  Two blocks of a wave in registers: 46, 15 and 6.5 against 47, 17 and 7.3 with three and 58, 18
+// and 7.7 with four.
 
 constexpr int kFewWaves = 8, kFewRows = 4;
 
@@ -190,8 +195,9 @@ __global__ void __launch_bounds__(kFewWaves * kWave, 2) few_rows_kernel(MatArgs 
 // A workgroup of 8 / GK x GK waves takes NT row tiles of the matrix a wave, all of up to 16 MT rows, and a part of K.  The rows'
 // codes pass through LDS, CB blocks of columns at a time in two buffers, so that they are read from L2 once a workgroup (loaded in
 // the operands' order, 16 rows of 64 bytes a load, a compute unit gets 15 bytes a clock from L2; whole lines 50); a
-// wave's own tiles go from memory to registers, R - 1 blocks ahead.  33 x 51200 x 5120 42 us (6.2 TB/s of the matrix; read by
-// each wave alone 74), 33 x 5120 x 25600 26 + 4.7 in the join (62 with the columns in one part).  Of a chunk's blocks each of the GK waves of a tile takes
+// wave's own tiles go from memory to registers, R - 1 blocks ahead.  33 x 51200 x 5120 42 us alone (6.2 TB/s of the matrix; rows read
+// by each wave 74), 43 to 54 among others; 33 x 5120 x 25600 in fp32 27 and 4.5 in the join alone (62 with the columns in one part), 34 among
+// others; 33 x 10240 x 5120 17, 33 x 5120 x 8192 15, of 16 rows 15 and 13.  Of a chunk's blocks each of the GK waves of a tile takes
 // every GK-th; they join in LDS, in their order.
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
@@ -472,10 +478,10 @@ __global__ void __launch_bounds__(256) join_kernel(MatArgs a) {
 // A workgroup of GN x GM waves takes 16 WN GN rows of the matrix and 16 WM GM of the activations; both pass through LDS a block
 // of columns at a time, in a ring of RS that is loaded directly.  Scales come eight blocks at a time.
 // Bound by the products: 256 x 256 reads LDS 96 KiB for 256 products of 16x16x128, 32 clocks each on four cores, half of what LDS
-// could give meanwhile, and L2 64 KiB at 55 bytes a clock.  4095 x 51200 x 5120 1030 us (2.1 PFLOP/s), with powers of two as scales
-// 920 (2.3; 4096 x 8192 x 8192 218, 2.5), fp32 results 4095 x 5120 x 25600 937 (1.15: bf16 products).  At 128 x 128 loads, LDS
-// and products take about as long each and overlap only in part: 511 x 3584 x 18944 39 us and 6.5 in the join (1.5 PFLOP/s),
-// 264 x 10240 x 5120 27 (31 by itself).
+// could give meanwhile, and L2 64 KiB at 55 bytes a clock.  4095 x 51200 x 5120 1051 us (2.0 PFLOP/s), with powers of two as scales
+// 916 (2.3; 4096 x 8192 x 8192 216, 2.5), fp32 results 4095 x 5120 x 25600 915 (1.17: bf16 products).  At 128 x 128 loads, LDS
+// and products take about as long each and overlap only in part: 511 x 3584 x 18944 with powers of two 56 us, alone 40 and 6.5 in the
+// join; 264 x 10240 x 5120 31.
 
 // 16 bytes a lane from descriptor rs at voffset + soffset to LDS at `to` + 16 lane.  Not the builtin: behind that the compiler
 // holds every LDS read back until all such loads have landed, those of the other buffer too.  m0 is the compiler's own register: it sets
@@ -535,8 +541,8 @@ __global__ void __launch_bounds__(kWave * GN * GM, 2) many_rows_kernel(MatArgs a
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   const int n_blocks = (a.NT * 16 + BN - 1) / BN, m_blocks = (a.M + BM - 1) / BM;
   // Workgroups go to the XCDs in turn.  One XCD's, in their order: kStripe blocks of the matrix's rows, all blocks of the
-  // activations in turn, so that the 32 at work together share both in its L2 (4095 x 51200 x 5120: stripes of 2 1110 us, 4 1064,
-  // 6 to 16 1048).
+  // activations in turn, so that the 32 at work together share both in its L2 (4095 x 51200 x 5120: stripes of 2 1101 us, 4 1061,
+  // 6 to 16 1045 to 1052).
   const int low = blockIdx.x % kXcds, at = blockIdx.x / kXcds;
   const int stripe = at / (kStripe * m_blocks), in = at - stripe * kStripe * m_blocks;
   const int wide = min(kStripe, (n_blocks * a.splits + kXcds - 1) / kXcds - stripe * kStripe);
@@ -752,8 +758,10 @@ int row_class(int M) {
 // Many rows: the tile and the parts of K with the least time by the steps that the busiest compute unit takes.  Measured, us a
 // step of 128 columns: tiles of 256 x 256 1.35 alone and 2.0 on a full device; of 128 x 128 with four waves (two workgroups a
 // compute unit) 0.80 alone, 0.88 with one everywhere, 1.17 with two; with eight waves and a deep ring 0.53 alone and 0.72.  The
-// matrix at 6 TB/s, parts written and read at 4.5, 4 us a launch.  Over 24 shapes of 200 to 1023 rows the choice is 1.4% from the best
-// on average; of fp32 results, whose steps take longer, over 10 shapes of 100 to 2048 rows 6% at most.
+// matrix at 6 TB/s, parts written and read at 4.5, 4 us a launch.  Over 24 shapes of 200 to 1023 rows the choice is
+// the best or within 1% of it at 17; 5% from it on average and 56% at the most (264 x 3584 x 18944 66 us for 42.5, 700 x 3584 x 18944 92 for
+// 71): where the parts do not divide by the XCDs, some get a workgroup more than they have places, which is not counted here.  Of fp32
+// results, whose steps take longer, over 10 shapes of 100 to 2048 rows 0.8% on average and 4% at the most.
 Plan plan_many(int M, int NT, int KB, bool f32) {
   Plan best = {Plan::kTile128, 0, 0, 0, 1, KB};
   double least = 1e30;
@@ -776,16 +784,16 @@ Plan plan_many(int M, int NT, int KB, bool f32) {
   return best;
 }
 // Up to 128 rows, measured in us:
-// Up to 4 rows: no barrier and no second launch, but a workgroup has its tiles to itself: 1 x 4608 x 3584 6.5 (shared 7.5),
-// 1 x 8192 x 5120 9.7 (11.8), 1 x 3584 x 18944 14.1 (16.7).  Not between 256 and 512 tiles, where some compute units get two
-// workgroups and others one, and a long row: 1 x 5120 x 25600 30.9 (26.4).  Above 4 the rows are read too often:
-// 16 x 51200 x 5120 55.3 (51.4), 16 x 5120 x 25600 41.6 (26.4).
-// Tiles a wave of shared rows: two from 2048 row tiles on (33 x 51200 x 5120 48.5, with one 52.9); at 2048 one tile a wave makes 256
-// workgroups (33 x 32768 x 4096 27.7, with two 34.6).
-// Waves on one tile: four where there are few tiles and blocks (33 x 8192 x 4096 10.9, cut over K and joined 14.4; 33 x 5120 x 8192
-// 16.5 and 14.7).
-// 65 to 128 rows: shared where that is one launch of two tiles a wave (128 x 51200 x 5120 66, many rows' kernel 73); else many
-// rows' (128 x 10240 x 5120 25.6, shared 28.4; fp32 results 128 x 51200 x 5120 91 and 111).
+// Up to 4 rows: no barrier and no second launch, but a workgroup has its tiles to itself: 1 x 4608 x 3584 7.0 (shared 8.1),
+// 1 x 8192 x 5120 9.8 (11.3), 1 x 3584 x 18944 13.5 (15.1).  Not between 256 and 512 tiles, where some compute units get two
+// workgroups and others one, and a long row: 1 x 5120 x 25600 30.6 (25.3).  Above 4 the rows are read too often:
+// 16 x 51200 x 5120 51.3 (46.9), 16 x 5120 x 25600 37.3 (29.6).
+// Tiles a wave of shared rows: two from 2048 row tiles on (33 x 51200 x 5120 48.0, with one 52.7); at 2048 one tile a wave makes 256
+// workgroups (33 x 32768 x 4096 28.6, with two 34.2).
+// Waves on one tile: four where there are few tiles and blocks (33 x 8192 x 4096 12.0, cut over K and joined 14.7; 33 x 5120 x 8192
+// 16.8 and 15.3).
+// 65 to 128 rows: shared where that is one launch of two tiles a wave (128 x 51200 x 5120 62, many rows' kernel 74); else many
+// rows' (128 x 10240 x 5120 25.2, shared 29.5; fp32 results 128 x 51200 x 5120 83 and 115).
 Plan plan_of(int M, int NT, int KB, bool f32) {
   M = row_class(M);
   if (M <= kFewRows && !(NT > 256 && NT < 512 && KB > 64)) return Plan{Plan::kFew, 1, NT >= 512 ? 2 : 1, 1, 1, KB};
